@@ -218,6 +218,86 @@ dgq_status dgq_self_attn_logq(const void* Q, const void* K, const void* V, int B
                               int score_bits, const float* fixed_scale, void* O, uint8_t* codes_out, void* stream);
 dgq_status dgq_cross_attn_workspace_bytes(int B, int H, int nq, int nk, int d, size_t* bytes);
 
+/* ---------------------------------------------------------------- attention over an encoder's states and over an 8-bit cache
+ * (The paper leaves text keys and values as they come from the encoder: one length, 16 bits.  The calls of this section
+ * are this library's own: prompts of different lengths, and their keys and values kept in 8 bits over all steps.)
+ * Like the hot-path calls above, all of them only enqueue work on `stream`: they allocate nothing, need no workspace and
+ * do not synchronise.  Work goes to the current device, where all memory has to be. */
+
+/* element type of the 16-bit tensors */
+enum { DGQ_F16 = 0, DGQ_BF16 = 1 };
+
+/* A 16-bit tensor [batch, tokens, heads, d], dev.  The d values of a row lie next to each other; the strides count
+ * elements and may be those of a view (a slice of a fused projection, [batch, heads, tokens, d] storage).  `ptr` is 16-byte
+ * aligned and strides are multiples of 8, else DGQ_ERR_ALIGNMENT; the stride of a dimension of size 1 is ignored.  Of
+ * tensors that are read, batch and head strides may be 0 (one prompt's states for a whole batch); no stride is negative. */
+typedef struct {
+  void* ptr;
+  int64_t batch, token, head;
+} dgq_rows;
+
+/* O[b, i, h] = sum_j softmax_j(scale Q[b, i, h] . K[b, j, h / (Hq / Hkv)]) V[b, j, h / (Hq / Hkv)] over the first
+ * kv_lens[b] of the nk keys (dev int32 [B]; values outside 0..nk are taken as the nearer end; NULL: all nk), with scores and
+ * softmax statistics in fp32 and weights rounded to the tensors' type for the product.  A request without keys gives zeros.
+ * What K and V hold behind kv_lens[b] may be anything, NaN included.  Q, O [B, nq, Hq, d]; K, V [B, nk, Hkv, d]; Hq a
+ * multiple of Hkv; d a multiple of 8 up to 160; any nq, nk >= 1.
+ * Errors: INVALID_ARG (also: a zero or negative stride where none may be, scale not finite), ALIGNMENT, UNSUPPORTED, CUDA. */
+dgq_status dgq_encoder_attn(const dgq_rows* Q, const dgq_rows* K, const dgq_rows* V, const dgq_rows* O, int dtype, int B,
+                            int Hq, int Hkv, int nq, int nk, int d, float scale, const int32_t* kv_lens, void* stream);
+
+/* A paged key/value cache in the caller's memory (codes 16-byte aligned).  Codes: dev int8 [n_pages, n_heads, page, row], row = d
+ * rounded up to a multiple of 16; a value is code * scale with one fp32 scale for each page and head, dev [n_pages, n_heads].
+ * page is 16, 32, 64 or 128; d a multiple of 8 up to 160; n_pages * page < 2^31.  Slot s is row s % page of page s / page. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int n_pages, n_heads, page, d;
+} dgq_kv_cache;
+
+/* Block tables and slot maps from lengths.  B requests hold lens[b] tokens and get n_new[b] more (dev int32 [B]).  Entry i
+ * of block_table[b] (dev int32 [B, max_pages]) is the page of tokens i * page .. : the pages that request b lacks are taken
+ * from the front of free_pages (dev int32 [n_free]) in the order of the requests and entered behind those it has; other
+ * entries stay as they are.  Written: token_start[B + 1] (prefix sums of n_new: where each request's rows begin in a
+ * packed batch), kv_lens[B] = lens + n_new, slots[n_slots] (the slot of every new token in that order; -1 behind the last
+ * one) and used[1] = free pages taken.
+ * What does not fit is found on the device, which records DGQ_ERR_INVALID_ARG in the status word: negative lengths count
+ * as 0, lengths beyond max_pages * page as that, a page that free_pages has no more entry for becomes -1, as do the slots of the
+ * tokens concerned and of those beyond n_slots or the table.
+ * The outputs may not overlap lens and n_new.  Errors: INVALID_ARG, UNSUPPORTED (page), CUDA. */
+dgq_status dgq_kv_plan(const int32_t* lens, const int32_t* n_new, int B, const int32_t* free_pages, int n_free,
+                       int32_t* block_table, int max_pages, int page, int32_t* token_start, int32_t* kv_lens, int32_t* slots,
+                       int n_slots, int32_t* used, void* stream);
+
+/* Rows K[t], V[t] (t < T; [1, T, n_heads, d]) into slots[t] (dev int32 [T]; negative: the row is skipped).  The rows of one page
+ * stand next to each other in ascending order, as dgq_kv_plan gives them, and no slot comes twice in a call.  For each page and
+ * head, in fp32: top = max |x| over the page's rows of this call, s = top * (1 / 127); a page whose row 0 is among them forgets what it
+ * held, any other one keeps its rows below the first new one: s = max(s, scale), and where s has grown, their codes become
+ * clamp(rint(code * scale / s), -127, 127).  New codes are clamp(rint(x / s), -127, 127), 0 where s is 0.  Rows behind the
+ * new ones stay as they are.  Inputs must be finite.  A slot beyond the cache is skipped and recorded as
+ * DGQ_ERR_INVALID_ARG in the status word.
+ * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED, CUDA. */
+dgq_status dgq_kv_write(const dgq_kv_cache* cache, const dgq_rows* K, const dgq_rows* V, int dtype, int64_t T,
+                        const int32_t* slots, void* stream);
+
+/* The rows of slots[t] as the values they stand for, code * scale rounded to `dtype`, into K[t], V[t] ([1, T, n_heads, d]):
+ * contiguous keys and values again, as dgq_cross_attn_logq takes them.  A negative slot gives zeros, one beyond the cache too
+ * (and DGQ_ERR_INVALID_ARG in the status word).  Errors: as above. */
+dgq_status dgq_kv_read(const dgq_kv_cache* cache, const int32_t* slots, int64_t T, const dgq_rows* K, const dgq_rows* V,
+                       int dtype, void* stream);
+
+/* Attention as in dgq_encoder_attn over the first kv_lens[b] tokens of each request's pages (block_table dev int32
+ * [B, max_pages], kv_lens dev int32 [B]; lengths outside 0 .. max_pages * page are taken as the nearer end).
+ * q_start NULL: Q, O [B, max_nq, Hq, d].  Else Q, O [1, n_rows, Hq, d] packed: request b has rows q_start[b] .. q_start[b + 1] - 1
+ * (dev int32 [B + 1], ascending), at most max_nq of them; other rows of O stay as they are.  causal != 0: row i of n sees the first
+ * kv_lens[b] - n + i + 1 tokens (the n queries belong to the last n tokens).  Hq a multiple of cache->n_heads.  Pages may be
+ * shared by requests.  Weights are rounded to fp16 for the product with the codes, whatever `dtype` is.
+ * Found on the device and recorded as DGQ_ERR_INVALID_ARG in the status word: table entries outside the cache (their tokens
+ * count as absent), more than max_nq rows or rows beyond n_rows (left out).  n_rows is ignored where q_start is NULL.
+ * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED, CUDA. */
+dgq_status dgq_cached_attn(const dgq_kv_cache* cache, const dgq_rows* Q, const dgq_rows* O, int dtype, int B, int Hq,
+                           int64_t n_rows, const int32_t* q_start, int max_nq, const int32_t* block_table, int max_pages,
+                           const int32_t* kv_lens, int causal, float scale, void* stream);
+
 /* ---------------------------------------------------------------- cross-attention without a caller workspace
  * (The paper has no counterpart: this is a deployment convenience of this library.)
  * Same computation, arguments and results as dgq_cross_attn_logq, for callers that

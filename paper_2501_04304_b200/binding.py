@@ -28,7 +28,8 @@ EXPORTS = [
     "dgq_calibrate_groups", "dgq_groups_from_host", "dgq_groups_destroy", "dgq_groups_info",
     "dgq_groups_export", "dgq_quantize_act", "dgq_weight_prepare", "dgq_weight_from_codes",
     "dgq_weight_destroy", "dgq_weight_export", "dgq_linear", "dgq_linear_workspace_bytes", "dgq_cross_attn_logq", "dgq_cross_attn_logq_qv", "dgq_self_attn_logq",
-    "dgq_cross_attn_workspace_bytes", "dgq_cross_attn_logq_noalloc", "dgq_selftest_wait_timeout", "dgq_device_status", "dgq_status_string", "dgq_launch_count",
+    "dgq_cross_attn_workspace_bytes", "dgq_cross_attn_logq_noalloc",
+    "dgq_encoder_attn", "dgq_kv_plan", "dgq_kv_write", "dgq_kv_read", "dgq_cached_attn", "dgq_selftest_wait_timeout", "dgq_device_status", "dgq_status_string", "dgq_launch_count",
 ]
 
 
@@ -298,6 +299,76 @@ def self_attn_logq(Q, K, V, score_bits=8, fixed_scale=None, out=None, want_codes
     r = (_native or native()).self_attn_logq(Q, K, V, score_bits, fixed_scale, out, bool(want_codes), stream)
     if type(r) is int:
         _check(r, "dgq_self_attn_logq")
+    return r
+
+
+def encoder_attn(Q, K, V, kv_lens=None, scale=None, out=None, stream=None):
+    """dgq_encoder_attn: softmax(scale Q K^T) V over the first kv_lens[b] keys (all of them for None), scale 1 / sqrt(d) by default.
+    Q [B, nq, Hq, d], K, V [B, nk, Hkv, d] CUDA fp16 or bf16, rows of d contiguous, other strides any multiples of 8;
+    kv_lens CUDA int32 [B].  Returns O [B, nq, Hq, d]."""
+    r = (_native or native()).encoder_attn(Q, K, V, kv_lens, scale, out, stream)
+    if type(r) is int:
+        _check(r, "dgq_encoder_attn")
+    return r
+
+
+class KvCache:
+    """A paged 8-bit key/value cache: int8 codes k, v [pages, heads, page, row] (rows of d codes, padded to a multiple of 16)
+    and fp32 scales k_scale, v_scale [pages, heads], all contiguous CUDA tensors of the caller."""
+
+    def __init__(self, k, v, k_scale, v_scale, d):
+        self.k, self.v, self.k_scale, self.v_scale, self.d = k, v, k_scale, v_scale, d
+
+    @classmethod
+    def empty(cls, n_pages, n_heads, page, d, device="cuda"):
+        row = (d + 15) // 16 * 16
+        k, v = (torch.zeros(n_pages, n_heads, page, row, dtype=torch.int8, device=device) for _ in range(2))
+        k_scale, v_scale = (torch.zeros(n_pages, n_heads, device=device) for _ in range(2))
+        return cls(k, v, k_scale, v_scale, d)
+
+    @property
+    def page(self):
+        return self.k.shape[2]
+
+
+def kv_plan(lens, n_new, free_pages, block_table, page, n_tokens, stream=None):
+    """dgq_kv_plan: enters the pages that the new tokens need into `block_table` (int32 [B, max_pages], in place), taken from the front
+    of `free_pages`.  Returns (token_start [B + 1], kv_lens [B], slots [n_tokens], used [1]), all int32 on the GPU; slots
+    behind the last new token are -1."""
+    r = (_native or native()).kv_plan(lens, n_new, free_pages, block_table, page, n_tokens, stream)
+    if type(r) is int:
+        _check(r, "dgq_kv_plan")
+    return r
+
+
+def kv_write(cache: KvCache, K, V, slots, stream=None):
+    """dgq_kv_write: rows K, V [T, heads, d] (fp16 or bf16) into the cache's slots [T] (int32), as kv_plan lays them out."""
+    r = (_native or native()).kv_write(cache.k, cache.v, cache.k_scale, cache.v_scale, cache.d, K, V, slots, stream)
+    if type(r) is int:
+        _check(r, "dgq_kv_write")
+
+
+def kv_read(cache: KvCache, slots, dtype=torch.float16, out=None, stream=None):
+    """dgq_kv_read: the values of slots [T] (int32) as (K, V) [T, heads, d] of `dtype`; zeros for a negative slot.  `out`: (K, V)."""
+    k, v = out if out is not None else (None, None)
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise ValueError("dtype is torch.float16 or torch.bfloat16")
+    r = (_native or native()).kv_read(cache.k, cache.v, cache.k_scale, cache.v_scale, cache.d, slots, dtype is torch.bfloat16, k, v,
+                                      stream)
+    if type(r) is int:
+        _check(r, "dgq_kv_read")
+    return r
+
+
+def cached_attn(Q, cache: KvCache, block_table, kv_lens, q_start=None, max_nq=None, causal=False, scale=None, out=None, stream=None):
+    """dgq_cached_attn: attention over the first kv_lens[b] (int32 [B]) tokens of each request's pages (block_table int32
+    [B, max_pages]).  Q [B, nq, Hq, d], or packed [rows, Hq, d] with q_start (int32 [B + 1]) and at most max_nq rows a request
+    (default: as many as there are; rows outside every request are not written).  causal: the queries are the last tokens.
+    Returns O like Q."""
+    r = (_native or native()).cached_attn(cache.k, cache.v, cache.k_scale, cache.v_scale, cache.d, Q, block_table, kv_lens, q_start,
+                                          max_nq, bool(causal), scale, out, stream)
+    if type(r) is int:
+        _check(r, "dgq_cached_attn")
     return r
 
 

@@ -6,10 +6,13 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+
+#include <cmath>
 
 #include "../../include/dgq.h"
 
@@ -264,12 +267,292 @@ PyObject* self_attn_logq(PyObject* const* a, Py_ssize_t n) {
   return tuple({output(a[5], o), wrap(codes)});
 }
 
+// ---------------------------------------------------------------- attention over encoder states and over the 8-bit cache
+// These calls go to the device of their first tensor, whichever is current, and check shapes before the library sees a pointer.
+
+bool fail(const char* what) {
+  PyErr_SetString(PyExc_ValueError, what);
+  return false;
+}
+
+// Type, device, innermost stride and (for its two or three outer dimensions) the strides of a 16-bit tensor.
+bool rows16(const at::Tensor& t, const at::Tensor& like, int64_t dims, const char* what, dgq_rows* r) {
+  if (!t.defined() || !t.is_cuda() || t.device() != like.device() || t.scalar_type() != like.scalar_type() || t.dim() != dims ||
+      (t.scalar_type() != at::kHalf && t.scalar_type() != at::kBFloat16) || (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1))
+    return fail(what);
+  *r = dgq_rows{t.data_ptr(), dims == 4 ? t.stride(0) : 0, t.stride(dims - 3), t.stride(dims - 2)};
+  return true;
+}
+
+bool ints(const at::Tensor& t, const at::Tensor& like, const char* what) {
+  if (!t.is_cuda() || t.device() != like.device() || t.scalar_type() != at::kInt || !t.is_contiguous()) return fail(what);
+  return true;
+}
+
+bool fits(int64_t v, int* out) {
+  if (v > INT32_MAX) return fail("a size is beyond 2^31");
+  *out = static_cast<int>(v);
+  return true;
+}
+
+int dtype_of(const at::Tensor& t) { return t.scalar_type() == at::kBFloat16 ? DGQ_BF16 : DGQ_F16; }
+
+// The stream for a call on `like`'s device: the given one or that device's current one.
+bool stream_on(PyObject* o, const at::Tensor& like, void** st) {
+  if (o == Py_None) {
+    *st = c10::cuda::getCurrentCUDAStream(like.device().index()).stream();
+    return true;
+  }
+  return stream_arg(o, st);
+}
+
+// An output made here that a stream other than the current one writes: torch gives its memory to nobody else before that has
+// happened, even if the caller drops it.
+void on_stream(const at::Tensor& t, PyObject* given, void* st) {
+  if (given != Py_None)
+    c10::cuda::CUDACachingAllocator::recordStream(
+        t.storage().data_ptr(), c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(st), t.device().index()));
+}
+
+bool scale_arg(PyObject* o, int64_t d, float* scale) {
+  if (o == Py_None) {
+    *scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(d)));
+    return true;
+  }
+  const double v = PyFloat_AsDouble(o);
+  if (v == -1.0 && PyErr_Occurred()) return false;
+  *scale = static_cast<float>(v);
+  return true;
+}
+
+// (k, v, k_scale, v_scale, d): codes [pages, heads, page, row], scales [pages, heads]
+bool cache_arg(PyObject* const* a, at::Tensor* k, dgq_kv_cache* c) {
+  at::Tensor v, ks, vs;
+  if (!tensor(a[0], k) || !tensor(a[1], &v) || !tensor(a[2], &ks) || !tensor(a[3], &vs) || !integer(a[4], &c->d)) return false;
+  if (!k->defined() || !v.defined() || !ks.defined() || !vs.defined() || !k->is_cuda() || k->dim() != 4 || v.sizes() != k->sizes() ||
+      ks.dim() != 2 || ks.size(0) != k->size(0) || ks.size(1) != k->size(1) || vs.sizes() != ks.sizes() ||
+      k->scalar_type() != at::kChar || v.scalar_type() != at::kChar || ks.scalar_type() != at::kFloat ||
+      vs.scalar_type() != at::kFloat || !k->is_contiguous() || !v.is_contiguous() || !ks.is_contiguous() || !vs.is_contiguous() ||
+      v.device() != k->device() || ks.device() != k->device() || vs.device() != k->device())
+    return fail("a cache is contiguous CUDA int8 codes [pages, heads, page, row] and fp32 scales [pages, heads]");
+  if (c->d <= 0 || k->size(3) != (c->d + 15) / 16 * 16) return fail("a cache's rows are d codes rounded up to a multiple of 16");
+  int page;
+  if (!fits(k->size(0), &c->n_pages) || !fits(k->size(1), &c->n_heads) || !fits(k->size(2), &page)) return false;
+  c->page = page;
+  c->k = k->data_ptr();
+  c->v = v.data_ptr();
+  c->k_scale = static_cast<float*>(ks.data_ptr());
+  c->v_scale = static_cast<float*>(vs.data_ptr());
+  return true;
+}
+
+// (Q, K, V, kv_lens | None, scale | None, out | None, stream) -> O
+PyObject* encoder_attn(PyObject* const* a, Py_ssize_t n) {
+  void* st;
+  at::Tensor q, k, v, lens, o;
+  dgq_rows rq, rk, rv, ro;
+  float scale;
+  if (!arity(n, 7) || !tensor(a[0], &q) || !tensor(a[1], &k) || !tensor(a[2], &v) || !tensor(a[3], &lens) || !tensor(a[5], &o)) return nullptr;
+  if (!rows16(q, q, 4, "Q is a CUDA fp16 or bf16 tensor [B, nq, Hq, d] with contiguous rows", &rq) ||
+      !rows16(k, q, 4, "K is a tensor [B, nk, Hkv, d] of Q's type and device with contiguous rows", &rk) ||
+      !rows16(v, q, 4, "V is a tensor [B, nk, Hkv, d] of Q's type and device with contiguous rows", &rv))
+    return nullptr;
+  int B, nq, hq, d, nk, hkv;
+  if (!fits(q.size(0), &B) || !fits(q.size(1), &nq) || !fits(q.size(2), &hq) || !fits(q.size(3), &d) || !fits(k.size(1), &nk) ||
+      !fits(k.size(2), &hkv))
+    return nullptr;
+  if ((k.size(0) != B || k.size(3) != d || v.sizes() != k.sizes()) && !fail("K and V are [B, nk, Hkv, d] with Q's B and d")) return nullptr;
+  if (lens.defined() && (!ints(lens, q, "kv_lens is a contiguous CUDA int32 tensor [B]") ||
+                         (lens.numel() != B && !fail("kv_lens has one length a request"))))
+    return nullptr;
+  if (!scale_arg(a[4], d, &scale)) return nullptr;
+  const c10::cuda::CUDAGuard on(q.device());
+  if (!stream_on(a[6], q, &st)) return nullptr;
+  if (!o.defined()) {
+    o = empty({B, nq, hq, d}, q.scalar_type(), q);
+    on_stream(o, a[6], st);
+  }
+  if (!rows16(o, q, 4, "out is a tensor like Q", &ro) || (o.sizes() != q.sizes() && !fail("out is a tensor like Q"))) return nullptr;
+  if (o.numel() == 0) return output(a[5], o);
+  if (nk == 0) {
+    if (st == c10::cuda::getCurrentCUDAStream().stream()) {
+      o.zero_();
+    } else {
+      c10::cuda::CUDAStreamGuard there(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(st), q.device().index()));
+      o.zero_();
+    }
+    return output(a[5], o);
+  }
+  const int32_t* p_lens = ptr<int32_t>(lens);
+  const int type = dtype_of(q);
+  dgq_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = dgq_encoder_attn(&rq, &rk, &rv, &ro, type, B, hq, hkv, nq, nk, d, scale, p_lens, st);
+  Py_END_ALLOW_THREADS
+  if (rc != DGQ_OK) return status(rc);
+  return output(a[5], o);
+}
+
+// (k, v, k_scale, v_scale, d, Q, block_table, kv_lens, q_start | None, max_nq | None, causal, scale | None, out | None, stream) -> O
+PyObject* cached_attn(PyObject* const* a, Py_ssize_t n) {
+  void* st;
+  dgq_kv_cache c;
+  at::Tensor kc, q, table, lens, start, o;
+  dgq_rows rq, ro;
+  float scale;
+  int causal, max_nq, B, hq, max_pages;
+  if (!arity(n, 14) || !cache_arg(a, &kc, &c) || !tensor(a[5], &q) || !tensor(a[6], &table) || !tensor(a[7], &lens) ||
+      !tensor(a[8], &start) || !integer(a[10], &causal) || !tensor(a[12], &o))
+    return nullptr;
+  const int dims = start.defined() ? 3 : 4;
+  if (!rows16(q, q, dims, "Q is a CUDA fp16 or bf16 tensor [B, nq, Hq, d] or, with q_start, [rows, Hq, d]; rows contiguous", &rq)) return nullptr;
+  if ((q.device() != kc.device() || q.size(dims - 1) != c.d) && !fail("Q has the cache's d and device")) return nullptr;
+  if ((!table.defined() || !lens.defined() || table.dim() != 2 || lens.dim() != 1 || lens.size(0) != table.size(0)) &&
+      !fail("block_table is [B, max_pages], kv_lens [B]"))
+    return nullptr;
+  if (!ints(table, q, "block_table is a contiguous CUDA int32 tensor") || !ints(lens, q, "kv_lens is a contiguous CUDA int32 tensor")) return nullptr;
+  if (!fits(table.size(0), &B) || !fits(table.size(1), &max_pages) || !fits(q.size(dims - 2), &hq)) return nullptr;
+  if (start.defined()) {
+    if (!ints(start, q, "q_start is a contiguous CUDA int32 tensor [B + 1]") || (start.numel() != B + 1ll && !fail("q_start is [B + 1]"))) return nullptr;
+    if (a[9] == Py_None) {
+      if (!fits(q.size(0), &max_nq)) return nullptr;
+    } else if (!integer(a[9], &max_nq)) {
+      return nullptr;
+    }
+  } else {
+    if (!fits(q.size(1), &max_nq) || (q.size(0) != B && !fail("Q has one entry a request"))) return nullptr;
+    if (a[9] != Py_None) {
+      int given;
+      if (!integer(a[9], &given) || (given != max_nq && !fail("max_nq is Q's own where there is no q_start"))) return nullptr;
+    }
+  }
+  if (!scale_arg(a[11], c.d, &scale)) return nullptr;
+  const c10::cuda::CUDAGuard on(q.device());
+  if (!stream_on(a[13], q, &st)) return nullptr;
+  if (!o.defined()) {
+    o = dims == 4 ? empty({B, max_nq, hq, c.d}, q.scalar_type(), q) : empty({q.size(0), hq, c.d}, q.scalar_type(), q);
+    on_stream(o, a[13], st);
+  }
+  if (!rows16(o, q, dims, "out is a tensor like Q", &ro) || (o.sizes() != q.sizes() && !fail("out is a tensor like Q"))) return nullptr;
+  if (o.numel() == 0 || B == 0) return output(a[12], o);
+  const int64_t n_rows = q.size(0);
+  const int32_t *p_table = ptr<int32_t>(table), *p_lens = ptr<int32_t>(lens), *p_start = ptr<int32_t>(start);
+  const int type = dtype_of(q);
+  dgq_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = dgq_cached_attn(&c, &rq, &ro, type, B, hq, n_rows, p_start, max_nq, p_table, max_pages, p_lens, causal, scale, st);
+  Py_END_ALLOW_THREADS
+  if (rc != DGQ_OK) return status(rc);
+  return output(a[12], o);
+}
+
+// (k, v, k_scale, v_scale, d, K, V, slots, stream) -> None
+PyObject* kv_write(PyObject* const* a, Py_ssize_t n) {
+  void* st;
+  dgq_kv_cache c;
+  at::Tensor kc, k, v, slots;
+  dgq_rows rk, rv;
+  if (!arity(n, 9) || !cache_arg(a, &kc, &c) || !tensor(a[5], &k) || !tensor(a[6], &v) || !tensor(a[7], &slots)) return nullptr;
+  if (!rows16(k, k, 3, "K is a CUDA fp16 or bf16 tensor [T, heads, d] with contiguous rows", &rk) ||
+      !rows16(v, k, 3, "V is a tensor [T, heads, d] of K's type and device with contiguous rows", &rv))
+    return nullptr;
+  if ((k.device() != kc.device() || v.sizes() != k.sizes() || k.size(1) != c.n_heads || k.size(2) != c.d || !slots.defined() ||
+       slots.numel() != k.size(0)) &&
+      !fail("K and V are [T, heads, d] of the cache's heads, d and device, slots [T]"))
+    return nullptr;
+  if (!ints(slots, k, "slots is a contiguous CUDA int32 tensor [T]")) return nullptr;
+  const int64_t T = k.size(0);
+  if (T == 0) Py_RETURN_NONE;
+  const c10::cuda::CUDAGuard on(k.device());
+  if (!stream_on(a[8], k, &st)) return nullptr;
+  const int32_t* p_slots = ptr<int32_t>(slots);
+  const int type = dtype_of(k);
+  dgq_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = dgq_kv_write(&c, &rk, &rv, type, T, p_slots, st);
+  Py_END_ALLOW_THREADS
+  if (rc != DGQ_OK) return status(rc);
+  Py_RETURN_NONE;
+}
+
+// (k, v, k_scale, v_scale, d, slots, bf16, K | None, V | None, stream) -> (K, V)
+PyObject* kv_read(PyObject* const* a, Py_ssize_t n) {
+  void* st;
+  dgq_kv_cache c;
+  at::Tensor kc, slots, out[2];
+  dgq_rows r[2];
+  int bf16;
+  if (!arity(n, 10) || !cache_arg(a, &kc, &c) || !tensor(a[5], &slots) || !integer(a[6], &bf16) || !tensor(a[7], &out[0]) ||
+      !tensor(a[8], &out[1]))
+    return nullptr;
+  if (!slots.defined() && !fail("slots is a contiguous CUDA int32 tensor [T]")) return nullptr;
+  if (!ints(slots, kc, "slots is a contiguous CUDA int32 tensor [T]")) return nullptr;
+  const int64_t T = slots.numel();
+  const at::ScalarType want = bf16 ? at::kBFloat16 : at::kHalf;
+  const c10::cuda::CUDAGuard on(kc.device());
+  if (!stream_on(a[9], kc, &st)) return nullptr;
+  for (int i = 0; i < 2; ++i) {
+    if (!out[i].defined()) {
+      out[i] = empty({T, c.n_heads, c.d}, want, kc);
+      on_stream(out[i], a[9], st);
+    }
+    if (!rows16(out[i], out[i], 3, "outputs are [T, heads, d] with contiguous rows", &r[i])) return nullptr;
+    if ((out[i].scalar_type() != want || out[i].device() != kc.device() || out[i].size(0) != T || out[i].size(1) != c.n_heads ||
+         out[i].size(2) != c.d) &&
+        !fail("outputs are [T, heads, d] of the asked type on the cache's device"))
+      return nullptr;
+  }
+  if (T > 0) {
+    const int32_t* p_slots = ptr<int32_t>(slots);
+    dgq_status rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = dgq_kv_read(&c, p_slots, T, &r[0], &r[1], bf16 ? DGQ_BF16 : DGQ_F16, st);
+    Py_END_ALLOW_THREADS
+    if (rc != DGQ_OK) return status(rc);
+  }
+  return tuple({output(a[7], out[0]), output(a[8], out[1])});
+}
+
+// (lens, n_new, free_pages, block_table, page, n_tokens, stream) -> (token_start, kv_lens, slots, used)
+PyObject* kv_plan(PyObject* const* a, Py_ssize_t n) {
+  void* st;
+  at::Tensor lens, add, pages, table;
+  int page, n_tokens, B, max_pages, n_free;
+  if (!arity(n, 7) || !tensor(a[0], &lens) || !tensor(a[1], &add) || !tensor(a[2], &pages) || !tensor(a[3], &table) ||
+      !integer(a[4], &page) || !integer(a[5], &n_tokens))
+    return nullptr;
+  if ((!lens.defined() || !add.defined() || !pages.defined() || !table.defined() || table.dim() != 2 || lens.dim() != 1 ||
+       add.dim() != 1 || lens.size(0) != table.size(0) || add.size(0) != table.size(0) || n_tokens < 0) &&
+      !fail("lens and n_new are [B], block_table [B, max_pages], n_tokens is not negative"))
+    return nullptr;
+  if (!ints(lens, lens, "lens is a contiguous CUDA int32 tensor") || !ints(add, lens, "n_new is a contiguous CUDA int32 tensor") ||
+      !ints(pages, lens, "free_pages is a contiguous CUDA int32 tensor") || !ints(table, lens, "block_table is a contiguous CUDA int32 tensor"))
+    return nullptr;
+  if (!fits(table.size(0), &B) || !fits(table.size(1), &max_pages) || !fits(pages.numel(), &n_free)) return nullptr;
+  const c10::cuda::CUDAGuard on(lens.device());
+  if (!stream_on(a[6], lens, &st)) return nullptr;
+  at::Tensor start = empty({B + 1ll}, at::kInt, lens), out_lens = empty({B}, at::kInt, lens), slots = empty({n_tokens}, at::kInt, lens),
+             used = empty({1}, at::kInt, lens);
+  for (const at::Tensor& t : {start, out_lens, slots, used}) on_stream(t, a[6], st);
+  const int32_t *p_lens = ptr<int32_t>(lens), *p_add = ptr<int32_t>(add), *p_pages = ptr<int32_t>(pages);
+  int32_t *p_table = ptr<int32_t>(table), *p_start = ptr<int32_t>(start), *p_out = ptr<int32_t>(out_lens), *p_slots = ptr<int32_t>(slots),
+          *p_used = ptr<int32_t>(used);
+  dgq_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = dgq_kv_plan(p_lens, p_add, B, p_pages, n_free, p_table, max_pages, page, p_start, p_out, p_slots, n_tokens, p_used, st);
+  Py_END_ALLOW_THREADS
+  if (rc != DGQ_OK) return status(rc);
+  return tuple({wrap(start), wrap(out_lens), wrap(slots), wrap(used)});
+}
+
 template <PyObject* (*BODY)(PyObject* const*, Py_ssize_t)>
 PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(entry<BODY>)), METH_FASTCALL, nullptr};
 }
 PyMethodDef methods[] = {method<quantize_act>("quantize_act"), method<linear>("linear"),
                          method<cross_attn_logq>("cross_attn_logq"), method<self_attn_logq>("self_attn_logq"),
+                         method<encoder_attn>("encoder_attn"), method<cached_attn>("cached_attn"), method<kv_plan>("kv_plan"),
+                         method<kv_write>("kv_write"), method<kv_read>("kv_read"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -9,6 +9,8 @@
 #include "linear.cuh"
 #include "attention.cuh"
 #include "self_attention.cuh"
+#include "kv_cache.cuh"
+#include "encoder_attention.cuh"
 
 // ---------------------------------------------------------------------------------------------
 // Cross-attention for callers that cannot allocate a workspace: the scratch is this fixed array
