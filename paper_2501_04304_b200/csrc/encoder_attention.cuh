@@ -133,10 +133,545 @@ __global__ void __launch_bounds__(128) enc_attn_rows_kernel(const __grid_constan
     if (lane + 32 * e < a.d) out[lane + 32 * e] = (uint16_t)pack16<BF>(z == 0.f ? 0.f : o[e] / z, 0.f);
 }
 
+// ------------------------------------------------------------------ many query rows: tcgen05
+constexpr int EA_Q = 128;                 // query rows of a tile
+constexpr int EA_K = 128;                 // keys of a block
+constexpr int EA_PANEL = 128 * 128;       // bytes of 64 features of 128 rows
+constexpr float EA_LAZY = 8.0f;           // a row's reference follows its maximum once that is 2^8 above it
+
+template <int NP, bool CACHED>
+struct EaCfg {
+  static constexpr int NT = NP <= 2 ? 2 : 1;          // query tiles of a block
+  static constexpr bool OWN_P = NP != 2;              // weights have tensor memory of their own (else they lie over the scores)
+  static constexpr int KST = 2, VST = NP <= 2 ? 2 : 1;
+  static constexpr int SOFTMAX_WARPS = 4 * NT;
+  static constexpr int WARP_TMA = SOFTMAX_WARPS, WARP_MMA = SOFTMAX_WARPS + 1;
+  static constexpr int CONV_WARP0 = SOFTMAX_WARPS + 2;  // CACHED: four warps that bring in keys, four for values
+  static constexpr int WARPS = SOFTMAX_WARPS + 2 + (CACHED ? 8 : 0);
+  static constexpr int THREADS = WARPS * 32;
+  static constexpr int TMEM_P = OWN_P ? NT * 128 : 0, P_STRIDE = OWN_P ? 64 : 128;
+  static constexpr int TMEM_O = OWN_P ? NT * 192 : NT * 128, O_STRIDE = NP * 64;
+  static constexpr int TILE = NP * EA_PANEL;
+  static constexpr int OFF_K = NT * TILE, OFF_V = OFF_K + KST * TILE, OFF_SH = OFF_V + VST * TILE;
+  static constexpr int SMEM = 1024 + OFF_SH + 1024;
+  static_assert(SMEM <= 232448, "shared memory budget");
+  static_assert(TMEM_O + NT * O_STRIDE <= 512, "tensor memory budget");
+};
+
+// Of sixteen keys of a cache: t = S * k, weight 2^(t + lv) with lv = log2 of the page's value scale, its inverse.
+struct EaPage {
+  float k, lv, iv, pad;
+};
+
+struct EaShared {
+  uint64_t q_full;
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+  uint64_t s_full[2], p_full[2], o_done[2];
+  uint32_t tmem_base;
+  int abort_flag;
+  EaPage page[4][8];  // four key blocks of eight groups
+};
+static_assert(sizeof(EaShared) <= 1024, "shared block");
+
+struct EaMaps {
+  CUtensorMap q, k, v;
+  int q_b, k_b, k_h, v_b, v_h;  // 0 where the tensor broadcasts along the dimension (its extent is then 1)
+  int q_h;
+};
+
+// kind::f16 instruction descriptor with both operands' type and the sign of A.
+__device__ __forceinline__ uint32_t ea_idesc(int n, bool b_mn_major, bool bf, bool negate_a) {
+  return (1u << 4) | ((bf ? 1u : 0u) << 7) | ((bf ? 1u : 0u) << 10) | ((negate_a ? 1u : 0u) << 13) |
+         ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(EA_Q >> 4) << 24);
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
+        "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
+        "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+
+// Waits for the thread's tensor-memory loads; what was loaded into r is not touched before.
+__device__ __forceinline__ void tmem_ld_wait32(uint32_t (&r)[32]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
+                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
+                 "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
+               ::"memory");
+}
+
+// Four codes as four 16-bit numbers, exactly.  fp16: 0x64 in front of a byte is 1024 + byte.  bf16: 0x43 in front of the low seven
+// bits is 128 + those, in front of the sign bit alone 128 or 256.
+template <bool BF>
+__device__ __forceinline__ void codes_to_16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  if (BF) {
+    const uint32_t y0 = __byte_perm(w, 0x43434343u, 0x4140), y1 = __byte_perm(w, 0x43434343u, 0x4342);
+    const uint32_t a0 = y0 & 0xFF7FFF7Fu, b0 = y0 & 0xFF80FF80u, a1 = y1 & 0xFF7FFF7Fu, b1 = y1 & 0xFF80FF80u;
+    const __nv_bfloat162 r0 = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a0), *reinterpret_cast<const __nv_bfloat162*>(&b0));
+    const __nv_bfloat162 r1 = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a1), *reinterpret_cast<const __nv_bfloat162*>(&b1));
+    lo = *reinterpret_cast<const uint32_t*>(&r0);
+    hi = *reinterpret_cast<const uint32_t*>(&r1);
+  } else {
+    const uint32_t x = w ^ 0x80808080u, bias = 0x64806480u;
+    const uint32_t y0 = __byte_perm(x, 0x64646464u, 0x4140), y1 = __byte_perm(x, 0x64646464u, 0x4342);
+    const __half2 r0 = __hsub2(*reinterpret_cast<const __half2*>(&y0), *reinterpret_cast<const __half2*>(&bias));
+    const __half2 r1 = __hsub2(*reinterpret_cast<const __half2*>(&y1), *reinterpret_cast<const __half2*>(&bias));
+    lo = *reinterpret_cast<const uint32_t*>(&r0);
+    hi = *reinterpret_cast<const uint32_t*>(&r1);
+  }
+}
+
+// The page of a request's token, or -1 (recorded) where the table says nothing usable.
+__device__ __forceinline__ int ea_page_of(const EncAttnArgs& a, int b, int token) {
+  const int p = __ldg(a.table + (int64_t)b * a.max_pages + token / a.page);
+  if (p >= 0 && p < a.n_pages) return p;
+  record_error(DGQ_ERR_INVALID_ARG);
+  return -1;
+}
+
+// The constants of sixteen keys that begin at `token`.  A page of zeros has no scale of its own: 2^-40 keeps its weights
+// (which count in the row sum) within range whatever the other pages' scales are; others are held above 2^-100.
+__device__ __forceinline__ EaPage ea_page_scales(const EncAttnArgs& a, int b, int g, int token, float scale_log2) {
+  EaPage c{1.17549435e-38f, -INFINITY, 0.f, 0.f};
+  const int p = ea_page_of(a, b, token);
+  if (p < 0) return c;
+  const int64_t ph = (int64_t)p * a.Hkv + g;
+  const float vs = __ldg(a.v_scale + ph);
+  const float v = vs == 0.f ? 9.094947e-13f : fmaxf(vs, 7.8886091e-31f);
+  c.k = fmaxf(__ldg(a.k_scale + ph) * scale_log2, 1.17549435e-38f);
+  c.lv = log2f(v);
+  c.iv = 1.0f / v;
+  return c;
+}
+
+template <int NP, bool BF, bool CACHED>
+__global__ void __launch_bounds__(EaCfg<NP, CACHED>::THREADS, 1)
+enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant__ EncAttnArgs a) {
+  using Cfg = EaCfg<NP, CACHED>;
+  constexpr int NT = Cfg::NT, KST = Cfg::KST, VST = Cfg::VST;
+  constexpr bool P_BF = BF && !CACHED;  // codes are whole numbers of 8 bits: fp16 holds them and three more bits of the weight
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
+  unsigned char* sQ = smem;
+  unsigned char* sK = smem + Cfg::OFF_K;
+  unsigned char* sV = smem + Cfg::OFF_V;
+  EaShared* sh = reinterpret_cast<EaShared*>(smem + Cfg::OFF_SH);
+  volatile int* abort_flag = &sh->abort_flag;
+
+  const int n_tiles = (a.nq + EA_Q * NT - 1) / (EA_Q * NT);
+  // the tiles that see most come first where that differs
+  const int tile = a.causal ? n_tiles - 1 - (int)(blockIdx.x % n_tiles) : (int)(blockIdx.x % n_tiles);
+  const int h = (int)(blockIdx.x / n_tiles) % a.Hq, b = (int)(blockIdx.x / n_tiles) / a.Hq;
+  const int g = h / (a.Hq / a.Hkv);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  pdl_launch_dependents();
+  if (threadIdx.x == 0) {
+    mbar_init(&sh->q_full, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh->k_full[i], CACHED ? 4 : 1);
+      mbar_init(&sh->v_full[i], CACHED ? 4 : 1);
+      mbar_init(&sh->k_empty[i], 1);
+      mbar_init(&sh->v_empty[i], 1);
+      mbar_init(&sh->s_full[i], 1);
+      mbar_init(&sh->p_full[i], 4);
+      mbar_init(&sh->o_done[i], 1);
+    }
+    sh->abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == Cfg::WARP_MMA) {
+    tmem_alloc(&sh->tmem_base, 512);
+    tmem_relinquish();
+  }
+  pdl_wait();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = sh->tmem_base;
+
+  const EncRequest rq = enc_request(a, b);
+  const int row0 = tile * (EA_Q * NT);
+  // key blocks that each tile walks: as many as its last row sees
+  int nbt[2] = {0, 0};
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const int first = row0 + t * EA_Q;
+    if (first < rq.nq) nbt[t] = (enc_sees(a, rq, min(first + EA_Q, rq.nq) - 1) + EA_K - 1) / EA_K;
+  }
+  const int nb = max(nbt[0], nbt[1]);
+  const float scale_log2 = fabsf(a.scale_log2);  // the sign is the MMA's
+  const int ksteps = (a.d + 15) / 16, dp = ksteps * 16;
+
+  if (warp == Cfg::WARP_TMA) {
+    // ------------------------------------------------------------ loads
+    if (lane == 0 && nb > 0) {
+      const int panels = (a.d + 63) / 64;  // panels of NP that hold features
+      tma_prefetch_desc(&maps.q);
+      mbar_arrive_expect_tx(&sh->q_full, (uint32_t)(NT * panels * EA_PANEL));
+      for (int t = 0; t < NT; ++t)
+        for (int p = 0; p < panels; ++p)
+          tma_load_4d(sQ + t * Cfg::TILE + p * EA_PANEL, &maps.q, &sh->q_full, p * 64, h * maps.q_h, (int)rq.q_row + row0 + t * EA_Q, b * maps.q_b);
+      if (!CACHED) {
+        tma_prefetch_desc(&maps.k);
+        tma_prefetch_desc(&maps.v);
+        for (int j = 0; j < nb; ++j) {
+          const int ks = j % KST, vs = j % VST;
+          mbar_wait_handover(smem_u32(&sh->k_empty[ks]), (((uint32_t)j / KST) & 1u) ^ 1u, abort_flag);
+          mbar_arrive_expect_tx(&sh->k_full[ks], (uint32_t)(panels * EA_PANEL));
+          for (int p = 0; p < panels; ++p)
+            tma_load_4d(sK + ks * Cfg::TILE + p * EA_PANEL, &maps.k, &sh->k_full[ks], p * 64, g * maps.k_h, j * EA_K, b * maps.k_b);
+          mbar_wait_handover(smem_u32(&sh->v_empty[vs]), (((uint32_t)j / VST) & 1u) ^ 1u, abort_flag);
+          mbar_arrive_expect_tx(&sh->v_full[vs], (uint32_t)(panels * EA_PANEL));
+          for (int p = 0; p < panels; ++p)
+            tma_load_4d(sV + vs * Cfg::TILE + p * EA_PANEL, &maps.v, &sh->v_full[vs], p * 64, g * maps.v_h, j * EA_K, b * maps.v_b);
+          if (*abort_flag) break;
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == Cfg::WARP_MMA) {
+    // ------------------------------------------------------------ products
+    // Scores of block j + 1 and O += P V of block j alternate between the tiles; a tile's softmax runs under the other tile's
+    // products.  The weights' hand-over also says that the scores have been read.
+    const uint32_t idesc_qk = ea_idesc(EA_K, false, BF, a.scale_log2 < 0.f), idesc_pv = ea_idesc(dp, true, P_BF, false);
+    constexpr uint32_t HI = smem_desc_hi(1024, 2);
+    const uint32_t q_lo = smem_desc_lo(smem_u32(sQ)), k_lo = smem_desc_lo(smem_u32(sK));
+    const uint32_t v_lo = ((smem_u32(sV) & 0x3FFFFu) >> 4) | ((uint32_t)(EA_PANEL >> 4) << 16);
+    auto scores = [&](int t, int j) {
+      const uint32_t a_lo = q_lo + (uint32_t)(t * Cfg::TILE >> 4), b_lo = k_lo + (uint32_t)((j % KST) * Cfg::TILE >> 4);
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < NP * 4; ++k) {
+          if (k >= ksteps) break;
+          const uint32_t off = (uint32_t)(((k >> 2) * EA_PANEL + (k & 3) * 32) >> 4);
+          mma_f16_lohi(tmem_base + t * 128, a_lo + off, HI, b_lo + off, HI, idesc_qk, k > 0 ? 1u : 0u);
+        }
+        mma_commit_addr(smem_u32(&sh->s_full[t]));
+      }
+      __syncwarp();
+    };
+    if (nb > 0) {
+      mbar_wait_handover(smem_u32(&sh->q_full), 0, abort_flag);
+      mbar_wait_handover(smem_u32(&sh->k_full[0]), 0, abort_flag);
+      tc_fence_after();
+      for (int t = 0; t < NT; ++t)
+        if (nbt[t] > 0) scores(t, 0);
+      if (elect_one()) mma_commit_addr(smem_u32(&sh->k_empty[0]));
+      __syncwarp();
+    }
+    for (int j = 0; j < nb; ++j) {
+      const int vs = j % VST;
+      bool have_k = false, have_v = false;
+      for (int t = 0; t < NT; ++t) {
+        if (j >= nbt[t]) continue;
+        auto next_scores = [&]() {
+          if (j + 1 >= nbt[t]) return;
+          if (!have_k) {
+            mbar_wait_handover(smem_u32(&sh->k_full[(j + 1) % KST]), (((uint32_t)j + 1) / KST) & 1u, abort_flag);
+            tc_fence_after();
+            have_k = true;
+          }
+          scores(t, j + 1);
+        };
+        mbar_wait_handover(smem_u32(&sh->p_full[t]), (uint32_t)j & 1u, abort_flag);
+        tc_fence_after();
+        if (Cfg::OWN_P) next_scores();
+        if (!have_v) {
+          mbar_wait_handover(smem_u32(&sh->v_full[vs]), ((uint32_t)j / VST) & 1u, abort_flag);
+          have_v = true;
+          // value rows behind the length meet weights of 0, which an infinity or NaN there would not survive
+          const int real = rq.len - j * EA_K;
+          if (!CACHED && real < EA_K && rq.len < a.nk) {
+            for (int i = lane; i < (EA_K - real) * NP * 8; i += 32) {
+              const int r = real + i / (NP * 8), c = i % (NP * 8);
+              *reinterpret_cast<uint4*>(sV + vs * Cfg::TILE + (c >> 3) * EA_PANEL + r * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+          }
+          tc_fence_after();
+        }
+        const uint32_t a_tmem = tmem_base + Cfg::TMEM_P + t * Cfg::P_STRIDE, d_tmem = tmem_base + Cfg::TMEM_O + t * Cfg::O_STRIDE;
+        const uint32_t b_lo = v_lo + (uint32_t)(vs * Cfg::TILE >> 4);
+        if (elect_one()) {
+#pragma unroll
+          for (int k = 0; k < EA_K / 16; ++k)
+            mma_f16_ts(d_tmem, a_tmem + k * 8, b_lo + (uint32_t)(k * 2048 >> 4), HI, idesc_pv, (j > 0 || k > 0) ? 1u : 0u);
+          mma_commit_addr(smem_u32(&sh->o_done[t]));
+        }
+        __syncwarp();
+        if (!Cfg::OWN_P) next_scores();
+      }
+      if (elect_one()) {
+        mma_commit_addr(smem_u32(&sh->v_empty[vs]));
+        if (j + 1 < nb) mma_commit_addr(smem_u32(&sh->k_empty[(j + 1) % KST]));
+      }
+      __syncwarp();
+      if ((j & 7) == 7 && *abort_flag) break;
+    }
+    __syncwarp();
+  } else if (CACHED && warp >= Cfg::CONV_WARP0) {
+    // ------------------------------------------------------------ codes to 16 bits
+    // Four warps bring in keys, four values: sixteen codes a load, the next block's in registers while this one's stage is
+    // still in use.
+    const bool values = warp >= Cfg::CONV_WARP0 + 4;
+    const int tid = (warp - Cfg::CONV_WARP0 - (values ? 4 : 0)) * 32 + lane;
+    const int row_bytes = kv_row_bytes(a.d), units = row_bytes / 16, total = EA_K * units;
+    constexpr int MAX_UNITS = NP * 4;
+    const int8_t* codes = values ? a.v_codes : a.k_codes;
+    const int st_n = values ? VST : KST;
+    uint4 x[MAX_UNITS];
+    auto load = [&](int j) {
+#pragma unroll
+      for (int i = 0; i < MAX_UNITS; ++i) {
+        const int u = tid + i * 128;
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (u >= total) continue;
+        const int r = u / units, c = u - r * units, token = j * EA_K + r;
+        if (token >= rq.len) continue;
+        const int p = ea_page_of(a, b, token);
+        if (p >= 0)
+          x[i] = __ldg(reinterpret_cast<const uint4*>(codes + (((int64_t)p * a.Hkv + g) * a.page + token % a.page) * row_bytes) + c);
+      }
+    };
+    if (nb > 0) load(0);
+    for (int j = 0; j < nb; ++j) {
+      const int st = j % st_n;
+      unsigned char* stage = (values ? sV : sK) + st * Cfg::TILE;
+      uint64_t* empty = values ? &sh->v_empty[st] : &sh->k_empty[st];
+      uint64_t* full = values ? &sh->v_full[st] : &sh->k_full[st];
+      EaPage pg;
+      if (!values && tid < 8) {
+        const int token = j * EA_K + tid * 16;
+        pg = EaPage{1.17549435e-38f, -INFINITY, 0.f, 0.f};
+        if (token < rq.len) pg = ea_page_scales(a, b, g, token, scale_log2);
+      }
+      mbar_wait_handover(smem_u32(empty), (((uint32_t)j / st_n) & 1u) ^ 1u, abort_flag);
+      if (!values && tid < 8) sh->page[j & 3][tid] = pg;
+#pragma unroll
+      for (int i = 0; i < MAX_UNITS; ++i) {
+        const int u = tid + i * 128;
+        if (u >= total) continue;
+        const int r = u / units, c = u - r * units;
+        uint32_t y[8];
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (BF && !values) codes_to_16<true>(w[k], y[2 * k], y[2 * k + 1]);
+          else codes_to_16<false>(w[k], y[2 * k], y[2 * k + 1]);
+        }
+        unsigned char* row = stage + (c >> 2) * EA_PANEL + r * 128;
+        const int c0 = (c & 3) * 2, sw = r & 7;
+        *reinterpret_cast<uint4*>(row + ((c0 ^ sw) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+        *reinterpret_cast<uint4*>(row + (((c0 + 1) ^ sw) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(full);
+      if (j + 1 < nb) load(j + 1);
+      if (*abort_flag) break;
+    }
+    __syncwarp();
+  } else if (warp < Cfg::SOFTMAX_WARPS) {
+    // ------------------------------------------------------------ softmax
+    // One thread has one row of a tile.
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane, i = row0 + t * EA_Q + row;
+    const uint32_t t_lane = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
+    const uint32_t t_s = t_lane + t * 128, t_p = t_lane + Cfg::TMEM_P + t * Cfg::P_STRIDE, t_o = t_lane + Cfg::TMEM_O + t * Cfg::O_STRIDE;
+    const int sees = i < rq.nq ? enc_sees(a, rq, i) : 0;
+    float m = -INFINITY;   // the reference: within 2^8 below the largest exponent so far
+    float z = 0.f;
+    const int blocks = nbt[t];
+    for (int j = 0; j < blocks; ++j) {
+      mbar_wait_handover(smem_u32(&sh->s_full[t]), (uint32_t)j & 1u, abort_flag);
+      __syncwarp();
+      tc_fence_after();
+      const int valid = sees - j * EA_K;
+      const EaPage* pages = sh->page[j & 3];
+      auto hide = [&](uint32_t (&r)[32], int c) {
+        if (valid < c * 32 + 32) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k)
+            if (c * 32 + k >= valid) r[k] = 0xFF800000u;
+        }
+      };
+      float top = -INFINITY;
+      uint32_t r[2][32];
+      tmem_ld32(t_s, r[0]);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t(&x)[32] = r[c & 1];
+        tmem_ld_wait32(x);
+        if (c < 3) tmem_ld32(t_s + (c + 1) * 32, r[(c + 1) & 1]);
+        hide(x, c);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+          for (int k = half * 16; k < half * 16 + 16; k += 4) {
+            m0 = max3(m0, __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+            m1 = max3(m1, __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+          }
+          if (CACHED) top = fmaxf(top, fmaf(fmaxf(m0, m1), pages[c * 2 + half].k, pages[c * 2 + half].lv));
+          else top = max3(top, m0, m1);
+        }
+      }
+      tmem_ld32(t_s, r[0]);
+      if (!CACHED) top *= scale_log2;
+      const bool move = top > (j == 0 ? -INFINITY : m + EA_LAZY);
+      if (j == 0) {
+        m = top;
+      } else if (__any_sync(0xFFFFFFFFu, move)) {
+        const float m1 = fmaxf(m, top);
+        const float fall = m1 == -INFINITY ? 1.f : ex2_approx(m - m1);  // m = -inf: 0
+        m = m1;
+        z *= fall;
+        tmem_ld_wait();
+        mbar_wait_handover(smem_u32(&sh->o_done[t]), (uint32_t)(j - 1) & 1u, abort_flag);
+        __syncwarp();
+        tc_fence_after();
+        for (int c = 0; c < dp; c += 16) {
+          uint32_t o[16];
+          tmem_ld16(t_o + c, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
+          tmem_st16(t_o + c, o);
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : m;
+      if (Cfg::OWN_P && j > 0) {  // the product before has read its weights
+        mbar_wait_handover(smem_u32(&sh->o_done[t]), (uint32_t)(j - 1) & 1u, abort_flag);
+        __syncwarp();
+        tc_fence_after();
+      }
+      unsigned long long z2 = 0ull;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t(&x)[32] = r[c & 1];
+        tmem_ld_wait32(x);
+        if (c < 3) tmem_ld32(t_s + (c + 1) * 32, r[(c + 1) & 1]);
+        hide(x, c);
+        uint32_t pk[16];
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float f = scale_log2, off = -base, iv = 1.f;
+          if (CACHED) {
+            const EaPage pg = pages[c * 2 + half];
+            f = pg.k;
+            off = pg.lv - base;
+            iv = pg.iv;
+          }
+          const unsigned long long f2 = pack_f32x2(f, f), off2 = pack_f32x2(off, off), iv2 = pack_f32x2(iv, iv);
+          unsigned long long zc = 0ull;
+#pragma unroll
+          for (int k = half * 16; k < half * 16 + 16; k += 2) {
+            float x0, x1;
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2, off2), x0, x1);
+            const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
+            zc = add_f32x2(zc, pack_f32x2(e0, e1));
+            pk[k >> 1] = pack16<P_BF>(e0, e1);
+          }
+          z2 = CACHED ? fma_f32x2(zc, iv2, z2) : add_f32x2(zc, z2);
+        }
+        tmem_st16(t_p + c * 16, pk);
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh->p_full[t]);
+      z += __uint_as_float((uint32_t)z2) + __uint_as_float((uint32_t)(z2 >> 32));
+    }
+    if (blocks > 0) {
+      mbar_wait_handover(smem_u32(&sh->o_done[t]), (uint32_t)(blocks - 1) & 1u, abort_flag);
+      __syncwarp();
+      tc_fence_after();
+    }
+    const float inv = z > 0.f || z != z ? 1.f / z : 0.f;
+    uint16_t* out = (uint16_t*)a.O.ptr + b * a.O.batch + (rq.q_row + i) * a.O.token + h * a.O.head;
+    for (int c = 0; c < a.d; c += 8) {
+      uint32_t o[8] = {};
+      if (blocks > 0) {
+        tmem_ld8(t_o + c, o);
+        tmem_ld_wait();
+      }
+      uint32_t y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = pack16<BF>(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
+      if (i < rq.nq) *reinterpret_cast<uint4*>(out + c) = sees > 0 ? make_uint4(y[0], y[1], y[2], y[3]) : make_uint4(0, 0, 0, 0);
+    }
+  }
+
+  // ------------------------------------------------------------ common exit
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    // give copies that may still be in flight time to land before the block's shared memory is released
+    const long long t0 = clock64();
+    while (clock64() - t0 < 200000) {
+    }
+    __syncthreads();
+  }
+  if (warp == Cfg::WARP_MMA) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 512);
+  }
+}
+
+// [B, n, H, d] with strides as a 4-D tensor (d, H, n, B), boxes of 64 features x 128 rows of one head.  A dimension along which
+// the tensor broadcasts has extent 1, and the kernel's coordinate there is 0.
+static bool ea_encode(CUtensorMap* m, const dgq_rows& r, int64_t B, int64_t n, int64_t H, int d, bool bf, int* use_b, int* use_h) {
+  *use_b = r.batch != 0;
+  *use_h = r.head != 0;
+  const uint64_t dims[4] = {(uint64_t)d, *use_h ? (uint64_t)H : 1u, (uint64_t)n, *use_b ? (uint64_t)B : 1u};
+  const auto bytes = [&](int64_t s) { return (uint64_t)(s ? s * 2 : (int64_t)kv_row_bytes(d) * 2); };
+  const uint64_t strides[3] = {bytes(r.head), bytes(r.token), bytes(r.batch)};
+  const uint32_t box[4] = {64, 1, 128, 1};
+  return encode_map(m, r.ptr, 4, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B,
+                    bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
+}
+
+template <int NP, bool BF, bool CACHED>
+static dgq_status ea_launch_tiles(const EncAttnArgs& a, cudaStream_t stream) {
+  using Cfg = EaCfg<NP, CACHED>;
+  static std::atomic<bool> attr_set[64];
+  int dev = 0;
+  DGQ_CUDA_OK(cudaGetDevice(&dev));
+  if (dev >= 64 || !attr_set[dev].load()) {
+    DGQ_CUDA_OK(cudaFuncSetAttribute(enc_attn_tiles_kernel<NP, BF, CACHED>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
+    if (dev < 64) attr_set[dev].store(true);
+  }
+  const int64_t grid = (int64_t)a.B * a.Hq * ((a.nq + EA_Q * Cfg::NT - 1) / (EA_Q * Cfg::NT));
+  if (grid > INT_MAX) return DGQ_ERR_UNSUPPORTED;
+  EaMaps maps;
+  std::memset(&maps, 0, sizeof(maps));
+  if (!ea_encode(&maps.q, a.Q, a.q_start ? 1 : a.B, a.q_start ? a.n_rows : a.nq, a.Hq, a.d, BF, &maps.q_b, &maps.q_h)) return DGQ_ERR_CUDA;
+  if (!CACHED && (!ea_encode(&maps.k, a.K, a.B, a.nk, a.Hkv, a.d, BF, &maps.k_b, &maps.k_h) ||
+                  !ea_encode(&maps.v, a.V, a.B, a.nk, a.Hkv, a.d, BF, &maps.v_b, &maps.v_h)))
+    return DGQ_ERR_CUDA;
+  DGQ_CUDA_OK(launch_pdl(enc_attn_tiles_kernel<NP, BF, CACHED>, dim3((unsigned)grid), dim3(Cfg::THREADS), (size_t)Cfg::SMEM, stream, maps, a));
+  g_launches += 1;
+  DGQ_CUDA_OK(cudaGetLastError());
+  return DGQ_OK;
+}
+
 template <bool BF, bool CACHED>
 static dgq_status enc_attn_launch(const EncAttnArgs& a, cudaStream_t stream) {
   const int64_t rows = (int64_t)a.B * a.nq * a.Hq;
   if (rows / 4 >= INT_MAX) return DGQ_ERR_UNSUPPORTED;
+  if (a.nq > 16) {
+    EncAttnArgs t = a;
+    if (t.scale_log2 == 0.f) t.scale_log2 = 1.17549435e-38f;  // hidden keys are -inf, which 0 would make NaN
+    if (a.d <= 64) return ea_launch_tiles<1, BF, CACHED>(t, stream);
+    if (a.d <= 128) return ea_launch_tiles<2, BF, CACHED>(t, stream);
+    return ea_launch_tiles<3, BF, CACHED>(t, stream);
+  }
   DGQ_CUDA_OK(launch_pdl(enc_attn_rows_kernel<BF, CACHED>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, stream, a));
   g_launches += 1;
   DGQ_CUDA_OK(cudaGetLastError());
@@ -182,7 +717,7 @@ extern "C" dgq_status dgq_cached_attn(const dgq_kv_cache* cache, const dgq_rows*
   if (!rows_pointer_ok(Q) || !rows_pointer_ok(O) || B <= 0 || Hq <= 0 || max_nq <= 0 || !block_table || max_pages <= 0 || !kv_lens ||
       (q_start && n_rows <= 0) || Hq % cache->n_heads || (dtype != DGQ_F16 && dtype != DGQ_BF16) || !std::isfinite(scale))
     return DGQ_ERR_INVALID_ARG;
-  if ((int64_t)max_pages * cache->page > INT_MAX) return DGQ_ERR_UNSUPPORTED;
+  if ((int64_t)max_pages * cache->page > INT_MAX || n_rows > INT_MAX) return DGQ_ERR_UNSUPPORTED;
   const int64_t qb = q_start ? 1 : B, qn = q_start ? n_rows : max_nq;
   if ((st = rows_check(*Q, qb, qn, Hq, false)) != DGQ_OK || (st = rows_check(*O, qb, qn, Hq, true)) != DGQ_OK) return st;
   EncAttnArgs a = {};
