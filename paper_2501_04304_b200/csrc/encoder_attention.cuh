@@ -23,6 +23,7 @@ struct EncAttnArgs {
   const int32_t* q_start;       // dev [B + 1] or null (nq queries each)
   int64_t n_rows;
   int causal;
+  int bf;                       // Q and O are bf16
 };
 
 // What a block needs to know of its request.
@@ -48,89 +49,6 @@ __device__ __forceinline__ EncRequest enc_request(const EncAttnArgs& a, int b) {
 // Keys that query i of the request sees.
 __device__ __forceinline__ int enc_sees(const EncAttnArgs& a, const EncRequest& r, int i) {
   return a.causal ? max(r.len - r.nq + i + 1, 0) : r.len;
-}
-
-// One warp for one query row and head: a lane has a key of 32 for the scores, every 32nd feature for the product.
-template <bool BF, bool CACHED>
-__global__ void __launch_bounds__(128) enc_attn_rows_kernel(const __grid_constant__ EncAttnArgs a) {
-  __shared__ float sq[4][KV_MAX_D];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int64_t at = (int64_t)blockIdx.x * 4 + warp;
-  pdl_launch_dependents();
-  pdl_wait();
-  if (at >= (int64_t)a.B * a.nq * a.Hq) return;
-  const int h = (int)(at % a.Hq), i = (int)(at / a.Hq % a.nq), b = (int)(at / a.Hq / a.nq);
-  const int g = h / (a.Hq / a.Hkv);
-  const EncRequest rq = enc_request(a, b);
-  if (i >= rq.nq) return;
-  const uint16_t* q = (const uint16_t*)a.Q.ptr + b * a.Q.batch + (rq.q_row + i) * a.Q.token + h * a.Q.head;
-  for (int u = lane; u < a.d / 2; u += 32) {
-    const float2 f = unpack16<BF>(reinterpret_cast<const uint32_t*>(q)[u]);
-    sq[warp][2 * u] = f.x;
-    sq[warp][2 * u + 1] = f.y;
-  }
-  __syncwarp();
-  const int sees = enc_sees(a, rq, i), row_bytes = kv_row_bytes(a.d);
-  float o[(KV_MAX_D + 31) / 32] = {};
-  float m = -INFINITY, z = 0.f;
-  for (int j0 = 0; j0 < sees; j0 += 32) {
-    const int j = j0 + lane;
-    bool real = j < sees;
-    float t = -INFINITY, vs = 1.f;
-    const int8_t* vc = nullptr;
-    if (CACHED) {
-      const int p = real ? a.table[(int64_t)b * a.max_pages + j / a.page] : 0;
-      if (p < 0 || p >= a.n_pages) {
-        real = false;
-        record_error(DGQ_ERR_INVALID_ARG);
-      }
-      if (real) {
-        const int64_t ph = (int64_t)p * a.Hkv + g;
-        const int8_t* kc = a.k_codes + (ph * a.page + j % a.page) * row_bytes;
-        vc = a.v_codes + (ph * a.page + j % a.page) * row_bytes;
-        float dot = 0.f;
-        for (int c = 0; c < a.d; ++c) dot = fmaf(sq[warp][c], (float)kc[c], dot);
-        t = dot * (a.k_scale[ph] * a.scale_log2);
-        vs = a.v_scale[ph];
-      }
-    } else if (real) {
-      const uint32_t* k = (const uint32_t*)((const uint16_t*)a.K.ptr + b * a.K.batch + (int64_t)j * a.K.token + g * a.K.head);
-      float dot = 0.f;
-      for (int c = 0; c < a.d / 2; ++c) {
-        const float2 f = unpack16<BF>(k[c]);
-        dot = fmaf(sq[warp][2 * c], f.x, dot);
-        dot = fmaf(sq[warp][2 * c + 1], f.y, dot);
-      }
-      t = dot * a.scale_log2;
-    }
-    float top = t;
-#pragma unroll
-    for (int x = 16; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, x));
-    const float m1 = fmaxf(m, top);
-    const float base = m1 == -INFINITY ? 0.f : m1;
-    const float p = real ? exp2f(t - base) : 0.f;
-    const float fall = m == -INFINITY ? 0.f : exp2f(m - base);
-    m = m1;
-    z = z * fall + p;
-#pragma unroll
-    for (int e = 0; e < (KV_MAX_D + 31) / 32; ++e) o[e] *= fall;
-    const unsigned some = __ballot_sync(0xFFFFFFFFu, real);
-    for (int jj = 0; jj < 32; ++jj) {
-      if (!(some >> jj & 1)) continue;
-      const float w = __shfl_sync(0xFFFFFFFFu, p * vs, jj);
-      const int8_t* c8 = (const int8_t*)__shfl_sync(0xFFFFFFFFu, (unsigned long long)vc, jj);
-      const uint16_t* v = CACHED ? nullptr : (const uint16_t*)a.V.ptr + b * a.V.batch + (int64_t)(j0 + jj) * a.V.token + g * a.V.head;
-#pragma unroll
-      for (int e = 0; e < (KV_MAX_D + 31) / 32; ++e)
-        if (lane + 32 * e < a.d) o[e] = fmaf(w, CACHED ? (float)c8[lane + 32 * e] : unpack16<BF>((uint32_t)v[lane + 32 * e]).x, o[e]);
-    }
-  }
-#pragma unroll
-  for (int x = 16; x > 0; x >>= 1) z += __shfl_xor_sync(0xFFFFFFFFu, z, x);
-  uint16_t* out = (uint16_t*)a.O.ptr + b * a.O.batch + (rq.q_row + i) * a.O.token + h * a.O.head;
-#pragma unroll
-  for (int e = 0; e < (KV_MAX_D + 31) / 32; ++e)
-    if (lane + 32 * e < a.d) out[lane + 32 * e] = (uint16_t)pack16<BF>(z == 0.f ? 0.f : o[e] / z, 0.f);
 }
 
 // ------------------------------------------------------------------ many query rows: tcgen05
@@ -661,21 +579,549 @@ static dgq_status ea_launch_tiles(const EncAttnArgs& a, cudaStream_t stream) {
   return DGQ_OK;
 }
 
-template <bool BF, bool CACHED>
-static dgq_status enc_attn_launch(const EncAttnArgs& a, cudaStream_t stream) {
-  const int64_t rows = (int64_t)a.B * a.nq * a.Hq;
-  if (rows / 4 >= INT_MAX) return DGQ_ERR_UNSUPPORTED;
-  if (a.nq > 16) {
-    EncAttnArgs t = a;
-    if (t.scale_log2 == 0.f) t.scale_log2 = 1.17549435e-38f;  // hidden keys are -inf, which 0 would make NaN
-    if (a.d <= 64) return ea_launch_tiles<1, BF, CACHED>(t, stream);
-    if (a.d <= 128) return ea_launch_tiles<2, BF, CACHED>(t, stream);
-    return ea_launch_tiles<3, BF, CACHED>(t, stream);
+// ------------------------------------------------------------------ few query rows: keys split over warps and blocks
+// The n x G rows of a request's queries that share a key head are columns of S^T = K Q^T (mma.m16n8k16: sixteen keys, eight
+// columns), so that a key or value is read once for all of them, straight from memory into the operand's registers: which
+// features a lane's sixteen bytes hold is the lane's choice as long as Q's fragment follows it.  Weights turn into the second
+// product's operand O^T = V^T P by transposing 8 x 8 tiles between lanes.  Codes become fp16 in registers (1.25 instructions a
+// code for keys, 1.5 for values).  Each warp has its own running maximum and sums; the warps of a block meet in shared memory,
+// the blocks of a request in the shared memory of their cluster, in a fixed order.
+enum { EF_I8 = 0, EF_F16 = 1, EF_BF16 = 2 };
+
+template <int SRC, int DC, int NTL>
+struct EfCfg {
+  static constexpr bool I8 = SRC == EF_I8;
+  static constexpr int DMAX = DC == 1 ? 64 : DC == 2 ? 128 : 160;
+  static constexpr int KU = I8 ? 16 : 8;                    // features in sixteen bytes of a key
+  static constexpr int KR = (DMAX / KU + 3) / 4;            // such loads of a lane per key
+  static constexpr int KW = I8 ? 4 : 2;                     // MMA steps per load
+  static constexpr int KSTEPS = KR * KW;
+  static constexpr int VB = I8 && DC == 1 ? 8 : 16;         // bytes of a value row per lane and load
+  static constexpr int VU = I8 ? VB : 8;                    // features in them
+  static constexpr int VR = (DMAX / VU + 7) / 8;
+  static constexpr int MT = VR * VU / 2;                    // tiles of sixteen features
+  static constexpr int GR = I8 && DC < 3 ? 2 : 1;           // groups of sixteen keys per step
+  static constexpr int CH = GR * 16;
+  static constexpr int WARPS = 4, N = NTL * 8;
+  static constexpr int O_LD = DMAX + 4;
+  static constexpr int SMEM_Q = NTL * KSTEPS * 32 * 8;
+  static constexpr int SMEM_O = WARPS * N * O_LD * 4;
+  static constexpr int SMEM = SMEM_Q + SMEM_O + (3 * WARPS + 3) * N * 4;
+};
+
+template <bool BF>
+__device__ __forceinline__ void ef_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint2 b) {
+  if (BF)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b.x), "r"(b.y));
+  else
+    mma_f16(c, a0, a1, a2, a3, b.x, b.y);
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+// Bytes 0, 1 (lo) or 2, 3 (hi) of biased codes as two fp16 numbers.
+__device__ __forceinline__ uint32_t biased_lo(uint32_t x) {
+  const uint32_t y = __byte_perm(x, 0x64646464u, 0x4140), bias = 0x64806480u;
+  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&y), *reinterpret_cast<const __half2*>(&bias));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t biased_hi(uint32_t x) {
+  const uint32_t y = __byte_perm(x, 0x64646464u, 0x4342), bias = 0x64806480u;
+  const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&y), *reinterpret_cast<const __half2*>(&bias));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint4 ld_stream16(const void* p) {
+  uint4 x;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "l"(p));
+  return x;
+}
+__device__ __forceinline__ uint2 ld_stream8(const void* p) {
+  uint2 x;
+  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0,%1}, [%2];" : "=r"(x.x), "=r"(x.y) : "l"(p));
+  return x;
+}
+
+template <int SRC, int DC, int NTL>
+__global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant__ EncAttnArgs a, int splits) {
+  using Cfg = EfCfg<SRC, DC, NTL>;
+  constexpr bool I8 = Cfg::I8;
+  constexpr bool M_BF = SRC == EF_BF16;       // type of both products' operands; codes: fp16
+  const bool bf = I8 ? a.bf != 0 : M_BF;      // type of Q and O
+  constexpr int GR = Cfg::GR, KR = Cfg::KR, KW = Cfg::KW, VR = Cfg::VR, MT = Cfg::MT, N = Cfg::N, KSTEPS = Cfg::KSTEPS;
+  extern __shared__ unsigned char smem_dyn[];
+  uint2* sQ = reinterpret_cast<uint2*>(smem_dyn);
+  float* sO = reinterpret_cast<float*>(smem_dyn + Cfg::SMEM_Q);  // [warp][column][feature]
+  float* sM = sO + Cfg::SMEM_O / 4;                              // [warp][column]
+  float* sZ = sM + Cfg::WARPS * N;
+  float* sF = sZ + Cfg::WARPS * N;
+  float* cM = sF + Cfg::WARPS * N;                               // the block's maximum, sum and the columns' factors
+  float* cZ = cM + N;
+  float* sC = cZ + N;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, lg = lane >> 2, lt = lane & 3;
+  const int group = a.Hq / a.Hkv;
+  const int split = (int)blockIdx.x % splits;
+  const int g = (int)blockIdx.y, b = (int)(blockIdx.x / splits), col0 = (int)blockIdx.z * N;
+  pdl_launch_dependents();
+  pdl_wait();
+  const EncRequest rq = enc_request(a, b);
+
+  // this block's keys: whole steps, the same number for every block of the cluster but the last ones
+  const int steps = (rq.len + Cfg::CH - 1) / Cfg::CH, share = (steps + splits - 1) / splits;
+  const int step1 = min((split + 1) * share, steps);
+  int step = split * share + warp;
+
+  // ------------------------------------------------------------ loads of a step
+  const int row_bytes = I8 ? kv_row_bytes(a.d) : a.d * 2;
+  uint4 kx[GR][2][KR];
+  uint4 vx[GR][4][VR];
+  float ks[GR], vs[GR];
+  int page_next[GR];
+  auto find_pages = [&](int st) {
+    if (!I8) return;
+#pragma unroll
+    for (int i = 0; i < GR; ++i) {
+      const int key = st * Cfg::CH + i * 16;
+      page_next[i] = -1;
+      if (st < step1 && key < rq.len) page_next[i] = __ldg(a.table + (int64_t)b * a.max_pages + key / a.page);
+    }
+  };
+  auto load_k = [&](int st) {
+#pragma unroll
+    for (int i = 0; i < GR; ++i) {
+      const int key = st * Cfg::CH + i * 16;
+      const uint8_t* base = nullptr;
+      int64_t pitch = row_bytes;
+      bool real = st < step1 && key < rq.len;
+      if (I8) {
+        const int p = page_next[i];
+        if (real && (p < 0 || p >= a.n_pages)) {
+          real = false;
+          record_error(DGQ_ERR_INVALID_ARG);
+        }
+        const int64_t ph = real ? (int64_t)p * a.Hkv + g : 0;
+        ks[i] = vs[i] = -1.f;  // absent
+        if (real) {
+          ks[i] = __ldg(a.k_scale + ph);
+          vs[i] = __ldg(a.v_scale + ph);
+        }
+        base = (const uint8_t*)a.k_codes + (ph * a.page + key % a.page) * row_bytes;
+      } else {
+        pitch = a.K.token * 2;
+        base = (const uint8_t*)a.K.ptr + 2 * (b * a.K.batch + g * a.K.head) + key * pitch;
+      }
+#pragma unroll
+      for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+        for (int r = 0; r < KR; ++r) {
+          const int c = (lt + 4 * r) * 16;
+          kx[i][hh][r] = make_uint4(0, 0, 0, 0);
+          if (real && c < row_bytes && (I8 || key + lg + 8 * hh < rq.len)) kx[i][hh][r] = ld_stream16(base + (lg + 8 * hh) * pitch + c);
+        }
+    }
+  };
+  auto load_v = [&](int st) {
+#pragma unroll
+    for (int i = 0; i < GR; ++i) {
+      const int key = st * Cfg::CH + i * 16;
+      const uint8_t* base = nullptr;
+      int64_t pitch = row_bytes;
+      bool real = st < step1 && key < rq.len;
+      if (I8) {
+        const int p = page_next[i];
+        real = real && p >= 0 && p < a.n_pages;
+        base = (const uint8_t*)a.v_codes + ((real ? (int64_t)p * a.Hkv + g : 0) * a.page + key % a.page) * row_bytes;
+      } else {
+        pitch = a.V.token * 2;
+        base = (const uint8_t*)a.V.ptr + 2 * (b * a.V.batch + g * a.V.head) + key * pitch;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+#pragma unroll
+        for (int r = 0; r < VR; ++r) {
+          const int c = (lg + 8 * r) * Cfg::VB, row = 2 * lt + (k & 1) + 8 * (k >> 1);
+          vx[i][k][r] = make_uint4(0, 0, 0, 0);
+          if (real && c < row_bytes && (I8 || key + row < rq.len)) {
+            if (Cfg::VB == 16) {
+              vx[i][k][r] = ld_stream16(base + row * pitch + c);
+            } else {
+              const uint2 x = ld_stream8(base + row * pitch + c);
+              vx[i][k][r].x = x.x;
+              vx[i][k][r].y = x.y;
+            }
+          }
+        }
+    }
+  };
+  find_pages(step);
+  load_k(step);
+  load_v(step);
+  find_pages(step + Cfg::WARPS);
+
+  // ------------------------------------------------------------ Q as the second operand
+  auto q_row = [&](int col) -> const uint16_t* {
+    const int i = col / group, h = g * group + col % group;
+    if (i >= rq.nq) return nullptr;
+    return (const uint16_t*)a.Q.ptr + b * a.Q.batch + (rq.q_row + i) * a.Q.token + h * a.Q.head;
+  };
+  for (int c = warp; c < N; c += Cfg::WARPS) {
+    // bf16 queries over codes: a power of two brings the row's largest value to 1 .. 2, so that fp16 holds what bf16 does
+    // (but for what is 2^24 times smaller than the largest)
+    float norm = 1.f;
+    if (I8 && bf) {
+      const uint16_t* q = q_row(col0 + c);
+      float top = 0.f;
+      if (q)
+        for (int k = lane; k < a.d; k += 32) top = fmaxf(top, fabsf(__uint_as_float((uint32_t)q[k] << 16)));
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+      const int e = (int)(__float_as_uint(top) >> 23) - 127;
+      if (top > 0.f && e < 128) norm = __uint_as_float((uint32_t)(127 - min(max(e, -126), 126)) << 23);
+    }
+    if (lane == 0) sC[c] = norm;
   }
-  DGQ_CUDA_OK(launch_pdl(enc_attn_rows_kernel<BF, CACHED>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, stream, a));
+  __syncthreads();
+  for (int i = threadIdx.x; i < NTL * KSTEPS * 32; i += 128) {
+    const int l = i & 31, k = (i >> 5) % KSTEPS, nt = (i >> 5) / KSTEPS;
+    const int c = nt * 8 + (l >> 2), f = ((l & 3) + 4 * (k / KW)) * Cfg::KU + (k % KW) * 4;
+    const uint16_t* q = q_row(col0 + c);
+    uint2 x = make_uint2(0, 0);
+    if (q && f < a.d) x = *reinterpret_cast<const uint2*>(q + f);
+    if (I8 && bf) {
+      const float2 lo = unpack16<true>(x.x), hi = unpack16<true>(x.y);
+      const float n = sC[c];
+      x = make_uint2(pack16<false>(lo.x * n, lo.y * n), pack16<false>(hi.x * n, hi.y * n));
+    }
+    sQ[i] = x;
+  }
+  __syncthreads();
+  float f[NTL][2];
+  int sees[NTL][2];
+#pragma unroll
+  for (int nt = 0; nt < NTL; ++nt)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int c = nt * 8 + 2 * lt + k, i = (col0 + c) / group;
+      f[nt][k] = a.scale_log2 / sC[c];
+      sees[nt][k] = i < rq.nq ? enc_sees(a, rq, i) : 0;
+    }
+
+  // ------------------------------------------------------------ the keys
+  float m[NTL][2], z[NTL][2], o[MT][NTL][4];
+#pragma unroll
+  for (int nt = 0; nt < NTL; ++nt)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      m[nt][k] = -INFINITY;
+      z[nt][k] = 0.f;
+    }
+#pragma unroll
+  for (int j = 0; j < MT; ++j)
+#pragma unroll
+    for (int nt = 0; nt < NTL; ++nt)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[j][nt][k] = 0.f;
+  uint2 qf[NTL == 1 ? KSTEPS : 1];
+  if (NTL == 1) {
+#pragma unroll
+    for (int k = 0; k < KSTEPS; ++k) qf[k] = sQ[k * 32 + lane];
+  }
+
+  for (; step < step1; step += Cfg::WARPS) {
+    float s[GR][NTL][4];
+#pragma unroll
+    for (int i = 0; i < GR; ++i)
+#pragma unroll
+      for (int nt = 0; nt < NTL; ++nt)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s[i][nt][k] = 0.f;
+#pragma unroll
+    for (int r = 0; r < KR; ++r)
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        uint32_t x[GR][4];
+#pragma unroll
+        for (int i = 0; i < GR; ++i) {
+          if (I8) {
+            const uint4 &p = kx[i][0][r], &q = kx[i][1][r];
+            const uint32_t u = (w == 0 ? p.x : w == 1 ? p.y : w == 2 ? p.z : p.w) ^ 0x80808080u;
+            const uint32_t v = (w == 0 ? q.x : w == 1 ? q.y : w == 2 ? q.z : q.w) ^ 0x80808080u;
+            x[i][0] = biased_lo(u);
+            x[i][1] = biased_lo(v);
+            x[i][2] = biased_hi(u);
+            x[i][3] = biased_hi(v);
+          } else {
+            x[i][0] = w ? kx[i][0][r].z : kx[i][0][r].x;
+            x[i][1] = w ? kx[i][1][r].z : kx[i][1][r].x;
+            x[i][2] = w ? kx[i][0][r].w : kx[i][0][r].y;
+            x[i][3] = w ? kx[i][1][r].w : kx[i][1][r].y;
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NTL; ++nt) {
+          const uint2 q = NTL == 1 ? qf[r * KW + w] : sQ[(nt * KSTEPS + r * KW + w) * 32 + lane];
+#pragma unroll
+          for (int i = 0; i < GR; ++i) ef_mma<M_BF>(s[i][nt], x[i][0], x[i][1], x[i][2], x[i][3], q);
+        }
+      }
+    // exponents, in units that include the value's scale
+    float fk[GR], lv[GR], iv[GR];
+    int key[GR];
+#pragma unroll
+    for (int i = 0; i < GR; ++i) {
+      key[i] = step * Cfg::CH + i * 16 + lg;
+      fk[i] = 1.f;
+      lv[i] = 0.f;
+      iv[i] = 1.f;
+      if (I8) {
+        const float v = vs[i] == 0.f ? 9.094947e-13f : fmaxf(vs[i], 7.8886091e-31f);
+        fk[i] = ks[i];
+        lv[i] = vs[i] < 0.f ? -INFINITY : log2f(v);
+        iv[i] = 1.f / v;
+        if (vs[i] < 0.f) key[i] = INT_MAX - 8;
+      }
+    }
+    load_k(step + Cfg::WARPS);
+    bool move = false;
+    float top[NTL][2];
+#pragma unroll
+    for (int nt = 0; nt < NTL; ++nt)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        top[nt][k] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < GR; ++i) {
+          const float fc = f[nt][k] * fk[i];
+          s[i][nt][k] = key[i] < sees[nt][k] ? fmaf(s[i][nt][k], fc, lv[i]) : -INFINITY;
+          s[i][nt][k + 2] = key[i] + 8 < sees[nt][k] ? fmaf(s[i][nt][k + 2], fc, lv[i]) : -INFINITY;
+          top[nt][k] = max3(top[nt][k], s[i][nt][k], s[i][nt][k + 2]);
+        }
+        move |= top[nt][k] > m[nt][k] + EA_LAZY;
+      }
+    if (__any_sync(0xFFFFFFFFu, move)) {
+#pragma unroll
+      for (int nt = 0; nt < NTL; ++nt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float t = fmaxf(top[nt][k], m[nt][k]);
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, x));
+          const float fall = t == -INFINITY ? 1.f : ex2_approx(m[nt][k] - t);
+          m[nt][k] = t;
+          z[nt][k] *= fall;
+#pragma unroll
+          for (int j = 0; j < MT; ++j) {
+            o[j][nt][k] *= fall;
+            o[j][nt][k + 2] *= fall;
+          }
+        }
+    }
+    uint2 pf[GR][NTL];
+#pragma unroll
+    for (int nt = 0; nt < NTL; ++nt)
+#pragma unroll
+      for (int i = 0; i < GR; ++i) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const float base = m[nt][k] == -INFINITY ? 0.f : m[nt][k];
+          s[i][nt][k] = ex2_approx(s[i][nt][k] - base);
+          s[i][nt][k + 2] = ex2_approx(s[i][nt][k + 2] - base);
+          z[nt][k] = fmaf(s[i][nt][k] + s[i][nt][k + 2], iv[i], z[nt][k]);
+        }
+        pf[i][nt].x = transpose8x8(pack16<M_BF>(s[i][nt][0], s[i][nt][1]));
+        pf[i][nt].y = transpose8x8(pack16<M_BF>(s[i][nt][2], s[i][nt][3]));
+      }
+#pragma unroll
+    for (int i = 0; i < GR; ++i)
+#pragma unroll
+      for (int r = 0; r < VR; ++r)
+#pragma unroll
+        for (int w = 0; w < Cfg::VB / 4; ++w) {
+          uint32_t x[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint4& p = vx[i][k][r];
+            x[k] = w == 0 ? p.x : w == 1 ? p.y : w == 2 ? p.z : p.w;
+          }
+          if (I8) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[k] ^= 0x80808080u;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              const uint32_t y0 = __byte_perm(x[0], x[1], half ? 0x7362 : 0x5140), y1 = __byte_perm(x[2], x[3], half ? 0x7362 : 0x5140);
+              const uint32_t a0 = biased_lo(y0), a1 = biased_hi(y0), a2 = biased_lo(y1), a3 = biased_hi(y1);
+#pragma unroll
+              for (int nt = 0; nt < NTL; ++nt) ef_mma<M_BF>(o[r * (Cfg::VU / 2) + w * 2 + half][nt], a0, a1, a2, a3, pf[i][nt]);
+            }
+          } else {
+            const uint32_t a0 = __byte_perm(x[0], x[1], 0x5410), a1 = __byte_perm(x[0], x[1], 0x7632);
+            const uint32_t a2 = __byte_perm(x[2], x[3], 0x5410), a3 = __byte_perm(x[2], x[3], 0x7632);
+#pragma unroll
+            for (int nt = 0; nt < NTL; ++nt) ef_mma<M_BF>(o[r * 4 + w][nt], a0, a1, a2, a3, pf[i][nt]);
+          }
+        }
+    load_v(step + Cfg::WARPS);
+    find_pages(step + 2 * Cfg::WARPS);
+  }
+
+  // ------------------------------------------------------------ the warps of the block
+#pragma unroll
+  for (int nt = 0; nt < NTL; ++nt)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      float t = z[nt][k];
+#pragma unroll
+      for (int x = 4; x < 32; x <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, x);
+      if (lg == 0) {
+        sM[warp * N + nt * 8 + 2 * lt + k] = m[nt][k];
+        sZ[warp * N + nt * 8 + 2 * lt + k] = t;
+      }
+    }
+#pragma unroll
+  for (int j = 0; j < MT; ++j) {
+    const int feature = (lg + 8 * (j / (Cfg::VU / 2))) * Cfg::VU + (j % (Cfg::VU / 2)) * 2;
+    if (feature < Cfg::DMAX) {
+#pragma unroll
+      for (int nt = 0; nt < NTL; ++nt)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          *reinterpret_cast<float2*>(sO + (warp * N + nt * 8 + 2 * lt + k) * Cfg::O_LD + feature) = make_float2(o[j][nt][k], o[j][nt][k + 2]);
+    }
+  }
+  __syncthreads();
+  if (threadIdx.x < N) {
+    const int c = threadIdx.x;
+    float top = sM[c];
+#pragma unroll
+    for (int w = 1; w < Cfg::WARPS; ++w) top = fmaxf(top, sM[w * N + c]);
+    float sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < Cfg::WARPS; ++w) {
+      const float fall = top == -INFINITY ? 0.f : ex2_approx(sM[w * N + c] - top);
+      sF[w * N + c] = fall;
+      sum = fmaf(sZ[w * N + c], fall, sum);
+    }
+    cM[c] = top;
+    cZ[c] = sum;
+  }
+  __syncthreads();
+  const int quads = a.d / 4;
+  const int cols = min(N, rq.nq * group - col0);  // columns that exist (none: negative)
+  auto of_block = [&](int c, int q) {
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < Cfg::WARPS; ++w) {
+      const float4 y = *reinterpret_cast<const float4*>(sO + (w * N + c) * Cfg::O_LD + q * 4);
+      const float fall = sF[w * N + c];
+      x = make_float4(fmaf(y.x, fall, x.x), fmaf(y.y, fall, x.y), fmaf(y.z, fall, x.z), fmaf(y.w, fall, x.w));
+    }
+    return x;
+  };
+  auto put = [&](int c, int q, float4 x, float sum) {
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    const int i = (col0 + c) / group, h = g * group + (col0 + c) % group;
+    uint16_t* out = (uint16_t*)a.O.ptr + b * a.O.batch + (rq.q_row + i) * a.O.token + h * a.O.head;
+    *reinterpret_cast<uint2*>(out + q * 4) = bf ? make_uint2(pack16<true>(x.x * inv, x.y * inv), pack16<true>(x.z * inv, x.w * inv))
+                                                : make_uint2(pack16<false>(x.x * inv, x.y * inv), pack16<false>(x.z * inv, x.w * inv));
+  };
+  if (splits == 1) {
+    for (int u = threadIdx.x; u < cols * quads; u += 128) put(u / quads, u % quads, of_block(u / quads, u % quads), cZ[u / quads]);
+    return;
+  }
+  // ------------------------------------------------------------ the blocks of the cluster
+  // Every block leaves its sum in its first slab (a thread reads and writes the same place), then adds up its share of the
+  // columns' features over all blocks.
+  for (int u = threadIdx.x; u < cols * quads; u += 128) {
+    const int c = u / quads, q = u % quads;
+    const float4 x = of_block(c, q);
+    *reinterpret_cast<float4*>(sO + c * Cfg::O_LD + q * 4) = x;
+  }
+  const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  cluster.sync();
+  for (int u = threadIdx.x * splits + split; u < cols * quads; u += 128 * splits) {
+    const int c = u / quads, q = u % quads;
+    float top = -INFINITY;
+    for (int r = 0; r < splits; ++r) top = fmaxf(top, *cluster.map_shared_rank(cM + c, r));
+    float sum = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int r = 0; r < splits; ++r) {
+      const float fall = top == -INFINITY ? 0.f : ex2_approx(*cluster.map_shared_rank(cM + c, r) - top);
+      const float4 y = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sO + c * Cfg::O_LD + q * 4, r));
+      sum = fmaf(*cluster.map_shared_rank(cZ + c, r), fall, sum);
+      x = make_float4(fmaf(y.x, fall, x.x), fmaf(y.y, fall, x.y), fmaf(y.z, fall, x.z), fmaf(y.w, fall, x.w));
+    }
+    put(c, q, x, sum);
+  }
+  cluster.sync();  // nobody leaves while its shared memory is being read
+}
+
+template <int SRC, int DC, int NTL>
+static dgq_status ef_launch(const EncAttnArgs& a, cudaStream_t stream) {
+  using Cfg = EfCfg<SRC, DC, NTL>;
+  const auto kernel = enc_attn_few_kernel<SRC, DC, NTL>;
+  static std::atomic<bool> attr_set[64];
+  int dev = 0, sms = 0;
+  DGQ_CUDA_OK(cudaGetDevice(&dev));
+  DGQ_CUDA_OK(sm_count(&sms));
+  if (dev >= 64 || !attr_set[dev].load()) {
+    DGQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
+    if (dev < 64) attr_set[dev].store(true);
+  }
+  const int64_t columns = (int64_t)a.nq * (a.Hq / a.Hkv), blocks_z = (columns + Cfg::N - 1) / Cfg::N;
+  // blocks of a request's head share its keys while each has 16 steps of its four warps or the GPU has room
+  const int64_t steps = ((int64_t)a.nk + Cfg::CH - 1) / Cfg::CH;
+  int splits = 1;
+  const int64_t base = a.B * (int64_t)a.Hkv * blocks_z;
+  while (splits < 8 && steps > splits * Cfg::WARPS && (steps > splits * 64 || base * splits < 2 * sms)) splits *= 2;
+  if ((int64_t)a.B * splits > INT_MAX || a.Hkv > 65535 || blocks_z > 65535) return DGQ_ERR_UNSUPPORTED;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(a.B * splits), (unsigned)a.Hkv, (unsigned)blocks_z);
+  cfg.blockDim = dim3(128);
+  cfg.dynamicSmemBytes = Cfg::SMEM;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)splits;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  DGQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a, splits));
   g_launches += 1;
   DGQ_CUDA_OK(cudaGetLastError());
   return DGQ_OK;
+}
+
+template <int SRC, int DC>
+static dgq_status ef_launch_columns(const EncAttnArgs& a, cudaStream_t stream) {
+  const int64_t columns = (int64_t)a.nq * (a.Hq / a.Hkv);
+  if (columns <= 8) return ef_launch<SRC, DC, 1>(a, stream);
+  if (columns <= 16 || DC == 3) return ef_launch<SRC, DC, 2>(a, stream);
+  return ef_launch<SRC, DC, DC == 3 ? 2 : 4>(a, stream);
+}
+template <bool BF, bool CACHED>
+static dgq_status ef_launch_size(const EncAttnArgs& a, cudaStream_t stream) {
+  constexpr int SRC = CACHED ? EF_I8 : BF ? EF_BF16 : EF_F16;
+  if (a.d <= 64) return ef_launch_columns<SRC, 1>(a, stream);
+  if (a.d <= 128) return ef_launch_columns<SRC, 2>(a, stream);
+  return ef_launch_columns<SRC, 3>(a, stream);
+}
+
+// ------------------------------------------------------------------ launch
+template <bool BF, bool CACHED>
+static dgq_status enc_attn_launch(const EncAttnArgs& a, cudaStream_t stream) {
+  if (a.nq <= 16) return ef_launch_size<BF, CACHED>(a, stream);
+  EncAttnArgs t = a;
+  if (t.scale_log2 == 0.f) t.scale_log2 = 1.17549435e-38f;  // hidden keys are -inf, which 0 would make NaN
+  if (a.d <= 64) return ea_launch_tiles<1, BF, CACHED>(t, stream);
+  if (a.d <= 128) return ea_launch_tiles<2, BF, CACHED>(t, stream);
+  return ea_launch_tiles<3, BF, CACHED>(t, stream);
 }
 
 }  // namespace dgq
@@ -705,7 +1151,8 @@ extern "C" dgq_status dgq_encoder_attn(const dgq_rows* Q, const dgq_rows* K, con
   a.d = d;
   a.scale_log2 = (float)(1.4426950408889634 * (double)scale);
   a.kv_lens = kv_lens;
-  return dtype == DGQ_BF16 ? enc_attn_launch<true, false>(a, (cudaStream_t)stream) : enc_attn_launch<false, false>(a, (cudaStream_t)stream);
+  a.bf = dtype == DGQ_BF16;
+  return a.bf ? enc_attn_launch<true, false>(a, (cudaStream_t)stream) : enc_attn_launch<false, false>(a, (cudaStream_t)stream);
 }
 
 extern "C" dgq_status dgq_cached_attn(const dgq_kv_cache* cache, const dgq_rows* Q, const dgq_rows* O, int dtype, int B,
@@ -742,5 +1189,6 @@ extern "C" dgq_status dgq_cached_attn(const dgq_kv_cache* cache, const dgq_rows*
   a.q_start = q_start;
   a.n_rows = n_rows;
   a.causal = causal != 0;
-  return dtype == DGQ_BF16 ? enc_attn_launch<true, true>(a, (cudaStream_t)stream) : enc_attn_launch<false, true>(a, (cudaStream_t)stream);
+  a.bf = dtype == DGQ_BF16;
+  return a.bf ? enc_attn_launch<true, true>(a, (cudaStream_t)stream) : enc_attn_launch<false, true>(a, (cudaStream_t)stream);
 }
