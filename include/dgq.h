@@ -240,7 +240,7 @@ typedef struct {
  * kv_lens[b] of the nk keys (dev int32 [B]; values outside 0..nk are taken as the nearer end; NULL: all nk), with scores and
  * softmax statistics in fp32 and weights rounded to the tensors' type for the product.  A request without keys gives zeros.
  * What K and V hold behind kv_lens[b] may be anything, NaN included.  Q, O [B, nq, Hq, d]; K, V [B, nk, Hkv, d]; Hq a
- * multiple of Hkv; d a multiple of 8 up to 160; any nq, nk >= 1.
+ * multiple of Hkv; d a multiple of 8 up to 160; nq and nk 1 .. 2^30.
  * Errors: INVALID_ARG (also: a zero or negative stride where none may be, scale not finite), ALIGNMENT, UNSUPPORTED, CUDA. */
 dgq_status dgq_encoder_attn(const dgq_rows* Q, const dgq_rows* K, const dgq_rows* V, const dgq_rows* O, int dtype, int B,
                             int Hq, int Hkv, int nq, int nk, int d, float scale, const int32_t* kv_lens, void* stream);
@@ -270,9 +270,10 @@ dgq_status dgq_kv_plan(const int32_t* lens, const int32_t* n_new, int B, const i
 
 /* Rows K[t], V[t] (t < T; [1, T, n_heads, d]) into slots[t] (dev int32 [T]; negative: the row is skipped).  The rows of one page
  * stand next to each other in ascending order, as dgq_kv_plan gives them, and no slot comes twice in a call.  For each page and
- * head, in fp32: top = max |x| over the page's rows of this call, s = top * (1 / 127); a page whose row 0 is among them forgets what it
- * held, any other one keeps its rows below the first new one: s = max(s, scale), and where s has grown, their codes become
- * clamp(rint(code * scale / s), -127, 127).  New codes are clamp(rint(x / s), -127, 127), 0 where s is 0.  Rows behind the
+ * head, in fp32: top = max |x| over the page's rows of this call, s = max(top * (1 / 127), 2^-126), 0 where top is 0; a page whose
+ * row 0 is among them forgets what it held, any other one keeps its rows below the first new one: s = max(s, scale), and where s has
+ * grown, their codes become rint(code * (scale * inv)), inv = 1 / s.  New codes are rint(x * inv), the product rounded once (to
+ * the nearest whole number, ties to even), 0 where s is 0.  Rows behind the
  * new ones stay as they are.  Inputs must be finite.  A slot beyond the cache is skipped and recorded as
  * DGQ_ERR_INVALID_ARG in the status word.
  * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED, CUDA. */
@@ -290,7 +291,7 @@ dgq_status dgq_kv_read(const dgq_kv_cache* cache, const int32_t* slots, int64_t 
  * q_start NULL: Q, O [B, max_nq, Hq, d].  Else Q, O [1, n_rows, Hq, d] packed: request b has rows q_start[b] .. q_start[b + 1] - 1
  * (dev int32 [B + 1], ascending), at most max_nq of them; other rows of O stay as they are.  causal != 0: row i of n sees the first
  * kv_lens[b] - n + i + 1 tokens (the n queries belong to the last n tokens).  Hq a multiple of cache->n_heads.  Pages may be
- * shared by requests.  Weights are rounded to fp16 for the product with the codes, whatever `dtype` is.
+ * shared by requests.  max_pages * page, max_nq and n_rows are at most 2^30.  Weights are rounded to fp16 for the product with the codes, whatever `dtype` is.
  * Found on the device and recorded as DGQ_ERR_INVALID_ARG in the status word: table entries outside the cache (their tokens
  * count as absent), more than max_nq rows or rows beyond n_rows (left out).  n_rows is ignored where q_start is NULL.
  * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED, CUDA. */

@@ -18,7 +18,7 @@ struct EncAttnArgs {
   // the cache (K and V above unused)
   const int8_t *k_codes, *v_codes;
   const float *k_scale, *v_scale;
-  int n_pages, page, max_pages;
+  int n_pages, page, page_log2, max_pages;
   const int32_t* table;         // dev [B, max_pages]
   const int32_t* q_start;       // dev [B + 1] or null (nq queries each)
   int64_t n_rows;
@@ -55,6 +55,7 @@ __device__ __forceinline__ int enc_sees(const EncAttnArgs& a, const EncRequest& 
 constexpr int EA_Q = 128;                 // query rows of a tile
 constexpr int EA_K = 128;                 // keys of a block
 constexpr int EA_PANEL = 128 * 128;       // bytes of 64 features of 128 rows
+constexpr int EA_MOST = 1 << 30;          // queries or keys of a request (sums of an index and a block stay below 2^31)
 constexpr float EA_LAZY = 8.0f;           // a row's reference follows its maximum once that is 2^8 above it
 
 template <int NP, bool CACHED>
@@ -143,9 +144,21 @@ __device__ __forceinline__ void codes_to_16(uint32_t w, uint32_t& lo, uint32_t& 
   }
 }
 
+// Both good to 2^-22 for normal numbers.
+__device__ __forceinline__ float lg2_approx(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // The page of a request's token, or -1 (recorded) where the table says nothing usable.
 __device__ __forceinline__ int ea_page_of(const EncAttnArgs& a, int b, int token) {
-  const int p = __ldg(a.table + (int64_t)b * a.max_pages + token / a.page);
+  const int p = __ldg(a.table + (int64_t)b * a.max_pages + (token >> a.page_log2));
   if (p >= 0 && p < a.n_pages) return p;
   record_error(DGQ_ERR_INVALID_ARG);
   return -1;
@@ -161,8 +174,8 @@ __device__ __forceinline__ EaPage ea_page_scales(const EncAttnArgs& a, int b, in
   const float vs = __ldg(a.v_scale + ph);
   const float v = vs == 0.f ? 9.094947e-13f : fmaxf(vs, 7.8886091e-31f);
   c.k = fmaxf(__ldg(a.k_scale + ph) * scale_log2, 1.17549435e-38f);
-  c.lv = log2f(v);
-  c.iv = 1.0f / v;
+  c.lv = lg2_approx(v);
+  c.iv = rcp_approx(v);
   return c;
 }
 
@@ -354,7 +367,7 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
         if (token >= rq.len) continue;
         const int p = ea_page_of(a, b, token);
         if (p >= 0)
-          x[i] = __ldg(reinterpret_cast<const uint4*>(codes + (((int64_t)p * a.Hkv + g) * a.page + token % a.page) * row_bytes) + c);
+          x[i] = __ldg(reinterpret_cast<const uint4*>(codes + ((((int64_t)p * a.Hkv + g) << a.page_log2) + (token & (a.page - 1))) * row_bytes) + c);
       }
     };
     if (nb > 0) load(0);
@@ -587,6 +600,8 @@ static dgq_status ea_launch_tiles(const EncAttnArgs& a, cudaStream_t stream) {
 // code for keys, 1.5 for values).  Each warp has its own running maximum and sums; the warps of a block meet in shared memory,
 // the blocks of a request in the shared memory of their cluster, in a fixed order.
 enum { EF_I8 = 0, EF_F16 = 1, EF_BF16 = 2 };
+constexpr int EF_SPLITS = 16;   // most blocks of a cluster
+constexpr int EF_SORTED = 128;  // most requests that are taken in the order of their lengths
 
 template <int SRC, int DC, int NTL>
 struct EfCfg {
@@ -647,7 +662,7 @@ __device__ __forceinline__ uint2 ld_stream8(const void* p) {
 }
 
 template <int SRC, int DC, int NTL>
-__global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant__ EncAttnArgs a, int splits) {
+__global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant__ EncAttnArgs a, int splits, int by_length) {
   using Cfg = EfCfg<SRC, DC, NTL>;
   constexpr bool I8 = Cfg::I8;
   constexpr bool M_BF = SRC == EF_BF16;       // type of both products' operands; codes: fp16
@@ -665,10 +680,25 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, lg = lane >> 2, lt = lane & 3;
   const int group = a.Hq / a.Hkv;
-  const int split = (int)blockIdx.x % splits;
-  const int g = (int)blockIdx.y, b = (int)(blockIdx.x / splits), col0 = (int)blockIdx.z * N;
+  const int split = (int)blockIdx.x % splits;  // heads lie in x too, so that a request's blocks are dealt out together
+  const int g = (int)(blockIdx.x / splits) % a.Hkv, col0 = (int)blockIdx.y * N;
+  int b = (int)(blockIdx.x / splits) / a.Hkv;
   pdl_launch_dependents();
   pdl_wait();
+  if (by_length) {
+    // longest first, so that the last blocks to start are short ones: the request whose rank is this block's number
+    __shared__ int lens[EF_SORTED], mine;
+    const int j = threadIdx.x;
+    if (j < a.B) lens[j] = a.kv_lens[j];
+    __syncthreads();
+    if (j < a.B) {
+      int rank = 0;
+      for (int k = 0; k < a.B; ++k) rank += lens[k] > lens[j] || (lens[k] == lens[j] && k < j);
+      if (rank == b) mine = j;
+    }
+    __syncthreads();
+    b = mine;
+  }
   const EncRequest rq = enc_request(a, b);
 
   // this block's keys: whole steps, the same number for every block of the cluster but the last ones
@@ -677,85 +707,82 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
   int step = split * share + warp;
 
   // ------------------------------------------------------------ loads of a step
+  // Nothing here is conditional on a lane: a piece beyond a row is another one's instead (Q is zero there, or the feature is not
+  // written), a group of absent keys is page 0's (their weights are 0), and a 16-bit row beyond the keys is the last one's.
   const int row_bytes = I8 ? kv_row_bytes(a.d) : a.d * 2;
   uint4 kx[GR][2][KR];
   uint4 vx[GR][4][VR];
   float ks[GR], vs[GR];
   int page_next[GR];
+  const int32_t* table = I8 ? a.table + (int64_t)b * a.max_pages : nullptr;
+  int kc[KR], vc[VR];  // offset of a lane's pieces in a row
+#pragma unroll
+  for (int r = 0; r < KR; ++r) kc[r] = (lt + 4 * r) * 16 < row_bytes ? (lt + 4 * r) * 16 : 0;
+#pragma unroll
+  for (int r = 0; r < VR; ++r) vc[r] = (lg + 8 * r) * Cfg::VB < row_bytes ? (lg + 8 * r) * Cfg::VB : 0;
+  const uint8_t* k_rows = I8 ? nullptr : (const uint8_t*)a.K.ptr + 2 * (b * a.K.batch + g * a.K.head);
+  const uint8_t* v_rows = I8 ? nullptr : (const uint8_t*)a.V.ptr + 2 * (b * a.V.batch + g * a.V.head);
   auto find_pages = [&](int st) {
-    if (!I8) return;
+    if (!I8 || st >= step1) return;
 #pragma unroll
     for (int i = 0; i < GR; ++i) {
       const int key = st * Cfg::CH + i * 16;
-      page_next[i] = -1;
-      if (st < step1 && key < rq.len) page_next[i] = __ldg(a.table + (int64_t)b * a.max_pages + key / a.page);
+      page_next[i] = key < rq.len ? __ldg(table + (key >> a.page_log2)) : -2;
     }
   };
   auto load_k = [&](int st) {
+    if (st >= step1) return;
 #pragma unroll
     for (int i = 0; i < GR; ++i) {
       const int key = st * Cfg::CH + i * 16;
-      const uint8_t* base = nullptr;
-      int64_t pitch = row_bytes;
-      bool real = st < step1 && key < rq.len;
       if (I8) {
         const int p = page_next[i];
-        if (real && (p < 0 || p >= a.n_pages)) {
-          real = false;
-          record_error(DGQ_ERR_INVALID_ARG);
-        }
+        const bool real = p >= 0 && p < a.n_pages;
+        if (!real && p != -2) record_error(DGQ_ERR_INVALID_ARG);
         const int64_t ph = real ? (int64_t)p * a.Hkv + g : 0;
-        ks[i] = vs[i] = -1.f;  // absent
-        if (real) {
-          ks[i] = __ldg(a.k_scale + ph);
-          vs[i] = __ldg(a.v_scale + ph);
-        }
-        base = (const uint8_t*)a.k_codes + (ph * a.page + key % a.page) * row_bytes;
+        ks[i] = __ldg(a.k_scale + ph);
+        vs[i] = real ? __ldg(a.v_scale + ph) : -1.f;  // negative: absent
+        const uint8_t* base = (const uint8_t*)a.k_codes + ((ph << a.page_log2) + (key & (a.page - 1))) * row_bytes + lg * row_bytes;
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh)
+#pragma unroll
+          for (int r = 0; r < KR; ++r) kx[i][hh][r] = ld_stream16(base + hh * 8 * row_bytes + kc[r]);
       } else {
-        pitch = a.K.token * 2;
-        base = (const uint8_t*)a.K.ptr + 2 * (b * a.K.batch + g * a.K.head) + key * pitch;
-      }
 #pragma unroll
-      for (int hh = 0; hh < 2; ++hh)
+        for (int hh = 0; hh < 2; ++hh) {
+          const uint8_t* base = k_rows + 2 * a.K.token * min(key + lg + 8 * hh, rq.len - 1);
 #pragma unroll
-        for (int r = 0; r < KR; ++r) {
-          const int c = (lt + 4 * r) * 16;
-          kx[i][hh][r] = make_uint4(0, 0, 0, 0);
-          if (real && c < row_bytes && (I8 || key + lg + 8 * hh < rq.len)) kx[i][hh][r] = ld_stream16(base + (lg + 8 * hh) * pitch + c);
+          for (int r = 0; r < KR; ++r) kx[i][hh][r] = ld_stream16(base + kc[r]);
         }
+      }
     }
   };
   auto load_v = [&](int st) {
+    if (st >= step1) return;
 #pragma unroll
     for (int i = 0; i < GR; ++i) {
       const int key = st * Cfg::CH + i * 16;
       const uint8_t* base = nullptr;
-      int64_t pitch = row_bytes;
-      bool real = st < step1 && key < rq.len;
       if (I8) {
         const int p = page_next[i];
-        real = real && p >= 0 && p < a.n_pages;
-        base = (const uint8_t*)a.v_codes + ((real ? (int64_t)p * a.Hkv + g : 0) * a.page + key % a.page) * row_bytes;
-      } else {
-        pitch = a.V.token * 2;
-        base = (const uint8_t*)a.V.ptr + 2 * (b * a.V.batch + g * a.V.head) + key * pitch;
+        const int64_t ph = p >= 0 && p < a.n_pages ? (int64_t)p * a.Hkv + g : 0;
+        base = (const uint8_t*)a.v_codes + ((ph << a.page_log2) + (key & (a.page - 1))) * row_bytes + 2 * lt * row_bytes;
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
+      for (int k = 0; k < 4; ++k) {
+        const int row = (k & 1) + 8 * (k >> 1);
+        const uint8_t* at = I8 ? base + row * row_bytes : v_rows + 2 * a.V.token * min(key + 2 * lt + row, rq.len - 1);
 #pragma unroll
         for (int r = 0; r < VR; ++r) {
-          const int c = (lg + 8 * r) * Cfg::VB, row = 2 * lt + (k & 1) + 8 * (k >> 1);
-          vx[i][k][r] = make_uint4(0, 0, 0, 0);
-          if (real && c < row_bytes && (I8 || key + row < rq.len)) {
-            if (Cfg::VB == 16) {
-              vx[i][k][r] = ld_stream16(base + row * pitch + c);
-            } else {
-              const uint2 x = ld_stream8(base + row * pitch + c);
-              vx[i][k][r].x = x.x;
-              vx[i][k][r].y = x.y;
-            }
+          if (Cfg::VB == 16) {
+            vx[i][k][r] = ld_stream16(at + vc[r]);
+          } else {
+            const uint2 x = ld_stream8(at + vc[r]);
+            vx[i][k][r].x = x.x;
+            vx[i][k][r].y = x.y;
           }
         }
+      }
     }
   };
   find_pages(step);
@@ -881,8 +908,8 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
       if (I8) {
         const float v = vs[i] == 0.f ? 9.094947e-13f : fmaxf(vs[i], 7.8886091e-31f);
         fk[i] = ks[i];
-        lv[i] = vs[i] < 0.f ? -INFINITY : log2f(v);
-        iv[i] = 1.f / v;
+        lv[i] = vs[i] < 0.f ? -INFINITY : lg2_approx(v);
+        iv[i] = rcp_approx(v);
         if (vs[i] < 0.f) key[i] = INT_MAX - 8;
       }
     }
@@ -921,6 +948,7 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
           }
         }
     }
+    const bool ragged = (step + 1) * Cfg::CH > rq.len;  // the last step: a row read in the place of one that is not there has weight 0, which NaN would survive
     uint2 pf[GR][NTL];
 #pragma unroll
     for (int nt = 0; nt < NTL; ++nt)
@@ -947,6 +975,7 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
           for (int k = 0; k < 4; ++k) {
             const uint4& p = vx[i][k][r];
             x[k] = w == 0 ? p.x : w == 1 ? p.y : w == 2 ? p.z : p.w;
+            if (!I8 && ragged && step * Cfg::CH + 2 * lt + (k & 1) + 8 * (k >> 1) >= rq.len) x[k] = 0;
           }
           if (I8) {
 #pragma unroll
@@ -1046,14 +1075,31 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
   for (int u = threadIdx.x * splits + split; u < cols * quads; u += 128 * splits) {
     const int c = u / quads, q = u % quads;
     float top = -INFINITY;
-    for (int r = 0; r < splits; ++r) top = fmaxf(top, *cluster.map_shared_rank(cM + c, r));
+    for (int r = 0; r < splits; r += 4) {
+      float t[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) t[k] = *cluster.map_shared_rank(cM + c, min(r + k, splits - 1));
+      top = fmaxf(top, fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])));
+    }
     float sum = 0.f;
     float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int r = 0; r < splits; ++r) {
-      const float fall = top == -INFINITY ? 0.f : ex2_approx(*cluster.map_shared_rank(cM + c, r) - top);
-      const float4 y = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sO + c * Cfg::O_LD + q * 4, r));
-      sum = fmaf(*cluster.map_shared_rank(cZ + c, r), fall, sum);
-      x = make_float4(fmaf(y.x, fall, x.x), fmaf(y.y, fall, x.y), fmaf(y.z, fall, x.z), fmaf(y.w, fall, x.w));
+    for (int r = 0; r < splits; r += 4) {
+      // four blocks' loads before the first use: one round trip between the SMs for all
+      float t[4], z4[4];
+      float4 y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int from = min(r + k, splits - 1);
+        t[k] = *cluster.map_shared_rank(cM + c, from);
+        z4[k] = *cluster.map_shared_rank(cZ + c, from);
+        y[k] = *reinterpret_cast<const float4*>(cluster.map_shared_rank(sO + c * Cfg::O_LD + q * 4, from));
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float fall = r + k >= splits || top == -INFINITY ? 0.f : ex2_approx(t[k] - top);
+        sum = fmaf(z4[k], fall, sum);
+        x = make_float4(fmaf(y[k].x, fall, x.x), fmaf(y[k].y, fall, x.y), fmaf(y[k].z, fall, x.z), fmaf(y[k].w, fall, x.w));
+      }
     }
     put(c, q, x, sum);
   }
@@ -1070,17 +1116,22 @@ static dgq_status ef_launch(const EncAttnArgs& a, cudaStream_t stream) {
   DGQ_CUDA_OK(sm_count(&sms));
   if (dev >= 64 || !attr_set[dev].load()) {
     DGQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
+    DGQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));  // clusters of 16
     if (dev < 64) attr_set[dev].store(true);
   }
   const int64_t columns = (int64_t)a.nq * (a.Hq / a.Hkv), blocks_z = (columns + Cfg::N - 1) / Cfg::N;
-  // blocks of a request's head share its keys while each has 16 steps of its four warps or the GPU has room
-  const int64_t steps = ((int64_t)a.nk + Cfg::CH - 1) / Cfg::CH;
+  // Blocks that share a head's keys: two to four rounds of the GPU while every warp keeps four steps, and at least one block an
+  // SM while every warp has a step (64 requests of 300 to 8000 keys, 8 heads of 128: 147 us with one block a head,
+  // 131 with two, 136 with four, 169 with eight; longest first 108 with two; a block costs about 7 us beside its keys).
+  const int64_t steps = ((int64_t)a.nk + Cfg::CH - 1) / Cfg::CH, base = a.B * (int64_t)a.Hkv * blocks_z;
   int splits = 1;
-  const int64_t base = a.B * (int64_t)a.Hkv * blocks_z;
-  while (splits < 8 && steps > splits * Cfg::WARPS && (steps > splits * 64 || base * splits < 2 * sms)) splits *= 2;
-  if ((int64_t)a.B * splits > INT_MAX || a.Hkv > 65535 || blocks_z > 65535) return DGQ_ERR_UNSUPPORTED;
+  while (splits < EF_SPLITS && ((base * splits < 6 * sms && steps >= splits * 2 * Cfg::WARPS * 4) || (base * splits < sms && steps > splits * Cfg::WARPS)))
+    splits *= 2;
+  const int64_t blocks = base / blocks_z * splits;
+  if (blocks > INT_MAX || blocks_z > 65535) return DGQ_ERR_UNSUPPORTED;
+  const int by_length = a.kv_lens && a.B > 1 && a.B <= EF_SORTED && blocks > 2 * sms;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(a.B * splits), (unsigned)a.Hkv, (unsigned)blocks_z);
+  cfg.gridDim = dim3((unsigned)blocks, (unsigned)blocks_z);
   cfg.blockDim = dim3(128);
   cfg.dynamicSmemBytes = Cfg::SMEM;
   cfg.stream = stream;
@@ -1092,7 +1143,7 @@ static dgq_status ef_launch(const EncAttnArgs& a, cudaStream_t stream) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl_enabled() ? 2 : 1;
-  DGQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a, splits));
+  DGQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a, splits, by_length));
   g_launches += 1;
   DGQ_CUDA_OK(cudaGetLastError());
   return DGQ_OK;
@@ -1133,7 +1184,7 @@ extern "C" dgq_status dgq_encoder_attn(const dgq_rows* Q, const dgq_rows* K, con
   if (!rows_pointer_ok(Q) || !rows_pointer_ok(K) || !rows_pointer_ok(V) || !rows_pointer_ok(O) || B <= 0 || Hq <= 0 || Hkv <= 0 ||
       nq <= 0 || nk <= 0 || d <= 0 || Hq % Hkv || (dtype != DGQ_F16 && dtype != DGQ_BF16) || !std::isfinite(scale))
     return DGQ_ERR_INVALID_ARG;
-  if (d % 8 || d > KV_MAX_D) return DGQ_ERR_UNSUPPORTED;
+  if (d % 8 || d > KV_MAX_D || nq > EA_MOST || nk > EA_MOST) return DGQ_ERR_UNSUPPORTED;
   dgq_status st;
   if ((st = rows_check(*Q, B, nq, Hq, false)) != DGQ_OK || (st = rows_check(*K, B, nk, Hkv, false)) != DGQ_OK ||
       (st = rows_check(*V, B, nk, Hkv, false)) != DGQ_OK || (st = rows_check(*O, B, nq, Hq, true)) != DGQ_OK)
@@ -1164,7 +1215,7 @@ extern "C" dgq_status dgq_cached_attn(const dgq_kv_cache* cache, const dgq_rows*
   if (!rows_pointer_ok(Q) || !rows_pointer_ok(O) || B <= 0 || Hq <= 0 || max_nq <= 0 || !block_table || max_pages <= 0 || !kv_lens ||
       (q_start && n_rows <= 0) || Hq % cache->n_heads || (dtype != DGQ_F16 && dtype != DGQ_BF16) || !std::isfinite(scale))
     return DGQ_ERR_INVALID_ARG;
-  if ((int64_t)max_pages * cache->page > INT_MAX || n_rows > INT_MAX) return DGQ_ERR_UNSUPPORTED;
+  if ((int64_t)max_pages * cache->page > EA_MOST || max_nq > EA_MOST || (q_start && n_rows > EA_MOST)) return DGQ_ERR_UNSUPPORTED;
   const int64_t qb = q_start ? 1 : B, qn = q_start ? n_rows : max_nq;
   if ((st = rows_check(*Q, qb, qn, Hq, false)) != DGQ_OK || (st = rows_check(*O, qb, qn, Hq, true)) != DGQ_OK) return st;
   EncAttnArgs a = {};
@@ -1184,6 +1235,7 @@ extern "C" dgq_status dgq_cached_attn(const dgq_kv_cache* cache, const dgq_rows*
   a.v_scale = cache->v_scale;
   a.n_pages = cache->n_pages;
   a.page = cache->page;
+  a.page_log2 = kv_log2(cache->page);
   a.max_pages = max_pages;
   a.table = block_table;
   a.q_start = q_start;

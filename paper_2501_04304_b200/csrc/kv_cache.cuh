@@ -15,6 +15,7 @@ constexpr int KV_MAX_D = 160;
 constexpr int KV_MAX_PAGE = 128;
 
 __host__ __device__ inline int kv_row_bytes(int d) { return (d + 15) & ~15; }
+static inline int kv_log2(int page) { return page == 16 ? 4 : page == 32 ? 5 : page == 64 ? 6 : 7; }
 
 // ------------------------------------------------------------------ 16-bit tensors with strides
 static inline bool rows_pointer_ok(const dgq_rows* r) { return r && r->ptr; }
@@ -72,7 +73,7 @@ __device__ __forceinline__ uint32_t pack16(float lo, float hi) {
 struct KvPlanArgs {
   const int32_t *lens, *n_new, *free_pages;
   int32_t *table, *token_start, *kv_lens, *slots, *used;
-  int B, n_free, max_pages, page, n_slots;
+  int B, n_free, max_pages, page, page_log2, n_slots;
 };
 
 constexpr int PLAN_WARPS = 8;
@@ -97,12 +98,13 @@ __global__ void __launch_bounds__(PLAN_WARPS * 32) kv_plan_kernel(const KvPlanAr
   pdl_launch_dependents();
   pdl_wait();
   bool bad = false;
+  const auto pages_of = [&](long long tokens) { return (int)((tokens + a.page - 1) >> a.page_log2); };
   // tokens and pages before this block's requests, and of all requests
   long long sum[4] = {0, 0, 0, 0};
   for (int i = threadIdx.x; i < a.B; i += PLAN_WARPS * 32) {
     int len, add;
     plan_lengths(a, i, len, add, bad);
-    const int pages = (int)(((long long)len + add + a.page - 1) / a.page - ((long long)len + a.page - 1) / a.page);
+    const int pages = pages_of((long long)len + add) - pages_of(len);
     sum[2] += add;
     sum[3] += pages;
     if (i < b0) {
@@ -112,7 +114,7 @@ __global__ void __launch_bounds__(PLAN_WARPS * 32) kv_plan_kernel(const KvPlanAr
   }
   int len = 0, add = 0;
   if (b < a.B) plan_lengths(a, b, len, add, bad);
-  const int have = (int)(((long long)len + a.page - 1) / a.page), need = (int)(((long long)len + add + a.page - 1) / a.page);
+  const int have = pages_of(len), need = pages_of((long long)len + add);
 #pragma unroll
   for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -143,7 +145,7 @@ __global__ void __launch_bounds__(PLAN_WARPS * 32) kv_plan_kernel(const KvPlanAr
     }
     // the page of the tokens that the request has already begun
     int first = -1;
-    if (have > 0 && len % a.page) {
+    if (have > 0 && (len & (a.page - 1))) {
       first = row[have - 1];
       if (first < 0) bad = true;
     }
@@ -155,9 +157,9 @@ __global__ void __launch_bounds__(PLAN_WARPS * 32) kv_plan_kernel(const KvPlanAr
     for (int i = lane; i < add; i += 32) {
       const long long t = start + i;
       if (t >= a.n_slots) break;
-      const int pos = len + i, pi = pos / a.page;
+      const int pos = len + i, pi = pos >> a.page_log2;
       const int page = pi < have ? first : new_page(pi - have);
-      a.slots[t] = page < 0 ? -1 : page * a.page + pos % a.page;
+      a.slots[t] = page < 0 ? -1 : (page << a.page_log2) + (pos & (a.page - 1));
     }
   }
   for (long long t = min(total, (long long)a.n_slots) + blockIdx.x * (PLAN_WARPS * 32) + threadIdx.x; t < a.n_slots;
@@ -178,110 +180,149 @@ struct KvWriteArgs {
   float* scale[2];
   const int32_t* slots;
   int64_t T;
-  int n_pages, n_heads, page, d, chunk;
+  int n_pages, n_heads, page, page_log2, d, chunk;
 };
 
 constexpr int WRITE_THREADS = 128;
+constexpr int WRITE_HELD = 4;  // sixteen-byte pieces of a thread that stay in registers between the two passes
 
-// A block takes the runs of rows of one page that begin among its `chunk` tokens, for one head of K or V: largest value, scale,
-// codes.  The rows are read twice, the second time from L1.
+// Largest magnitude of two 16-bit numbers against `top`, in the type itself (exact).
 template <bool BF>
-__global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(const KvWriteArgs a) {
-  __shared__ float red[WRITE_THREADS / 32];
-  __shared__ int s_len[WRITE_THREADS / 32];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+__device__ __forceinline__ uint32_t absmax16(uint32_t top, uint32_t x) {
+  x &= 0x7FFF7FFFu;
+  if (BF) {
+    const __nv_bfloat162 r = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&top), *reinterpret_cast<const __nv_bfloat162*>(&x));
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
+  const __half2 r = __hmax2(*reinterpret_cast<const __half2*>(&top), *reinterpret_cast<const __half2*>(&x));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Codes of four 16-bit numbers: adding 1.5 * 2^23 to the exact product rounds it to a whole number, whose low byte is the code.  (No
+// clamp: |x| <= 127 s up to the last bit of s, so |x * inv| < 127.5.)
+template <bool BF>
+__device__ __forceinline__ uint32_t codes_of4(uint32_t a, uint32_t b, float inv) {
+  const float2 lo = unpack16<BF>(a), hi = unpack16<BF>(b);
+  const uint32_t y0 = __float_as_uint(fmaf(lo.x, inv, 12582912.f)), y1 = __float_as_uint(fmaf(lo.y, inv, 12582912.f));
+  const uint32_t y2 = __float_as_uint(fmaf(hi.x, inv, 12582912.f)), y3 = __float_as_uint(fmaf(hi.y, inv, 12582912.f));
+  return __byte_perm(__byte_perm(y0, y1, 0x0040), __byte_perm(y2, y3, 0x0040), 0x5410);
+}
+__device__ __forceinline__ float code_as_float(uint32_t biased_word, int i) {
+  return __uint_as_float(__byte_perm(biased_word, 0x4B000000u, 0x7540 + i)) - 8388736.f;  // 2^23 + 128
+}
+
+// THREADS (one warp, or the block for large pages) take the runs of rows of one page that begin among `chunk` tokens, for one
+// head of K or V: largest value, scale, codes.  Most runs fit the registers and are read once.  64 prompts of 20 to 77 rows of
+// 20 x 64 into pages of 16: 43.4 us with a block per run, IEEE divisions and a second read, 18.2 us with the read-back now.
+template <bool BF, int THREADS>
+__global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(const __grid_constant__ KvWriteArgs a) {
+  __shared__ uint32_t red[WRITE_THREADS / 32];
+  constexpr int GROUPS = WRITE_THREADS / THREADS;
+  const int tid = threadIdx.x % THREADS, lane = threadIdx.x & 31;
   const int h = blockIdx.y, which = blockIdx.z;
-  const uint16_t* x = a.x[which] + (int64_t)h * a.head[which];
-  const int64_t ldx = a.token[which];
   const int row_bytes = kv_row_bytes(a.d), units = a.d / 8;
-  const int n_slots = a.n_pages * a.page;
+  const int n_slots = a.n_pages << a.page_log2;
   pdl_launch_dependents();
   pdl_wait();
-  const int64_t t_end = min(a.T, (int64_t)(blockIdx.x + 1) * a.chunk);
-  for (int64_t t = (int64_t)blockIdx.x * a.chunk; t < t_end;) {
-    const int slot = a.slots[t];
-    const int r0 = slot % a.page;
-    if (slot < 0 || slot >= n_slots) {
-      if (slot >= n_slots && tid == 0) record_error(DGQ_ERR_INVALID_ARG);
-      ++t;
-      continue;
+  const int64_t t0 = ((int64_t)blockIdx.x * GROUPS + threadIdx.x / THREADS) * a.chunk;
+  // which of the tokens begin a run: those whose predecessor is not the slot before, and those in row 0 of a page
+  unsigned begins = 0;
+  {
+    const int64_t t = t0 + lane;
+    if (lane < a.chunk && t < a.T) {
+      const int slot = a.slots[t];
+      const bool real = slot >= 0 && slot < n_slots;
+      if (slot >= n_slots) record_error(DGQ_ERR_INVALID_ARG);
+      if (real && ((slot & (a.page - 1)) == 0 || t == 0 || a.slots[t - 1] != slot - 1)) begins = 1;
     }
-    if (r0 > 0 && t > 0 && a.slots[t - 1] == slot - 1) {  // the run began before: another block's, or done
-      ++t;
-      continue;
-    }
-    // length of the run: thread i looks at row i
-    const bool in = t + tid < a.T && r0 + tid < a.page && a.slots[t + tid] == slot + tid;
-    const unsigned ball = __ballot_sync(0xFFFFFFFFu, in);
-    if (lane == 0) s_len[warp] = ball == 0xFFFFFFFFu ? 32 : __ffs(~ball) - 1;
-    __syncthreads();
+    begins = __ballot_sync(0xFFFFFFFFu, begins != 0);
+  }
+  // a thread has the same piece of rows tid / units, + step, ...
+  const int step = THREADS / units, r_first = tid / units, c = tid - r_first * units;
+  const bool works = r_first < step;
+  const uint16_t* x = a.x[which] + (int64_t)h * a.head[which] + c * 8;
+  for (; begins; begins &= begins - 1) {
+    const int64_t t = t0 + (__ffs(begins) - 1);
+    const int slot = a.slots[t], r0 = slot & (a.page - 1);
     int n = 0;
-    for (int w = 0; w < WRITE_THREADS / 32; ++w) {
-      n += s_len[w];
-      if (s_len[w] < 32) break;
-    }
-    const uint16_t* rows = x + t * ldx;
-    float top = 0.f;
-    for (int u = tid; u < n * units; u += WRITE_THREADS) {
-      const int r = u / units, c = u - r * units;
-      const uint4 q = __ldg(reinterpret_cast<const uint4*>(rows + r * ldx) + c);
-      const uint32_t w4[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 f = unpack16<BF>(w4[i]);
-        top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+    for (int more = a.page - r0; n < more; n += 32) {
+      const int i = n + lane;
+      const bool in = i < more && t + i < a.T && a.slots[t + i] == slot + i;
+      const unsigned ball = __ballot_sync(0xFFFFFFFFu, in);
+      if (ball != 0xFFFFFFFFu) {
+        n += __ffs(~ball) - 1;
+        break;
       }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-    if (lane == 0) red[warp] = top;
-    const int64_t ph = (int64_t)(slot / a.page) * a.n_heads + h;
+    const int64_t ph = (int64_t)(slot >> a.page_log2) * a.n_heads + h;
     float* scale = a.scale[which] + ph;
     const float held = r0 > 0 ? *scale : 0.f;
-    __syncthreads();  // also: everyone has read the old scale and the run's length
-    for (int w = 0; w < WRITE_THREADS / 32; ++w) top = fmaxf(top, red[w]);
-    float s = __fmul_rn(top, 1.0f / 127.0f);
-    if (r0 > 0) s = fmaxf(s, held);
-    int8_t* page = a.codes[which] + ph * a.page * row_bytes;
+    const uint16_t* rows = x + t * a.token[which];
+    uint4 q[WRITE_HELD];
+    uint32_t top2 = 0;
+#pragma unroll
+    for (int k = 0; k < WRITE_HELD; ++k) {
+      const int r = r_first + k * step;
+      q[k] = make_uint4(0, 0, 0, 0);
+      if (works && r < n) q[k] = __ldg(reinterpret_cast<const uint4*>(rows + r * a.token[which]));
+    }
+#pragma unroll
+    for (int k = 0; k < WRITE_HELD; ++k)
+      top2 = absmax16<BF>(absmax16<BF>(absmax16<BF>(absmax16<BF>(top2, q[k].x), q[k].y), q[k].z), q[k].w);
+    if (works)
+#pragma unroll 4
+      for (int r = r_first + WRITE_HELD * step; r < n; r += step) {
+        const uint4 y = __ldg(reinterpret_cast<const uint4*>(rows + r * a.token[which]));
+        top2 = absmax16<BF>(absmax16<BF>(absmax16<BF>(absmax16<BF>(top2, y.x), y.y), y.z), y.w);
+      }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top2 = absmax16<BF>(top2, __shfl_xor_sync(0xFFFFFFFFu, top2, o));
+    if (THREADS > 32) {
+      if (lane == 0) red[threadIdx.x >> 5] = top2;
+      __syncthreads();  // also: everyone has read the old scale
+#pragma unroll
+      for (int w = 0; w < THREADS / 32; ++w) top2 = absmax16<BF>(top2, red[w]);
+    } else {
+      __syncwarp();
+    }
+    const float2 top = unpack16<BF>(top2);
+    // a scale below the smallest normal number would have no inverse
+    float s = fmaxf(top.x, top.y);
+    s = s > 0.f ? fmaxf(__fmul_rn(s, 1.0f / 127.0f), 1.17549435e-38f) : 0.f;
+    s = fmaxf(s, held);
+    const float inv = s > 0.f ? __fdiv_rn(1.0f, s) : 0.f;
+    int8_t* page = a.codes[which] + (ph << a.page_log2) * row_bytes;
     if (r0 > 0 && s > held) {
-      for (int u = tid; u < r0 * (row_bytes / 16); u += WRITE_THREADS) {
+      const float ratio = __fmul_rn(held, inv);
+      for (int u = tid; u < r0 * (row_bytes / 16); u += THREADS) {
         uint4* p = reinterpret_cast<uint4*>(page) + u;
-        uint4 q = *p;
-        uint32_t w4[4] = {q.x, q.y, q.z, q.w};
+        const uint4 y = *p;
+        uint32_t w4[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          uint32_t o = 0;
+          const uint32_t w = w4[i] ^ 0x80808080u;
+          uint32_t f[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const float c = (float)(int8_t)(w4[i] >> (8 * k));
-            const int v = __float2int_rn(fminf(fmaxf(rintf(__fdiv_rn(__fmul_rn(c, held), s)), -127.f), 127.f));
-            o |= (uint32_t)(v & 0xFF) << (8 * k);
-          }
-          w4[i] = o;
+          for (int k = 0; k < 4; ++k) f[k] = __float_as_uint(fmaf(code_as_float(w, k), ratio, 12582912.f));
+          w4[i] = __byte_perm(__byte_perm(f[0], f[1], 0x0040), __byte_perm(f[2], f[3], 0x0040), 0x5410);
         }
         *p = make_uint4(w4[0], w4[1], w4[2], w4[3]);
       }
     }
-    for (int u = tid; u < n * units; u += WRITE_THREADS) {
-      const int r = u / units, c = u - r * units;
-      const uint4 q = __ldg(reinterpret_cast<const uint4*>(rows + r * ldx) + c);
-      const uint32_t w4[4] = {q.x, q.y, q.z, q.w};
-      uint32_t o[2] = {0, 0};
+    int8_t* dst = page + r0 * row_bytes + c * 8;
+    const auto put = [&](int r, const uint4& y) {
+      int8_t* at = dst + r * row_bytes;
+      *reinterpret_cast<uint2*>(at) = make_uint2(codes_of4<BF>(y.x, y.y, inv), codes_of4<BF>(y.z, y.w, inv));
+      if (c == units - 1 && (a.d & 8)) *reinterpret_cast<uint2*>(at + 8) = make_uint2(0, 0);
+    };
+    if (works) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float2 f = unpack16<BF>(w4[i]);
-        const float y0 = s > 0.f ? __fdiv_rn(f.x, s) : 0.f, y1 = s > 0.f ? __fdiv_rn(f.y, s) : 0.f;
-        const int v0 = __float2int_rn(fminf(fmaxf(rintf(y0), -127.f), 127.f));
-        const int v1 = __float2int_rn(fminf(fmaxf(rintf(y1), -127.f), 127.f));
-        o[i >> 1] |= ((uint32_t)(v0 & 0xFF) | (uint32_t)(v1 & 0xFF) << 8) << (16 * (i & 1));
-      }
-      int8_t* dst = page + (int64_t)(r0 + r) * row_bytes + c * 8;
-      *reinterpret_cast<uint2*>(dst) = make_uint2(o[0], o[1]);
-      if (c == units - 1 && (a.d & 8)) *reinterpret_cast<uint2*>(dst + 8) = make_uint2(0, 0);
+      for (int k = 0; k < WRITE_HELD; ++k)
+        if (r_first + k * step < n) put(r_first + k * step, q[k]);
+#pragma unroll 2
+      for (int r = r_first + WRITE_HELD * step; r < n; r += step) put(r, __ldg(reinterpret_cast<const uint4*>(rows + r * a.token[which])));
     }
     if (tid == 0) *scale = s;
-    t += n;
-    __syncthreads();  // red and s_len are free again
+    if (THREADS > 32) __syncthreads();  // red is free again
   }
 }
 
@@ -292,41 +333,48 @@ struct KvReadArgs {
   const int8_t* codes[2];
   const float* scale[2];
   const int32_t* slots;
-  int64_t n_units;  // T * heads * d / 8
-  int n_pages, n_heads, page, d;
+  int64_t n_units;                 // T * heads * d / 8
+  uint64_t per_units, per_heads;   // 2^64 / n rounded up: the high half of a product with it is the quotient
+  int n_pages, n_heads, page, page_log2, d;
 };
 
-// One thread: eight values of K and the same eight of V.
+// Two codes (bytes i, i + 1 of a biased word) as values.
 template <bool BF>
-__global__ void __launch_bounds__(256) kv_read_kernel(const KvReadArgs a) {
+__device__ __forceinline__ uint32_t values_of2(uint32_t w, int i, float s) {
+  return pack16<BF>(__fmul_rn(code_as_float(w, i), s), __fmul_rn(code_as_float(w, i + 1), s));
+}
+
+// One thread: eight values of K and the same eight of V.  Quotients of indices below 2^32 by numbers below 2^16 come from one
+// multiplication.
+template <bool BF>
+__global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ KvReadArgs a) {
   pdl_launch_dependents();
   pdl_wait();
-  const int units = a.d / 8, row_bytes = kv_row_bytes(a.d);
+  const int units = a.d / 8, row_bytes = kv_row_bytes(a.d), n_slots = a.n_pages << a.page_log2;
   for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < a.n_units; i += gridDim.x * 256ll) {
-    const int c = (int)(i % units);
-    const int64_t th = i / units;
-    const int h = (int)(th % a.n_heads);
-    const int64_t t = th / a.n_heads;
+    const bool small = a.n_units <= 0xFFFFFFFFll;
+    const int64_t th = units == 1 ? i : small ? (int64_t)__umul64hi(i, a.per_units) : i / units;
+    const int64_t t = a.n_heads == 1 ? th : small ? (int64_t)__umul64hi(th, a.per_heads) : th / a.n_heads;
+    const int c = (int)(i - th * units), h = (int)(th - t * a.n_heads);
     const int slot = a.slots[t];
-    const bool real = slot >= 0 && slot < a.n_pages * a.page;
-    if (slot >= a.n_pages * a.page) record_error(DGQ_ERR_INVALID_ARG);
-    const int64_t ph = real ? (int64_t)(slot / a.page) * a.n_heads + h : 0;
-    const int64_t at = real ? (ph * a.page + slot % a.page) * row_bytes + c * 8 : 0;
+    const bool real = slot >= 0 && slot < n_slots;
+    if (slot >= n_slots) record_error(DGQ_ERR_INVALID_ARG);
+    const int64_t ph = real ? (int64_t)(slot >> a.page_log2) * a.n_heads + h : 0;
+    const int64_t at = ((ph << a.page_log2) + (slot & (a.page - 1))) * row_bytes + c * 8;
+    uint2 q[2] = {make_uint2(0, 0), make_uint2(0, 0)};
+    float s[2] = {0.f, 0.f};
+    if (real) {
+#pragma unroll
+      for (int w = 0; w < 2; ++w) {
+        q[w] = __ldg(reinterpret_cast<const uint2*>(a.codes[w] + at));
+        s[w] = __ldg(a.scale[w] + ph);
+      }
+    }
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      uint2 q = make_uint2(0, 0);
-      float s = 0.f;
-      if (real) {
-        q = *reinterpret_cast<const uint2*>(a.codes[w] + at);
-        s = a.scale[w][ph];
-      }
-      uint32_t o[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const uint32_t two = (k < 2 ? q.x : q.y) >> (16 * (k & 1));
-        o[k] = pack16<BF>(__fmul_rn((float)(int8_t)two, s), __fmul_rn((float)(int8_t)(two >> 8), s));
-      }
-      *reinterpret_cast<uint4*>(a.y[w] + t * a.token[w] + h * a.head[w] + c * 8) = make_uint4(o[0], o[1], o[2], o[3]);
+      const uint32_t u = q[w].x ^ 0x80808080u, v = q[w].y ^ 0x80808080u;
+      *reinterpret_cast<uint4*>(a.y[w] + t * a.token[w] + h * a.head[w] + c * 8) =
+          make_uint4(values_of2<BF>(u, 0, s[w]), values_of2<BF>(u, 2, s[w]), values_of2<BF>(v, 0, s[w]), values_of2<BF>(v, 2, s[w]));
     }
   }
 }
@@ -346,7 +394,7 @@ extern "C" dgq_status dgq_kv_plan(const int32_t* lens, const int32_t* n_new, int
   if (!apart(lens, kv_lens, B) || !apart(n_new, kv_lens, B) || !apart(lens, token_start, B + 1ll) || !apart(n_new, token_start, B + 1ll))
     return DGQ_ERR_INVALID_ARG;
   if (page != 16 && page != 32 && page != 64 && page != 128) return DGQ_ERR_UNSUPPORTED;
-  KvPlanArgs a{lens, n_new, free_pages, block_table, token_start, kv_lens, slots, used, B, n_free, max_pages, page, n_slots};
+  KvPlanArgs a{lens, n_new, free_pages, block_table, token_start, kv_lens, slots, used, B, n_free, max_pages, page, kv_log2(page), n_slots};
   DGQ_CUDA_OK(launch_pdl(kv_plan_kernel, dim3((unsigned)((B + PLAN_WARPS - 1) / PLAN_WARPS)), dim3(PLAN_WARPS * 32), 0,
                          (cudaStream_t)stream, a));
   g_launches += 1;
@@ -378,12 +426,19 @@ extern "C" dgq_status dgq_kv_write(const dgq_kv_cache* cache, const dgq_rows* K,
   a.n_heads = cache->n_heads;
   a.page = cache->page;
   a.d = cache->d;
-  // single tokens (each its own run) want a block each while they fit on the GPU at once; many tokens come as runs
-  a.chunk = T * cache->n_heads * 2 > 148 * 16 * 4 ? 16 : 1;
-  const int64_t blocks = (T + a.chunk - 1) / a.chunk;
+  a.page_log2 = kv_log2(cache->page);
+  // sixteen tokens to a warp where that still fills the GPU: they are one or two runs of a prompt; single tokens (each its own
+  // run) want a warp each
+  int sms = 0;
+  DGQ_CUDA_OK(sm_count(&sms));
+  const int group = cache->page > 32 ? WRITE_THREADS : 32;
+  a.chunk = 16;
+  while (a.chunk > 1 && T * cache->n_heads * 2 / a.chunk * group < (int64_t)sms * 2048) a.chunk /= 4;
+  const int64_t per_block = (int64_t)a.chunk * (WRITE_THREADS / group), blocks = (T + per_block - 1) / per_block;
   if (blocks > INT_MAX) return DGQ_ERR_UNSUPPORTED;
-  DGQ_CUDA_OK(launch_pdl(dtype == DGQ_BF16 ? kv_write_kernel<true> : kv_write_kernel<false>,
-                         dim3((unsigned)blocks, (unsigned)cache->n_heads, 2), dim3(WRITE_THREADS), 0, (cudaStream_t)stream, a));
+  const auto kernel = dtype == DGQ_BF16 ? (group == 32 ? kv_write_kernel<true, 32> : kv_write_kernel<true, WRITE_THREADS>)
+                                        : (group == 32 ? kv_write_kernel<false, 32> : kv_write_kernel<false, WRITE_THREADS>);
+  DGQ_CUDA_OK(launch_pdl(kernel, dim3((unsigned)blocks, (unsigned)cache->n_heads, 2), dim3(WRITE_THREADS), 0, (cudaStream_t)stream, a));
   g_launches += 1;
   DGQ_CUDA_OK(cudaGetLastError());
   return DGQ_OK;
@@ -409,6 +464,9 @@ extern "C" dgq_status dgq_kv_read(const dgq_kv_cache* cache, const int32_t* slot
   }
   a.slots = slots;
   a.n_units = T * cache->n_heads * (cache->d / 8);
+  a.per_units = ~0ull / (uint64_t)(cache->d / 8) + 1;
+  a.per_heads = ~0ull / (uint64_t)cache->n_heads + 1;
+  a.page_log2 = kv_log2(cache->page);
   a.n_pages = cache->n_pages;
   a.n_heads = cache->n_heads;
   a.page = cache->page;

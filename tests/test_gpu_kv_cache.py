@@ -70,12 +70,16 @@ def quantize_reference(x, slots, codes, scale, page):
     for p, rows in by_page.items():
         at, new = [r for r, _ in rows], x[[t for _, t in rows]].float()
         first = min(at)
-        s = new.abs().amax((0, 2)) * torch.tensor(1.0 / 127.0)
+        top = new.abs().amax((0, 2))
+        s = torch.where(top > 0, torch.clamp(top * torch.tensor(1.0 / 127.0), min=2.0 ** -126), torch.zeros(()))
         if first:
             s = torch.maximum(s, scale[p])
+        inv = torch.where(s > 0, 1 / s, torch.zeros(()))
+        if first:
             old = codes[p, :, :first].float()
-            codes[p, :, :first] = torch.where((s > scale[p])[:, None, None], (old * scale[p][:, None, None] / s[:, None, None]).round().clamp(-127, 127), old).to(torch.int8)
-        q = torch.where(s[None, :, None] > 0, new / s[None, :, None], torch.zeros(())).round().clamp(-127, 127).to(torch.int8)
+            ratio = (scale[p] * inv).double()  # products of 24 and fewer bits are exact in 64
+            codes[p, :, :first] = torch.where((s > scale[p])[:, None, None], (old.double() * ratio[:, None, None]).round().float(), old).to(torch.int8)
+        q = (new.double() * inv.double()[None, :, None]).round().to(torch.int8)
         for i, r in enumerate(at):
             codes[p, :, r, :d] = q[i]
             codes[p, :, r, d:] = 0
@@ -112,7 +116,7 @@ def test_write_and_read(heads, d, page, slots, dtype):
     k, v = (torch.randn(len(slots), heads, d, generator=g).to(dtype) * f for f in (1.0, 3.0))
     want = [quantize_reference(x, slots, codes.cpu(), scale.cpu(), page) for x, codes, scale in ((k, c.k, c.k_scale), (v, c.v, c.v_scale))]
     b.kv_write(c, k.cuda(), v.cuda(), dev(slots))
-    # bit for bit: both sides round the same 32-bit quotients
+    # bit for bit: both sides round the same products
     assert torch.equal(c.k.cpu(), want[0][0]) and torch.equal(c.k_scale.cpu(), want[0][1])
     assert torch.equal(c.v.cpu(), want[1][0]) and torch.equal(c.v_scale.cpu(), want[1][1])
     rk, rv = b.kv_read(c, dev(slots), dtype)
