@@ -58,23 +58,29 @@ constexpr int EA_PANEL = 128 * 128;       // bytes of 64 features of 128 rows
 constexpr int EA_MOST = 1 << 30;          // queries or keys of a request (sums of an index and a block stay below 2^31)
 constexpr float EA_LAZY = 8.0f;           // a row's reference follows its maximum once that is 2^8 above it
 
+// NT: query tiles of a block.  Over 16-bit keys one, and two blocks to an SM, whose starts, products and softmaxes then drift apart
+// and run under each other (2 x 10 x 4096 x 64 over 4173 keys: 153 us, with two tiles in one block 191; 128 features 214 and 277).
+// Over a cache two, which share the work of widening every code (2 x 16 of 4 x 2048 x 128 over 6000 codes: 283 us, with one 489).
 template <int NP, bool CACHED>
 struct EaCfg {
-  static constexpr int NT = NP <= 2 ? 2 : 1;          // query tiles of a block
+  static constexpr int NT = CACHED && NP <= 2 ? 2 : 1;
+  static constexpr int BLOCKS = CACHED || NP == 3 ? 1 : 2;   // per SM
   static constexpr bool OWN_P = NP != 2;              // weights have tensor memory of their own (else they lie over the scores)
-  static constexpr int KST = 2, VST = NP <= 2 ? 2 : 1;
+  static constexpr int KST = BLOCKS == 2 && NP == 2 ? 1 : 2, VST = NP == 3 ? 1 : KST;
   static constexpr int SOFTMAX_WARPS = 4 * NT;
-  static constexpr int WARP_TMA = SOFTMAX_WARPS, WARP_MMA = SOFTMAX_WARPS + 1;
-  static constexpr int CONV_WARP0 = SOFTMAX_WARPS + 2;  // CACHED: four warps that bring in keys, four for values
-  static constexpr int WARPS = SOFTMAX_WARPS + 2 + (CACHED ? 8 : 0);
+  static constexpr int WARP_TMA = SOFTMAX_WARPS, WARP_MMA = SOFTMAX_WARPS + 1;  // one issuing warp per tile
+  static constexpr int CONV_WARP0 = SOFTMAX_WARPS + 1 + NT;  // CACHED: the first CONV warps bring in keys, the others values
+  static constexpr int CONV = 4;
+  static constexpr int WARPS = CONV_WARP0 + (CACHED ? 2 * CONV : 0);
   static constexpr int THREADS = WARPS * 32;
+  static constexpr int TMEM = BLOCKS == 2 ? 256 : 512;
   static constexpr int TMEM_P = OWN_P ? NT * 128 : 0, P_STRIDE = OWN_P ? 64 : 128;
   static constexpr int TMEM_O = OWN_P ? NT * 192 : NT * 128, O_STRIDE = NP * 64;
   static constexpr int TILE = NP * EA_PANEL;
   static constexpr int OFF_K = NT * TILE, OFF_V = OFF_K + KST * TILE, OFF_SH = OFF_V + VST * TILE;
   static constexpr int SMEM = 1024 + OFF_SH + 1024;
-  static_assert(SMEM <= 232448, "shared memory budget");
-  static_assert(TMEM_O + NT * O_STRIDE <= 512, "tensor memory budget");
+  static_assert(SMEM * BLOCKS <= 232448 - 1024 * (BLOCKS - 1), "shared memory budget");
+  static_assert(TMEM_O + NT * O_STRIDE <= TMEM, "tensor memory budget");
 };
 
 // Of sixteen keys of a cache: t = S * k, weight 2^(t + lv) with lv = log2 of the page's value scale, its inverse.
@@ -84,7 +90,7 @@ struct EaPage {
 
 struct EaShared {
   uint64_t q_full;
-  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2];
+  uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], v_clean;
   uint64_t s_full[2], p_full[2], o_done[2];
   uint32_t tmem_base;
   int abort_flag;
@@ -103,24 +109,12 @@ __device__ __forceinline__ uint32_t ea_idesc(int n, bool b_mn_major, bool bf, bo
   return (1u << 4) | ((bf ? 1u : 0u) << 7) | ((bf ? 1u : 0u) << 10) | ((negate_a ? 1u : 0u) << 13) |
          ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(EA_Q >> 4) << 24);
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
-        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]),
-        "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
-        "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-      : "memory");
-}
-
-// Waits for the thread's tensor-memory loads; what was loaded into r is not touched before.
-__device__ __forceinline__ void tmem_ld_wait32(uint32_t (&r)[32]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]),
-                 "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]),
-                 "+r"(r[22]), "+r"(r[23]), "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])
-               ::"memory");
+// Nothing that uses r moves in front of this (of a wait for its load before it).
+__device__ __forceinline__ void pin32(uint32_t (&r)[32]) {
+  asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                    "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
+                    "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
+                    "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
 }
 
 // Four codes as four 16-bit numbers, exactly.  fp16: 0x64 in front of a byte is 1024 + byte.  bf16: 0x43 in front of the low seven
@@ -180,7 +174,7 @@ __device__ __forceinline__ EaPage ea_page_scales(const EncAttnArgs& a, int b, in
 }
 
 template <int NP, bool BF, bool CACHED>
-__global__ void __launch_bounds__(EaCfg<NP, CACHED>::THREADS, 1)
+__global__ void __launch_bounds__(EaCfg<NP, CACHED>::THREADS, EaCfg<NP, CACHED>::BLOCKS)
 enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant__ EncAttnArgs a) {
   using Cfg = EaCfg<NP, CACHED>;
   constexpr int NT = Cfg::NT, KST = Cfg::KST, VST = Cfg::VST;
@@ -204,19 +198,20 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
   if (threadIdx.x == 0) {
     mbar_init(&sh->q_full, 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&sh->k_full[i], CACHED ? 4 : 1);
-      mbar_init(&sh->v_full[i], CACHED ? 4 : 1);
-      mbar_init(&sh->k_empty[i], 1);
-      mbar_init(&sh->v_empty[i], 1);
+      mbar_init(&sh->k_full[i], CACHED ? Cfg::CONV : 1);
+      mbar_init(&sh->v_full[i], CACHED ? Cfg::CONV : 1);
+      mbar_init(&sh->k_empty[i], NT);
+      mbar_init(&sh->v_empty[i], NT);
       mbar_init(&sh->s_full[i], 1);
       mbar_init(&sh->p_full[i], 4);
       mbar_init(&sh->o_done[i], 1);
     }
+    mbar_init(&sh->v_clean, 1);
     sh->abort_flag = 0;
     fence_barrier_init();
   }
   if (warp == Cfg::WARP_MMA) {
-    tmem_alloc(&sh->tmem_base, 512);
+    tmem_alloc(&sh->tmem_base, Cfg::TMEM);
     tmem_relinquish();
   }
   pdl_wait();
@@ -227,150 +222,155 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
 
   const EncRequest rq = enc_request(a, b);
   const int row0 = tile * (EA_Q * NT);
-  // key blocks that each tile walks: as many as its last row sees
-  int nbt[2] = {0, 0};
+  // keys and key blocks that each tile walks: as many as its last row sees
+  int most[2] = {0, 0}, nbt[2] = {0, 0};
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     const int first = row0 + t * EA_Q;
-    if (first < rq.nq) nbt[t] = (enc_sees(a, rq, min(first + EA_Q, rq.nq) - 1) + EA_K - 1) / EA_K;
+    if (first < rq.nq) most[t] = enc_sees(a, rq, min(first + EA_Q, rq.nq) - 1);
+    nbt[t] = (most[t] + EA_K - 1) / EA_K;
   }
   const int nb = max(nbt[0], nbt[1]);
+  // columns of block j that a tile computes, in sixteens
+  const auto columns = [](int keys, int j) { return (min(EA_K, keys - j * EA_K) + 15) & ~15; };
+  // value rows behind the length meet weights of 0, which an infinity or NaN there would not survive
+  const bool clean = !CACHED && rq.len < a.nk && rq.len % EA_K != 0;
   const float scale_log2 = fabsf(a.scale_log2);  // the sign is the MMA's
   const int ksteps = (a.d + 15) / 16, dp = ksteps * 16;
 
   if (warp == Cfg::WARP_TMA) {
     // ------------------------------------------------------------ loads
-    if (lane == 0 && nb > 0) {
-      const int panels = (a.d + 63) / 64;  // panels of NP that hold features
+    const int panels = (a.d + 63) / 64;  // panels of NP that hold features
+    if (lane == 0) {
       tma_prefetch_desc(&maps.q);
+      if (!CACHED) {
+        tma_prefetch_desc(&maps.k);
+        tma_prefetch_desc(&maps.v);
+      }
+    }
+    if (lane == 0 && nb > 0) {
       mbar_arrive_expect_tx(&sh->q_full, (uint32_t)(NT * panels * EA_PANEL));
       for (int t = 0; t < NT; ++t)
         for (int p = 0; p < panels; ++p)
           tma_load_4d(sQ + t * Cfg::TILE + p * EA_PANEL, &maps.q, &sh->q_full, p * 64, h * maps.q_h, (int)rq.q_row + row0 + t * EA_Q, b * maps.q_b);
-      if (!CACHED) {
-        tma_prefetch_desc(&maps.k);
-        tma_prefetch_desc(&maps.v);
-        for (int j = 0; j < nb; ++j) {
-          const int ks = j % KST, vs = j % VST;
-          mbar_wait_handover(smem_u32(&sh->k_empty[ks]), (((uint32_t)j / KST) & 1u) ^ 1u, abort_flag);
-          mbar_arrive_expect_tx(&sh->k_full[ks], (uint32_t)(panels * EA_PANEL));
-          for (int p = 0; p < panels; ++p)
-            tma_load_4d(sK + ks * Cfg::TILE + p * EA_PANEL, &maps.k, &sh->k_full[ks], p * 64, g * maps.k_h, j * EA_K, b * maps.k_b);
-          mbar_wait_handover(smem_u32(&sh->v_empty[vs]), (((uint32_t)j / VST) & 1u) ^ 1u, abort_flag);
-          mbar_arrive_expect_tx(&sh->v_full[vs], (uint32_t)(panels * EA_PANEL));
-          for (int p = 0; p < panels; ++p)
-            tma_load_4d(sV + vs * Cfg::TILE + p * EA_PANEL, &maps.v, &sh->v_full[vs], p * 64, g * maps.v_h, j * EA_K, b * maps.v_b);
-          if (*abort_flag) break;
-        }
+      for (int j = 0; !CACHED && j < nb; ++j) {
+        const uint32_t ks = (uint32_t)j % KST, vs = (uint32_t)j % VST;
+        mbar_wait_handover(smem_u32(&sh->k_empty[ks]), (((uint32_t)j / KST) & 1u) ^ 1u, abort_flag);
+        mbar_arrive_expect_tx(&sh->k_full[ks], (uint32_t)(panels * EA_PANEL));
+        for (int p = 0; p < panels; ++p)
+          tma_load_4d(sK + ks * Cfg::TILE + p * EA_PANEL, &maps.k, &sh->k_full[ks], p * 64, g * maps.k_h, j * EA_K, b * maps.k_b);
+        mbar_wait_handover(smem_u32(&sh->v_empty[vs]), (((uint32_t)j / VST) & 1u) ^ 1u, abort_flag);
+        mbar_arrive_expect_tx(&sh->v_full[vs], (uint32_t)(panels * EA_PANEL));
+        for (int p = 0; p < panels; ++p)
+          tma_load_4d(sV + vs * Cfg::TILE + p * EA_PANEL, &maps.v, &sh->v_full[vs], p * 64, g * maps.v_h, j * EA_K, b * maps.v_b);
+        if (*abort_flag) break;
       }
     }
     __syncwarp();
-  } else if (warp == Cfg::WARP_MMA) {
+    if (clean && nb > 0) {
+      const uint32_t vs = (uint32_t)(nb - 1) % VST;
+      const int real = rq.len - (nb - 1) * EA_K;
+      mbar_wait_handover(smem_u32(&sh->v_full[vs]), ((uint32_t)(nb - 1) / VST) & 1u, abort_flag);
+      for (int k = lane; k < (EA_K - real) * NP * 8; k += 32) {
+        const int r = real + k / (NP * 8), c = k % (NP * 8);
+        *reinterpret_cast<uint4*>(sV + vs * Cfg::TILE + (c >> 3) * EA_PANEL + r * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+      }
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh->v_clean);
+    }
+    __syncwarp();
+  } else if (warp == Cfg::WARP_MMA || (NT == 2 && warp == Cfg::WARP_MMA + 1)) {
     // ------------------------------------------------------------ products
-    // Scores of block j + 1 and O += P V of block j alternate between the tiles; a tile's softmax runs under the other tile's
-    // products.  The weights' hand-over also says that the scores have been read.
-    const uint32_t idesc_qk = ea_idesc(EA_K, false, BF, a.scale_log2 < 0.f), idesc_pv = ea_idesc(dp, true, P_BF, false);
+    // One warp per tile issues its scores of block j + 1 and its O += P V of block j, so that neither tile's hand-overs wait
+    // behind the other's; a tile's softmax runs under the other tile's products.  The weights' hand-over also says that the
+    // scores have been read.
+    const int t = NT == 2 ? warp - Cfg::WARP_MMA : 0;
+    const uint32_t idesc_pv = ea_idesc(dp, true, P_BF, false);
     constexpr uint32_t HI = smem_desc_hi(1024, 2);
-    const uint32_t q_lo = smem_desc_lo(smem_u32(sQ)), k_lo = smem_desc_lo(smem_u32(sK));
+    const uint32_t q_lo = smem_desc_lo(smem_u32(sQ)) + (uint32_t)(t * Cfg::TILE >> 4), k_lo = smem_desc_lo(smem_u32(sK));
     const uint32_t v_lo = ((smem_u32(sV) & 0x3FFFFu) >> 4) | ((uint32_t)(EA_PANEL >> 4) << 16);
-    auto scores = [&](int t, int j) {
-      const uint32_t a_lo = q_lo + (uint32_t)(t * Cfg::TILE >> 4), b_lo = k_lo + (uint32_t)((j % KST) * Cfg::TILE >> 4);
+    const uint32_t s_full = smem_u32(&sh->s_full[t]), p_full = smem_u32(&sh->p_full[t]), o_done = smem_u32(&sh->o_done[t]);
+    const int keys = t == 0 ? most[0] : most[1], blocks = t == 0 ? nbt[0] : nbt[1];
+    auto scores = [&](int j) {
+      const uint32_t ks = (uint32_t)j % KST, b_lo = k_lo + ks * (uint32_t)(Cfg::TILE >> 4);
+      const uint32_t idesc_qk = ea_idesc(columns(keys, j), false, BF, a.scale_log2 < 0.f);
+      mbar_wait_handover(smem_u32(&sh->k_full[ks]), ((uint32_t)j / KST) & 1u, abort_flag);
+      tc_fence_after();
       if (elect_one()) {
 #pragma unroll
         for (int k = 0; k < NP * 4; ++k) {
           if (k >= ksteps) break;
           const uint32_t off = (uint32_t)(((k >> 2) * EA_PANEL + (k & 3) * 32) >> 4);
-          mma_f16_lohi(tmem_base + t * 128, a_lo + off, HI, b_lo + off, HI, idesc_qk, k > 0 ? 1u : 0u);
+          mma_f16_lohi(tmem_base + t * 128, q_lo + off, HI, b_lo + off, HI, idesc_qk, k > 0 ? 1u : 0u);
         }
-        mma_commit_addr(smem_u32(&sh->s_full[t]));
+        mma_commit_addr(s_full);
+        mma_commit_addr(smem_u32(&sh->k_empty[ks]));
       }
       __syncwarp();
     };
-    if (nb > 0) {
+    if (blocks > 0) {
       mbar_wait_handover(smem_u32(&sh->q_full), 0, abort_flag);
-      mbar_wait_handover(smem_u32(&sh->k_full[0]), 0, abort_flag);
-      tc_fence_after();
-      for (int t = 0; t < NT; ++t)
-        if (nbt[t] > 0) scores(t, 0);
-      if (elect_one()) mma_commit_addr(smem_u32(&sh->k_empty[0]));
-      __syncwarp();
+      scores(0);
     }
-    for (int j = 0; j < nb; ++j) {
-      const int vs = j % VST;
-      bool have_k = false, have_v = false;
-      for (int t = 0; t < NT; ++t) {
-        if (j >= nbt[t]) continue;
-        auto next_scores = [&]() {
-          if (j + 1 >= nbt[t]) return;
-          if (!have_k) {
-            mbar_wait_handover(smem_u32(&sh->k_full[(j + 1) % KST]), (((uint32_t)j + 1) / KST) & 1u, abort_flag);
-            tc_fence_after();
-            have_k = true;
-          }
-          scores(t, j + 1);
-        };
-        mbar_wait_handover(smem_u32(&sh->p_full[t]), (uint32_t)j & 1u, abort_flag);
-        tc_fence_after();
-        if (Cfg::OWN_P) next_scores();
-        if (!have_v) {
-          mbar_wait_handover(smem_u32(&sh->v_full[vs]), ((uint32_t)j / VST) & 1u, abort_flag);
-          have_v = true;
-          // value rows behind the length meet weights of 0, which an infinity or NaN there would not survive
-          const int real = rq.len - j * EA_K;
-          if (!CACHED && real < EA_K && rq.len < a.nk) {
-            for (int i = lane; i < (EA_K - real) * NP * 8; i += 32) {
-              const int r = real + i / (NP * 8), c = i % (NP * 8);
-              *reinterpret_cast<uint4*>(sV + vs * Cfg::TILE + (c >> 3) * EA_PANEL + r * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-          }
-          tc_fence_after();
-        }
-        const uint32_t a_tmem = tmem_base + Cfg::TMEM_P + t * Cfg::P_STRIDE, d_tmem = tmem_base + Cfg::TMEM_O + t * Cfg::O_STRIDE;
-        const uint32_t b_lo = v_lo + (uint32_t)(vs * Cfg::TILE >> 4);
-        if (elect_one()) {
-#pragma unroll
-          for (int k = 0; k < EA_K / 16; ++k)
-            mma_f16_ts(d_tmem, a_tmem + k * 8, b_lo + (uint32_t)(k * 2048 >> 4), HI, idesc_pv, (j > 0 || k > 0) ? 1u : 0u);
-          mma_commit_addr(smem_u32(&sh->o_done[t]));
-        }
-        __syncwarp();
-        if (!Cfg::OWN_P) next_scores();
-      }
+    for (int j = 0; j < blocks; ++j) {
+      const uint32_t vs = (uint32_t)j % VST;
+      mbar_wait_handover(p_full, (uint32_t)j & 1u, abort_flag);
+      tc_fence_after();
+      if (Cfg::OWN_P && j + 1 < blocks) scores(j + 1);
+      mbar_wait_handover(smem_u32(&sh->v_full[vs]), ((uint32_t)j / VST) & 1u, abort_flag);
+      if (clean && j == nb - 1) mbar_wait_handover(smem_u32(&sh->v_clean), 0, abort_flag);
+      tc_fence_after();
+      const uint32_t a_tmem = tmem_base + Cfg::TMEM_P + t * Cfg::P_STRIDE, d_tmem = tmem_base + Cfg::TMEM_O + t * Cfg::O_STRIDE;
+      const uint32_t b_lo = v_lo + vs * (uint32_t)(Cfg::TILE >> 4);
+      const int n = columns(keys, j) / 16;
       if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < EA_K / 16; ++k) {
+          if (k >= n) break;
+          mma_f16_ts(d_tmem, a_tmem + k * 8, b_lo + (uint32_t)(k * 2048 >> 4), HI, idesc_pv, (j > 0 || k > 0) ? 1u : 0u);
+        }
+        mma_commit_addr(o_done);
         mma_commit_addr(smem_u32(&sh->v_empty[vs]));
-        if (j + 1 < nb) mma_commit_addr(smem_u32(&sh->k_empty[(j + 1) % KST]));
       }
       __syncwarp();
+      if (!Cfg::OWN_P && j + 1 < blocks) scores(j + 1);
       if ((j & 7) == 7 && *abort_flag) break;
+    }
+    // blocks that only the other tile walks
+    for (int j = blocks; NT == 2 && j < nb && !*abort_flag; ++j) {
+      const uint32_t ks = (uint32_t)j % KST, vs = (uint32_t)j % VST;
+      mbar_wait_handover(smem_u32(&sh->k_full[ks]), ((uint32_t)j / KST) & 1u, abort_flag);
+      if (lane == 0) mbar_arrive(&sh->k_empty[ks]);
+      mbar_wait_handover(smem_u32(&sh->v_full[vs]), ((uint32_t)j / VST) & 1u, abort_flag);
+      if (lane == 0) mbar_arrive(&sh->v_empty[vs]);
     }
     __syncwarp();
   } else if (CACHED && warp >= Cfg::CONV_WARP0) {
     // ------------------------------------------------------------ codes to 16 bits
-    // Four warps bring in keys, four values: sixteen codes a load, the next block's in registers while this one's stage is
-    // still in use.
-    const bool values = warp >= Cfg::CONV_WARP0 + 4;
-    const int tid = (warp - Cfg::CONV_WARP0 - (values ? 4 : 0)) * 32 + lane;
-    const int row_bytes = kv_row_bytes(a.d), units = row_bytes / 16, total = EA_K * units;
-    constexpr int MAX_UNITS = NP * 4;
+    // Half of these warps bring in keys, half values: sixteen codes a load, the next block's first loads in registers while
+    // this one's stage is still in use.
+    const bool values = warp >= Cfg::CONV_WARP0 + Cfg::CONV;
+    constexpr int N = Cfg::CONV * 32;
+    const int tid = (warp - Cfg::CONV_WARP0) % Cfg::CONV * 32 + lane;
+    const int row_bytes = kv_row_bytes(a.d), units = row_bytes / 16;
+    constexpr int BATCH = NP * 512 / N < 8 ? NP * 512 / N : 8, BATCHES = (NP * 512 / N + BATCH - 1) / BATCH;
     const int8_t* codes = values ? a.v_codes : a.k_codes;
     const int st_n = values ? VST : KST;
-    uint4 x[MAX_UNITS];
-    auto load = [&](int j) {
+    uint4 x[BATCH];
+    auto load = [&](int j, int batch) {
 #pragma unroll
-      for (int i = 0; i < MAX_UNITS; ++i) {
-        const int u = tid + i * 128;
-        x[i] = make_uint4(0, 0, 0, 0);
-        if (u >= total) continue;
+      for (int i = 0; i < BATCH; ++i) {
+        const int u = tid + (batch * BATCH + i) * N;
         const int r = u / units, c = u - r * units, token = j * EA_K + r;
-        if (token >= rq.len) continue;
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (r >= EA_K || token >= rq.len) continue;
         const int p = ea_page_of(a, b, token);
         if (p >= 0)
           x[i] = __ldg(reinterpret_cast<const uint4*>(codes + ((((int64_t)p * a.Hkv + g) << a.page_log2) + (token & (a.page - 1))) * row_bytes) + c);
       }
     };
-    if (nb > 0) load(0);
+    if (nb > 0) load(0, 0);
     for (int j = 0; j < nb; ++j) {
       const int st = j % st_n;
       unsigned char* stage = (values ? sV : sK) + st * Cfg::TILE;
@@ -385,87 +385,114 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
       mbar_wait_handover(smem_u32(empty), (((uint32_t)j / st_n) & 1u) ^ 1u, abort_flag);
       if (!values && tid < 8) sh->page[j & 3][tid] = pg;
 #pragma unroll
-      for (int i = 0; i < MAX_UNITS; ++i) {
-        const int u = tid + i * 128;
-        if (u >= total) continue;
-        const int r = u / units, c = u - r * units;
-        uint32_t y[8];
-        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      for (int batch = 0; batch < BATCHES; ++batch) {
+        if (batch > 0) load(j, batch);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (BF && !values) codes_to_16<true>(w[k], y[2 * k], y[2 * k + 1]);
-          else codes_to_16<false>(w[k], y[2 * k], y[2 * k + 1]);
+        for (int i = 0; i < BATCH; ++i) {
+          const int u = tid + (batch * BATCH + i) * N;
+          const int r = u / units, c = u - r * units;
+          if (r >= EA_K) continue;
+          uint32_t y[8];
+          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (BF && !values) codes_to_16<true>(w[k], y[2 * k], y[2 * k + 1]);
+            else codes_to_16<false>(w[k], y[2 * k], y[2 * k + 1]);
+          }
+          unsigned char* row = stage + (c >> 2) * EA_PANEL + r * 128;
+          const int c0 = (c & 3) * 2, sw = r & 7;
+          *reinterpret_cast<uint4*>(row + ((c0 ^ sw) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+          *reinterpret_cast<uint4*>(row + (((c0 + 1) ^ sw) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
         }
-        unsigned char* row = stage + (c >> 2) * EA_PANEL + r * 128;
-        const int c0 = (c & 3) * 2, sw = r & 7;
-        *reinterpret_cast<uint4*>(row + ((c0 ^ sw) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-        *reinterpret_cast<uint4*>(row + (((c0 + 1) ^ sw) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
       }
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(full);
-      if (j + 1 < nb) load(j + 1);
+      if (j + 1 < nb) load(j + 1, 0);
       if (*abort_flag) break;
     }
     __syncwarp();
   } else if (warp < Cfg::SOFTMAX_WARPS) {
     // ------------------------------------------------------------ softmax
-    // One thread has one row of a tile.
-    const int t = warp >> 2, row = (warp & 3) * 32 + lane, i = row0 + t * EA_Q + row;
+    // One thread has one row of a tile.  Its weights are powers of two relative to a reference that need not be the row's maximum:
+    // a later block starts with the reference it finds and looks for a larger maximum on the way; only when that is more than
+    // 2^8 above is the block done again.  Where the weights lie over the scores the maximum has to come first.
+    const int t = warp >> 2, row = (warp & 3) * 32 + lane;
     const uint32_t t_lane = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
     const uint32_t t_s = t_lane + t * 128, t_p = t_lane + Cfg::TMEM_P + t * Cfg::P_STRIDE, t_o = t_lane + Cfg::TMEM_O + t * Cfg::O_STRIDE;
-    const int sees = i < rq.nq ? enc_sees(a, rq, i) : 0;
-    float m = -INFINITY;   // the reference: within 2^8 below the largest exponent so far
+    const uint32_t o_done = smem_u32(&sh->o_done[t]);
+    const int i = row0 + t * EA_Q + row;
+    const int keys = t == 0 ? most[0] : most[1], blocks = t == 0 ? nbt[0] : nbt[1];
+    const int sees = i < rq.nq ? enc_sees(a, rq, i) : keys;  // rows that are not there are not written
+    float m = -INFINITY;   // the reference
     float z = 0.f;
-    const int blocks = nbt[t];
     for (int j = 0; j < blocks; ++j) {
       mbar_wait_handover(smem_u32(&sh->s_full[t]), (uint32_t)j & 1u, abort_flag);
       __syncwarp();
       tc_fence_after();
-      const int valid = sees - j * EA_K;
+      const int n = columns(keys, j), valid = sees - j * EA_K;  // columns below `valid` are keys that the row sees
       const EaPage* pages = sh->page[j & 3];
-      auto hide = [&](uint32_t (&r)[32], int c) {
-        if (valid < c * 32 + 32) {
+      auto hide = [&](int c, uint32_t (&r)[32]) {
+        pin32(r);
+        if (valid < c + 32) {
 #pragma unroll
           for (int k = 0; k < 32; ++k)
-            if (c * 32 + k >= valid) r[k] = 0xFF800000u;
+            if (c + k >= valid) r[k] = 0xFF800000u;
         }
       };
-      float top = -INFINITY;
-      uint32_t r[2][32];
-      tmem_ld32(t_s, r[0]);
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t(&x)[32] = r[c & 1];
-        tmem_ld_wait32(x);
-        if (c < 3) tmem_ld32(t_s + (c + 1) * 32, r[(c + 1) & 1]);
-        hide(x, c);
+      // the largest exponent of 32 columns that begin at c
+      auto most_of = [&](int c, const uint32_t (&r)[32], float top) {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           float m0 = -INFINITY, m1 = -INFINITY;
 #pragma unroll
           for (int k = half * 16; k < half * 16 + 16; k += 4) {
-            m0 = max3(m0, __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
-            m1 = max3(m1, __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+            m0 = max3(m0, __uint_as_float(r[k]), __uint_as_float(r[k + 1]));
+            m1 = max3(m1, __uint_as_float(r[k + 2]), __uint_as_float(r[k + 3]));
           }
-          if (CACHED) top = fmaxf(top, fmaf(fmaxf(m0, m1), pages[c * 2 + half].k, pages[c * 2 + half].lv));
-          else top = max3(top, m0, m1);
+          const float f = CACHED ? pages[c / 16 + half].k : scale_log2, off = CACHED ? pages[c / 16 + half].lv : 0.f;
+          top = fmaxf(top, fmaf(fmaxf(m0, m1), f, off));
         }
-      }
-      tmem_ld32(t_s, r[0]);
-      if (!CACHED) top *= scale_log2;
-      const bool move = top > (j == 0 ? -INFINITY : m + EA_LAZY);
-      if (j == 0) {
-        m = top;
-      } else if (__any_sync(0xFFFFFFFFu, move)) {
+        return top;
+      };
+      // their weights in pairs, added to z2
+      auto weigh = [&](int c, const uint32_t (&r)[32], float base, unsigned long long& z2, uint32_t (&pk)[16]) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          float f = scale_log2, off = -base, iv = 1.f;
+          if (CACHED) {
+            const EaPage pg = pages[c / 16 + half];
+            f = pg.k;
+            off = pg.lv - base;
+            iv = pg.iv;
+          }
+          const unsigned long long f2 = pack_f32x2(f, f), off2 = pack_f32x2(off, off);
+          unsigned long long zc = 0ull;
+#pragma unroll
+          for (int k = 0; k < 16; k += 2) {
+            const unsigned long long x2 = fma_f32x2(pack_f32x2(__uint_as_float(r[half * 16 + k]), __uint_as_float(r[half * 16 + k + 1])), f2, off2);
+            float x0, x1;
+            unpack_f32x2(x2, x0, x1);
+            const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
+            zc = add_f32x2(zc, pack_f32x2(e0, e1));
+            pk[half * 8 + k / 2] = pack16<P_BF>(e0, e1);
+          }
+          z2 = CACHED ? fma_f32x2(zc, pack_f32x2(iv, iv), z2) : add_f32x2(zc, z2);
+        }
+      };
+      auto after_product = [&]() {  // of the block before: its weights have been read, the accumulator is complete
+        mbar_wait_handover(o_done, (uint32_t)(j - 1) & 1u, abort_flag);
+        __syncwarp();
+        tc_fence_after();
+      };
+      auto follow = [&](float top) {
         const float m1 = fmaxf(m, top);
         const float fall = m1 == -INFINITY ? 1.f : ex2_approx(m - m1);  // m = -inf: 0
         m = m1;
         z *= fall;
-        tmem_ld_wait();
-        mbar_wait_handover(smem_u32(&sh->o_done[t]), (uint32_t)(j - 1) & 1u, abort_flag);
-        __syncwarp();
-        tc_fence_after();
+        tmem_st_wait();
+        after_product();
+#pragma unroll 1
         for (int c = 0; c < dp; c += 16) {
           uint32_t o[16];
           tmem_ld16(t_o + c, o);
@@ -474,43 +501,66 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
           for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * fall);
           tmem_st16(t_o + c, o);
         }
-      }
-      const float base = m == -INFINITY ? 0.f : m;
-      if (Cfg::OWN_P && j > 0) {  // the product before has read its weights
-        mbar_wait_handover(smem_u32(&sh->o_done[t]), (uint32_t)(j - 1) & 1u, abort_flag);
-        __syncwarp();
-        tc_fence_after();
-      }
+      };
       unsigned long long z2 = 0ull;
+      // Whole blocks run without a branch; the loops below serve the others.
+      const bool whole = __all_sync(0xFFFFFFFFu, valid >= EA_K);
+      bool done = false;
+      if (whole && (j > 0 || !Cfg::OWN_P)) {
+        uint32_t x[2][32];
+        if (!Cfg::OWN_P) {
+          float top = -INFINITY;
+          tmem_ld32(t_s, x[0]);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        uint32_t(&x)[32] = r[c & 1];
-        tmem_ld_wait32(x);
-        if (c < 3) tmem_ld32(t_s + (c + 1) * 32, r[(c + 1) & 1]);
-        hide(x, c);
-        uint32_t pk[16];
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          float f = scale_log2, off = -base, iv = 1.f;
-          if (CACHED) {
-            const EaPage pg = pages[c * 2 + half];
-            f = pg.k;
-            off = pg.lv - base;
-            iv = pg.iv;
+          for (int c = 0; c < 4; ++c) {
+            tmem_ld_wait();
+            pin32(x[c & 1]);
+            if (c < 3) tmem_ld32(t_s + (c + 1) * 32, x[(c + 1) & 1]);
+            top = most_of(c * 32, x[c & 1], top);
           }
-          const unsigned long long f2 = pack_f32x2(f, f), off2 = pack_f32x2(off, off), iv2 = pack_f32x2(iv, iv);
-          unsigned long long zc = 0ull;
-#pragma unroll
-          for (int k = half * 16; k < half * 16 + 16; k += 2) {
-            float x0, x1;
-            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2, off2), x0, x1);
-            const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
-            zc = add_f32x2(zc, pack_f32x2(e0, e1));
-            pk[k >> 1] = pack16<P_BF>(e0, e1);
-          }
-          z2 = CACHED ? fma_f32x2(zc, iv2, z2) : add_f32x2(zc, z2);
+          if (j == 0) m = top;
+          else if (__any_sync(0xFFFFFFFFu, top > m + EA_LAZY)) follow(top);
         }
-        tmem_st16(t_p + c * 16, pk);
+        const float base = m == -INFINITY ? 0.f : m;
+        float top = -INFINITY;
+        tmem_ld32(t_s, x[0]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          tmem_ld_wait();
+          pin32(x[c & 1]);
+          if (c < 3) tmem_ld32(t_s + (c + 1) * 32, x[(c + 1) & 1]);
+          if (Cfg::OWN_P) top = most_of(c * 32, x[c & 1], top);
+          uint32_t pk[16];
+          weigh(c * 32, x[c & 1], base, z2, pk);
+          if (Cfg::OWN_P && c == 0 && j > 0) after_product();
+          tmem_st16(t_p + c * 16, pk);
+        }
+        done = !Cfg::OWN_P || !__any_sync(0xFFFFFFFFu, top > m + EA_LAZY);
+      }
+      if (!done) {
+        float top = -INFINITY;
+#pragma unroll 1
+        for (int c = 0; c < n; c += 32) {
+          uint32_t r[32];
+          tmem_ld32(t_s + c, r);
+          tmem_ld_wait();
+          hide(c, r);
+          top = most_of(c, r, top);
+        }
+        if (j == 0) m = top;
+        else if (__any_sync(0xFFFFFFFFu, top > m + EA_LAZY)) follow(top);
+        const float base = m == -INFINITY ? 0.f : m;
+        if (Cfg::OWN_P && j > 0) after_product();
+        z2 = 0ull;
+#pragma unroll 1
+        for (int c = 0; c < n; c += 32) {
+          uint32_t r[32], pk[16];
+          tmem_ld32(t_s + c, r);
+          tmem_ld_wait();
+          hide(c, r);
+          weigh(c, r, base, z2, pk);
+          tmem_st16(t_p + c / 2, pk);
+        }
       }
       tmem_st_wait();
       tc_fence_before();
@@ -519,7 +569,7 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
       z += __uint_as_float((uint32_t)z2) + __uint_as_float((uint32_t)(z2 >> 32));
     }
     if (blocks > 0) {
-      mbar_wait_handover(smem_u32(&sh->o_done[t]), (uint32_t)(blocks - 1) & 1u, abort_flag);
+      mbar_wait_handover(o_done, (uint32_t)(blocks - 1) & 1u, abort_flag);
       __syncwarp();
       tc_fence_after();
     }
@@ -551,7 +601,7 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
   if (warp == Cfg::WARP_MMA) {
     __syncwarp();
     tc_fence_after();
-    tmem_dealloc(tmem_base, 512);
+    tmem_dealloc(tmem_base, Cfg::TMEM);
   }
 }
 
