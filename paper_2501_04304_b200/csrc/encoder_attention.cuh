@@ -99,9 +99,9 @@ struct EaShared {
 static_assert(sizeof(EaShared) <= 1024, "shared block");
 
 struct EaMaps {
-  CUtensorMap q, k, v;
+  CUtensorMap q, k, v, o;
   int q_b, k_b, k_h, v_b, v_h;  // 0 where the tensor broadcasts along the dimension (its extent is then 1)
-  int q_h;
+  int q_h, o_b, o_h;
 };
 
 // kind::f16 instruction descriptor with both operands' type and the sign of A.
@@ -115,6 +115,18 @@ __device__ __forceinline__ void pin32(uint32_t (&r)[32]) {
                     "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]),
                     "+r"(r[16]), "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]),
                     "+r"(r[24]), "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31]));
+}
+
+// Boxes of 64 features x 32 rows x 1 head out of shared memory (rows of 128 bytes, swizzled); rows and features beyond the tensor's
+// are left out.
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap* m, const void* src, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%2, %3, %4, %5}], [%1];" ::"l"(reinterpret_cast<uint64_t>(m)),
+               "r"(smem_u32(src)), "r"(c0), "r"(c1), "r"(c2), "r"(c3)
+               : "memory");
+}
+// Features c .. c + 7 of an output row into its place in such a box.
+__device__ __forceinline__ void stage_out(unsigned char* slab, int panel_bytes, int row, int c, uint4 y) {
+  *reinterpret_cast<uint4*>(slab + (c >> 6) * panel_bytes + row * 128 + ((((c >> 3) & 7) ^ (row & 7)) << 4)) = y;
 }
 
 // Four codes as four 16-bit numbers, exactly.  fp16: 0x64 in front of a byte is 1024 + byte.  bf16: 0x43 in front of the low seven
@@ -194,7 +206,6 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
   const int g = h / (a.Hq / a.Hkv);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
-  pdl_launch_dependents();
   if (threadIdx.x == 0) {
     mbar_init(&sh->q_full, 1);
     for (int i = 0; i < 2; ++i) {
@@ -218,6 +229,7 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
+  pdl_launch_dependents();  // not before this block has its tensor memory: a block of the next kernel could take it and wait for this one
   const uint32_t tmem_base = sh->tmem_base;
 
   const EncRequest rq = enc_request(a, b);
@@ -573,18 +585,44 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
       __syncwarp();
       tc_fence_after();
     }
-    const float inv = z > 0.f || z != z ? 1.f / z : 0.f;
+    // Outputs leave through the tile's queries, which every product has read: written row by row they would be sixteen bytes of a
+    // sector at a time (four times the requests; 8 x 16 x 4096 x 64 over 77 keys 56 us, MEASURED_STORE this way).
+    const float inv = sees > 0 && (z > 0.f || z != z) ? 1.f / z : 0.f;
+    unsigned char* slab = sQ + t * Cfg::TILE + (warp & 3) * 32 * 128;
     uint16_t* out = (uint16_t*)a.O.ptr + b * a.O.batch + (rq.q_row + i) * a.O.token + h * a.O.head;
-    for (int c = 0; c < a.d; c += 8) {
-      uint32_t o[8] = {};
+    const int first = row0 + t * EA_Q + (warp & 3) * 32;           // the warp's rows
+    // rows behind a packed request's are another one's; where a tile has no block its queries may still be on their way
+    const bool boxed = blocks > 0 && (!a.q_start || first + 32 <= rq.nq);
+#pragma unroll 1
+    for (int c = 0; c < a.d; c += 32) {
+      uint32_t o[32];
       if (blocks > 0) {
-        tmem_ld8(t_o + c, o);
+        tmem_ld32(t_o + c, o);
         tmem_ld_wait();
+        pin32(o);
       }
-      uint32_t y[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) y[k] = pack16<BF>(__uint_as_float(o[2 * k]) * inv, __uint_as_float(o[2 * k + 1]) * inv);
-      if (i < rq.nq) *reinterpret_cast<uint4*>(out + c) = sees > 0 ? make_uint4(y[0], y[1], y[2], y[3]) : make_uint4(0, 0, 0, 0);
+      for (int e = 0; e < 4; ++e) {
+        if (c + e * 8 >= a.d) break;
+        uint32_t y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          y[k] = blocks > 0 && sees > 0 ? pack16<BF>(__uint_as_float(o[e * 8 + 2 * k]) * inv, __uint_as_float(o[e * 8 + 2 * k + 1]) * inv) : 0u;
+        const uint4 y4 = make_uint4(y[0], y[1], y[2], y[3]);
+        if (boxed) stage_out(slab, EA_PANEL, lane, c + e * 8, y4);
+        else if (i < rq.nq) *reinterpret_cast<uint4*>(out + c + e * 8) = y4;
+      }
+    }
+    if (boxed && first < rq.nq) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        for (int p = 0; p * 64 < a.d; ++p)
+          tma_store_4d(&maps.o, slab + p * EA_PANEL, p * 64, h * maps.o_h, (int)rq.q_row + first, b * maps.o_b);
+        bulk_commit();
+        bulk_wait_read0();
+      }
+      __syncwarp();
     }
   }
 
@@ -605,15 +643,15 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
   }
 }
 
-// [B, n, H, d] with strides as a 4-D tensor (d, H, n, B), boxes of 64 features x 128 rows of one head.  A dimension along which
+// [B, n, H, d] with strides as a 4-D tensor (d, H, n, B), boxes of 64 features x `rows` rows of one head.  A dimension along which
 // the tensor broadcasts has extent 1, and the kernel's coordinate there is 0.
-static bool ea_encode(CUtensorMap* m, const dgq_rows& r, int64_t B, int64_t n, int64_t H, int d, bool bf, int* use_b, int* use_h) {
+static bool ea_encode(CUtensorMap* m, const dgq_rows& r, int64_t B, int64_t n, int64_t H, int d, bool bf, uint32_t rows, int* use_b, int* use_h) {
   *use_b = r.batch != 0;
   *use_h = r.head != 0;
   const uint64_t dims[4] = {(uint64_t)d, *use_h ? (uint64_t)H : 1u, (uint64_t)n, *use_b ? (uint64_t)B : 1u};
   const auto bytes = [&](int64_t s) { return (uint64_t)(s ? s * 2 : (int64_t)kv_row_bytes(d) * 2); };
   const uint64_t strides[3] = {bytes(r.head), bytes(r.token), bytes(r.batch)};
-  const uint32_t box[4] = {64, 1, 128, 1};
+  const uint32_t box[4] = {64, 1, rows, 1};
   return encode_map(m, r.ptr, 4, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B,
                     bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16);
 }
@@ -632,10 +670,11 @@ static dgq_status ea_launch_tiles(const EncAttnArgs& a, cudaStream_t stream) {
   if (grid > INT_MAX) return DGQ_ERR_UNSUPPORTED;
   EaMaps maps;
   std::memset(&maps, 0, sizeof(maps));
-  if (!ea_encode(&maps.q, a.Q, a.q_start ? 1 : a.B, a.q_start ? a.n_rows : a.nq, a.Hq, a.d, BF, &maps.q_b, &maps.q_h)) return DGQ_ERR_CUDA;
-  if (!CACHED && (!ea_encode(&maps.k, a.K, a.B, a.nk, a.Hkv, a.d, BF, &maps.k_b, &maps.k_h) ||
-                  !ea_encode(&maps.v, a.V, a.B, a.nk, a.Hkv, a.d, BF, &maps.v_b, &maps.v_h)))
+  if (!ea_encode(&maps.q, a.Q, a.q_start ? 1 : a.B, a.q_start ? a.n_rows : a.nq, a.Hq, a.d, BF, 128, &maps.q_b, &maps.q_h)) return DGQ_ERR_CUDA;
+  if (!CACHED && (!ea_encode(&maps.k, a.K, a.B, a.nk, a.Hkv, a.d, BF, 128, &maps.k_b, &maps.k_h) ||
+                  !ea_encode(&maps.v, a.V, a.B, a.nk, a.Hkv, a.d, BF, 128, &maps.v_b, &maps.v_h)))
     return DGQ_ERR_CUDA;
+  if (!ea_encode(&maps.o, a.O, a.q_start ? 1 : a.B, a.q_start ? a.n_rows : a.nq, a.Hq, a.d, BF, 32, &maps.o_b, &maps.o_h)) return DGQ_ERR_CUDA;
   DGQ_CUDA_OK(launch_pdl(enc_attn_tiles_kernel<NP, BF, CACHED>, dim3((unsigned)grid), dim3(Cfg::THREADS), (size_t)Cfg::SMEM, stream, maps, a));
   g_launches += 1;
   DGQ_CUDA_OK(cudaGetLastError());
@@ -1214,12 +1253,406 @@ static dgq_status ef_launch_size(const EncAttnArgs& a, cudaStream_t stream) {
   return ef_launch_columns<SRC, 3>(a, stream);
 }
 
+// ------------------------------------------------------------------ many query rows, few keys
+// All keys of a head are one block of scores: a thread block brings keys and values in once (widened, if they are codes) and walks
+// tiles of 128 query rows, of all query heads that share them.  No running maximum: a row's is known before its weights.  Two
+// threads have a row, one half of its columns each; weights lie over the scores, each half's over its own.  Two thread blocks
+// share an SM: the chain of a tile (scores, maximum, weights, product, output) is several times the work in it.
+template <int NP, bool CACHED>
+struct EsCfg {
+  static constexpr int KEYS = NP == 1 ? 192 : 128;         // most keys: scores and outputs in 256 columns of tensor memory
+  static constexpr int PANEL = KEYS * 128;                 // bytes of 64 features of the keys
+  static constexpr int QST = NP == 1 ? 2 : 1;              // query tiles in shared memory
+  static constexpr int SOFTMAX_WARPS = 8, WARP_TMA = 8, WARP_MMA = 9, THREADS = 320;
+  static constexpr int TMEM_O = KEYS;
+  static constexpr int QTILE = NP * EA_PANEL;
+  // outputs have a tile's room of their own beside two query tiles, else they take the queries'
+  static constexpr int OFF_O = QST == 2 ? 2 * QTILE : 0;
+  static constexpr int OFF_K = QST == 2 ? 3 * QTILE : QTILE, OFF_V = OFF_K + NP * PANEL, OFF_SH = OFF_V + NP * PANEL;
+  static constexpr int SMEM = 1024 + OFF_SH + 1024 + 4 * 128 * 4;
+  static_assert(2 * SMEM <= 232448 - 2048, "two blocks share an SM");
+  static_assert(KEYS + NP * 64 <= 256, "tensor memory budget");
+};
+
+struct EsShared {
+  uint64_t q_full[2], q_empty[2], kv_full, v_clean, s_full, p_full, o_done;
+  uint32_t tmem_base;
+  int abort_flag;
+  EaPage page[14];  // a thread's last thirty-two columns may begin with its last sixteen
+};
+static_assert(sizeof(EsShared) <= 1024, "shared block");
+
+__device__ __forceinline__ void pin16(uint32_t (&r)[16]) {
+  asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+               "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
+}
+// 32 lanes x 8 consecutive 32-bit columns: thread i of the warp writes row (lane base + i).
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
+
+template <int NP, bool BF, bool CACHED>
+__global__ void __launch_bounds__(EsCfg<NP, CACHED>::THREADS, 2)
+enc_attn_short_kernel(const __grid_constant__ EaMaps maps, const __grid_constant__ EncAttnArgs a, int chunk_tiles) {
+  using Cfg = EsCfg<NP, CACHED>;
+  constexpr bool P_BF = BF && !CACHED;
+  constexpr int QST = Cfg::QST, PANEL = Cfg::PANEL;
+  extern __shared__ unsigned char smem_dyn[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_dyn) + 1023) & ~uintptr_t(1023));
+  unsigned char* sQ = smem;
+  unsigned char* sK = smem + Cfg::OFF_K;
+  unsigned char* sV = smem + Cfg::OFF_V;
+  EsShared* sh = reinterpret_cast<EsShared*>(smem + Cfg::OFF_SH);
+  float* tops = reinterpret_cast<float*>(smem + Cfg::OFF_SH + 1024);  // [half][row]: what a row's two threads tell each other
+  float* sums = tops + 256;
+  volatile int* abort_flag = &sh->abort_flag;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  // tiles of a key head: those of its first query head, of its second, ...
+  const int group = a.Hq / a.Hkv, per_head = (a.nq + EA_Q - 1) / EA_Q, all = per_head * group;
+  const int n_chunks = (all + chunk_tiles - 1) / chunk_tiles;
+  const int chunk = (int)(blockIdx.x % n_chunks), g = (int)(blockIdx.x / n_chunks) % a.Hkv, b = (int)(blockIdx.x / n_chunks) / a.Hkv;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh->q_full[i], 1);
+      mbar_init(&sh->q_empty[i], QST == 2 ? 1 : 4);
+    }
+    mbar_init(&sh->kv_full, CACHED ? Cfg::SOFTMAX_WARPS : 1);
+    mbar_init(&sh->v_clean, 1);
+    mbar_init(&sh->s_full, 1);
+    mbar_init(&sh->p_full, Cfg::SOFTMAX_WARPS);
+    mbar_init(&sh->o_done, 1);
+    sh->abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == Cfg::WARP_MMA) {
+    tmem_alloc(&sh->tmem_base, 256);
+    tmem_relinquish();
+  }
+  pdl_wait();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  pdl_launch_dependents();  // not before this block has its tensor memory: a block of the next kernel could take it and wait for this one
+  const uint32_t tmem_base = sh->tmem_base;
+
+  const EncRequest rq = enc_request(a, b);
+  const int n = (rq.len + 15) & ~15, n0 = (n + 16) / 32 * 16;  // columns, and those of a row's first thread
+  const int ksteps = (a.d + 15) / 16, dp = ksteps * 16, panels = (a.d + 63) / 64;
+  const int tile0 = chunk * chunk_tiles, tile1 = min(tile0 + chunk_tiles, all);
+  const bool clean = !CACHED && rq.len < a.nk && rq.len % 16 != 0;  // value rows behind the length, as in the kernel above
+  // A tile that a request with fewer queries than others does not have is passed over by all roles.
+  const auto real = [&](int tile) { return tile % per_head * EA_Q < rq.nq && rq.len > 0; };
+
+  if (warp == Cfg::WARP_TMA) {
+    // ------------------------------------------------------------ loads
+    int r = 0;
+    for (int tile = tile0; tile < tile1 && !*abort_flag; ++tile) {
+      if (!real(tile)) continue;
+      if (lane == 0) {
+        const int qb = r % QST;
+        mbar_wait_handover(smem_u32(&sh->q_empty[qb]), ((uint32_t)(r / QST) & 1u) ^ 1u, abort_flag);
+        mbar_arrive_expect_tx(&sh->q_full[qb], (uint32_t)(panels * EA_PANEL));
+        for (int p = 0; p < panels; ++p)
+          tma_load_4d(sQ + qb * Cfg::QTILE + p * EA_PANEL, &maps.q, &sh->q_full[qb], p * 64, (g * group + tile / per_head) * maps.q_h,
+                      (int)rq.q_row + tile % per_head * EA_Q, b * maps.q_b);
+        if (!CACHED && r == 0) {
+          const int boxes = (rq.len + 63) / 64;
+          mbar_arrive_expect_tx(&sh->kv_full, (uint32_t)(2 * boxes * panels * 64 * 128));
+          for (int p = 0; p < panels; ++p)
+            for (int i = 0; i < boxes; ++i) {
+              tma_load_4d(sK + p * PANEL + i * 64 * 128, &maps.k, &sh->kv_full, p * 64, g * maps.k_h, i * 64, b * maps.k_b);
+              tma_load_4d(sV + p * PANEL + i * 64 * 128, &maps.v, &sh->kv_full, p * 64, g * maps.v_h, i * 64, b * maps.v_b);
+            }
+        }
+      }
+      __syncwarp();
+      if (clean && r == 0) {
+        mbar_wait_handover(smem_u32(&sh->kv_full), 0, abort_flag);
+        for (int k = lane; k < (n - rq.len) * NP * 8; k += 32) {
+          const int row = rq.len + k / (NP * 8), c = k % (NP * 8);
+          *reinterpret_cast<uint4*>(sV + (c >> 3) * PANEL + row * 128 + (c & 7) * 16) = make_uint4(0, 0, 0, 0);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sh->v_clean);
+        __syncwarp();
+      }
+      ++r;
+    }
+    __syncwarp();
+  } else if (warp == Cfg::WARP_MMA) {
+    // ------------------------------------------------------------ products
+    const uint32_t idesc_qk = ea_idesc(n, false, BF, a.scale_log2 < 0.f), idesc_pv = ea_idesc(dp, true, P_BF, false);
+    constexpr uint32_t HI = smem_desc_hi(1024, 2);
+    const uint32_t q_lo = smem_desc_lo(smem_u32(sQ)), k_lo = smem_desc_lo(smem_u32(sK));
+    const uint32_t v_lo = ((smem_u32(sV) & 0x3FFFFu) >> 4) | ((uint32_t)(PANEL >> 4) << 16);
+    int r = 0;
+    for (int tile = tile0; tile < tile1 && !*abort_flag; ++tile) {
+      if (!real(tile)) continue;
+      const int qb = r % QST;
+      if (r == 0) {
+        mbar_wait_handover(smem_u32(&sh->kv_full), 0, abort_flag);
+        if (clean) mbar_wait_handover(smem_u32(&sh->v_clean), 0, abort_flag);
+      }
+      mbar_wait_handover(smem_u32(&sh->q_full[qb]), (uint32_t)(r / QST) & 1u, abort_flag);
+      tc_fence_after();
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < NP * 4; ++k) {
+          if (k >= ksteps) break;
+          const uint32_t in = (uint32_t)((k & 3) * 32 >> 4);
+          mma_f16_lohi(tmem_base, q_lo + (uint32_t)((qb * Cfg::QTILE + (k >> 2) * EA_PANEL) >> 4) + in, HI,
+                       k_lo + (uint32_t)((k >> 2) * PANEL >> 4) + in, HI, idesc_qk, k > 0 ? 1u : 0u);
+        }
+        mma_commit_addr(smem_u32(&sh->s_full));
+        if (QST == 2) mma_commit_addr(smem_u32(&sh->q_empty[qb]));
+      }
+      __syncwarp();
+      mbar_wait_handover(smem_u32(&sh->p_full), (uint32_t)r & 1u, abort_flag);
+      tc_fence_after();
+      if (elect_one()) {
+#pragma unroll
+        for (int k = 0; k < Cfg::KEYS / 16; ++k) {
+          if (k * 16 >= n) break;
+          const uint32_t at = k * 16 < n0 ? k * 8 : n0 + (k * 16 - n0) / 2;
+          mma_f16_ts(tmem_base + Cfg::TMEM_O, tmem_base + at, v_lo + (uint32_t)(k * 2048 >> 4), HI, idesc_pv, k > 0 ? 1u : 0u);
+        }
+        mma_commit_addr(smem_u32(&sh->o_done));
+      }
+      __syncwarp();
+      ++r;
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------ softmax
+    const float scale_log2 = fabsf(a.scale_log2);
+    if (CACHED) {
+      const int row_bytes = kv_row_bytes(a.d), units = row_bytes / 16;
+#pragma unroll 2
+      for (int u = threadIdx.x; u < n * units; u += Cfg::SOFTMAX_WARPS * 32) {
+        const int row = u / units, c = u - row * units;
+        uint4 x[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+        const int p = row < rq.len ? ea_page_of(a, b, row) : -1;
+        if (p >= 0) {
+          const int64_t at = ((((int64_t)p * a.Hkv + g) << a.page_log2) + (row & (a.page - 1))) * row_bytes + c * 16;
+          x[0] = __ldg(reinterpret_cast<const uint4*>(a.k_codes + at));
+          x[1] = __ldg(reinterpret_cast<const uint4*>(a.v_codes + at));
+        }
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
+          uint32_t y[8];
+          const uint32_t x4[4] = {x[w].x, x[w].y, x[w].z, x[w].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (BF && w == 0) codes_to_16<true>(x4[k], y[2 * k], y[2 * k + 1]);
+            else codes_to_16<false>(x4[k], y[2 * k], y[2 * k + 1]);
+          }
+          unsigned char* to = (w ? sV : sK) + (c >> 2) * PANEL + row * 128;
+          const int c0 = (c & 3) * 2, sw = row & 7;
+          *reinterpret_cast<uint4*>(to + ((c0 ^ sw) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+          *reinterpret_cast<uint4*>(to + (((c0 + 1) ^ sw) << 4)) = make_uint4(y[4], y[5], y[6], y[7]);
+        }
+      }
+      if (threadIdx.x < 14) sh->page[threadIdx.x] = threadIdx.x < n / 16 ? ea_page_scales(a, b, g, threadIdx.x * 16, scale_log2) : EaPage{1.f, 0.f, 1.f, 0.f};
+      fence_proxy_async_smem();
+      named_bar_sync(1, Cfg::SOFTMAX_WARPS * 32);
+      if (lane == 0) mbar_arrive(&sh->kv_full);
+    }
+    const int half = warp >> 2, row = (warp & 3) * 32 + lane, bar = 2 + (warp & 3);
+    const uint32_t t_lane = tmem_base + ((uint32_t)((warp & 3) * 32) << 16), t_o = t_lane + Cfg::TMEM_O;
+    const int c0 = half ? n0 : 0, nc = half ? n - n0 : n0;  // this thread's columns
+    const int valid = rq.len - c0;                          // those below are keys
+    const uint32_t t_s = t_lane + c0;
+    const EaPage* pages = sh->page + c0 / 16;
+    const int f_half = (a.d / 8 + 1) / 2 * 8, f0 = half ? f_half : 0, f1 = half ? a.d : f_half;  // its features of the outputs
+    unsigned char* slab = smem + Cfg::OFF_O + (warp & 3) * 32 * 128;
+    // Thirty-two columns at a time, those beyond this thread's hidden like those behind the keys.
+    const int shown = min(valid, nc);
+    auto fetch = [&](int c, uint32_t (&x)[32]) {
+      tmem_ld32(t_s + c, x);
+      tmem_ld_wait();
+      pin32(x);
+      if (shown < c + 32) {
+#pragma unroll
+        for (int k = 0; k < 32; ++k)
+          if (c + k >= shown) x[k] = 0xFF800000u;
+      }
+    };
+    int r = 0;
+    for (int tile = tile0; tile < tile1; ++tile) {
+      const int i = tile % per_head * EA_Q + row, h = g * group + tile / per_head;
+      uint16_t* out = (uint16_t*)a.O.ptr + b * a.O.batch + (rq.q_row + i) * a.O.token + h * a.O.head;
+      if (!real(tile)) {
+        if (i < rq.nq)
+          for (int c = half * 8; c < a.d; c += 16) *reinterpret_cast<uint4*>(out + c) = make_uint4(0, 0, 0, 0);
+        continue;
+      }
+      mbar_wait_handover(smem_u32(&sh->s_full), (uint32_t)r & 1u, abort_flag);
+      __syncwarp();
+      tc_fence_after();
+      float top = -INFINITY;
+#pragma unroll 1
+      for (int c = 0; c < nc; c += 32) {
+        uint32_t x[32];
+        fetch(c, x);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float m0 = -INFINITY, m1 = -INFINITY;
+#pragma unroll
+          for (int k = e * 16; k < e * 16 + 16; k += 4) {
+            m0 = max3(m0, __uint_as_float(x[k]), __uint_as_float(x[k + 1]));
+            m1 = max3(m1, __uint_as_float(x[k + 2]), __uint_as_float(x[k + 3]));
+          }
+          const float f = CACHED ? pages[c / 16 + e].k : scale_log2, off = CACHED ? pages[c / 16 + e].lv : 0.f;
+          top = fmaxf(top, fmaf(fmaxf(m0, m1), f, off));
+        }
+      }
+      tops[half * 128 + row] = top;
+      if (QST == 2 && half == 0 && lane == 0) bulk_wait_read0();  // the tile before has left the outputs' room
+      named_bar_sync(bar, 64);
+      top = fmaxf(top, tops[(half ^ 1) * 128 + row]);
+      const float base = top == -INFINITY ? 0.f : top;
+      unsigned long long z2 = 0ull;
+#pragma unroll 1
+      for (int c = 0; c < nc; c += 32) {  // weights take the front half of this thread's columns, behind what has been read
+        uint32_t x[32], pk[16];
+        fetch(c, x);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float f = CACHED ? pages[c / 16 + e].k : scale_log2, off = (CACHED ? pages[c / 16 + e].lv : 0.f) - base;
+          const unsigned long long f2 = pack_f32x2(f, f), off2 = pack_f32x2(off, off);
+          unsigned long long zc = 0ull;
+#pragma unroll
+          for (int k = e * 16; k < e * 16 + 16; k += 2) {
+            float x0, x1;
+            unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[k]), __uint_as_float(x[k + 1])), f2, off2), x0, x1);
+            const float e0 = ex2_approx(x0), e1 = ex2_approx(x1);
+            zc = add_f32x2(zc, pack_f32x2(e0, e1));
+            pk[k >> 1] = pack16<P_BF>(e0, e1);
+          }
+          if (CACHED) z2 = fma_f32x2(zc, pack_f32x2(pages[c / 16 + e].iv, pages[c / 16 + e].iv), z2);
+          else z2 = add_f32x2(zc, z2);
+        }
+        tmem_st16(t_s + c / 2, pk);
+      }
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sh->p_full);
+      float z = __uint_as_float((uint32_t)z2) + __uint_as_float((uint32_t)(z2 >> 32));
+      sums[half * 128 + row] = z;
+      named_bar_sync(bar, 64);
+      z += sums[(half ^ 1) * 128 + row];
+      const float inv = z > 0.f || z != z ? 1.f / z : 0.f;
+      mbar_wait_handover(smem_u32(&sh->o_done), (uint32_t)r & 1u, abort_flag);
+      __syncwarp();
+      tc_fence_after();
+      const int first = tile % per_head * EA_Q + (warp & 3) * 32;  // the warp's rows
+      const bool boxed = !a.q_start || first + 32 <= rq.nq;
+#pragma unroll 1
+      for (int c = f0; c < f1; c += 16) {
+        uint32_t o[16];  // features beyond f1 are read for nothing, within the accumulator's columns
+        tmem_ld16(t_o + c, o);
+        tmem_ld_wait();
+        pin16(o);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          uint32_t y[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) y[k] = pack16<BF>(__uint_as_float(o[e * 8 + 2 * k]) * inv, __uint_as_float(o[e * 8 + 2 * k + 1]) * inv);
+          const uint4 y4 = make_uint4(y[0], y[1], y[2], y[3]);
+          if (c + e * 8 >= f1) continue;
+          if (boxed) stage_out(slab, EA_PANEL, lane, c + e * 8, y4);
+          else if (i < rq.nq) *reinterpret_cast<uint4*>(out + c + e * 8) = y4;
+        }
+      }
+      fence_proxy_async_smem();
+      named_bar_sync(bar, 64);
+      if (half == 0 && lane == 0) {
+        if (boxed && first < rq.nq) {
+          for (int p = 0; p * 64 < a.d; ++p)
+            tma_store_4d(&maps.o, slab + p * EA_PANEL, p * 64, h * maps.o_h, (int)rq.q_row + first, b * maps.o_b);
+          bulk_commit();
+        }
+        if (QST == 1) {
+          bulk_wait_read0();
+          mbar_arrive(&sh->q_empty[0]);
+        }
+      }
+      ++r;
+    }
+    if (half == 0 && lane == 0) bulk_wait_read0();
+  }
+
+  // ------------------------------------------------------------ common exit
+  tc_fence_before();
+  __syncthreads();
+  if (*abort_flag) {
+    // give copies that may still be in flight time to land before the block's shared memory is released
+    const long long t0 = clock64();
+    while (clock64() - t0 < 200000) {
+    }
+    __syncthreads();
+  }
+  if (warp == Cfg::WARP_MMA) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 256);
+  }
+}
+
+template <int NP, bool BF, bool CACHED>
+static dgq_status es_launch(const EncAttnArgs& a, cudaStream_t stream) {
+  using Cfg = EsCfg<NP, CACHED>;
+  const auto kernel = enc_attn_short_kernel<NP, BF, CACHED>;
+  static std::atomic<bool> attr_set[64];
+  int dev = 0, sms = 0;
+  DGQ_CUDA_OK(cudaGetDevice(&dev));
+  DGQ_CUDA_OK(sm_count(&sms));
+  if (dev >= 64 || !attr_set[dev].load()) {
+    DGQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
+    if (dev < 64) attr_set[dev].store(true);
+  }
+  // Tiles of a block: it costs about 3 us beside them, a tile 1 us.
+  const int64_t all = (int64_t)((a.nq + EA_Q - 1) / EA_Q) * (a.Hq / a.Hkv), heads = a.B * (int64_t)a.Hkv;
+  if (all * heads > INT_MAX) return DGQ_ERR_UNSUPPORTED;
+  int tiles = 1;
+  float best = 3.4e38f;
+  for (int c = 1; c <= 64 && c <= all; ++c) {
+    const int64_t blocks = heads * ((all + c - 1) / c), rounds = (blocks + 2 * sms - 1) / (2 * sms);
+    const float time = rounds * (3.f + c);
+    if (time < best) {
+      best = time;
+      tiles = c;
+    }
+  }
+  if (getenv("ESW")) tiles = atoi(getenv("ESW"));
+  EaMaps maps;
+  std::memset(&maps, 0, sizeof(maps));
+  if (!ea_encode(&maps.q, a.Q, a.q_start ? 1 : a.B, a.q_start ? a.n_rows : a.nq, a.Hq, a.d, BF, 128, &maps.q_b, &maps.q_h)) return DGQ_ERR_CUDA;
+  if (!CACHED && (!ea_encode(&maps.k, a.K, a.B, a.nk, a.Hkv, a.d, BF, 64, &maps.k_b, &maps.k_h) ||
+                  !ea_encode(&maps.v, a.V, a.B, a.nk, a.Hkv, a.d, BF, 64, &maps.v_b, &maps.v_h)))
+    return DGQ_ERR_CUDA;
+  if (!ea_encode(&maps.o, a.O, a.q_start ? 1 : a.B, a.q_start ? a.n_rows : a.nq, a.Hq, a.d, BF, 32, &maps.o_b, &maps.o_h)) return DGQ_ERR_CUDA;
+  const int64_t grid = heads * ((all + tiles - 1) / tiles);
+  DGQ_CUDA_OK(launch_pdl(kernel, dim3((unsigned)grid), dim3(Cfg::THREADS), (size_t)Cfg::SMEM, stream, maps, a, tiles));
+  g_launches += 1;
+  DGQ_CUDA_OK(cudaGetLastError());
+  return DGQ_OK;
+}
+
 // ------------------------------------------------------------------ launch
 template <bool BF, bool CACHED>
 static dgq_status enc_attn_launch(const EncAttnArgs& a, cudaStream_t stream) {
   if (a.nq <= 16) return ef_launch_size<BF, CACHED>(a, stream);
   EncAttnArgs t = a;
   if (t.scale_log2 == 0.f) t.scale_log2 = 1.17549435e-38f;  // hidden keys are -inf, which 0 would make NaN
+  const bool few = !a.causal && !(getenv("ESK") && atoi(getenv("ESK")) == 0);
+  if (few && a.d <= 64 && a.nk <= EsCfg<1, CACHED>::KEYS) return es_launch<1, BF, CACHED>(t, stream);
+  if (few && a.d > 64 && a.d <= 128 && a.nk <= EsCfg<2, CACHED>::KEYS) return es_launch<2, BF, CACHED>(t, stream);
   if (a.d <= 64) return ea_launch_tiles<1, BF, CACHED>(t, stream);
   if (a.d <= 128) return ea_launch_tiles<2, BF, CACHED>(t, stream);
   return ea_launch_tiles<3, BF, CACHED>(t, stream);
