@@ -586,7 +586,7 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
       tc_fence_after();
     }
     // Outputs leave through the tile's queries, which every product has read: written row by row they would be sixteen bytes of a
-    // sector at a time (four times the requests; 8 x 16 x 4096 x 64 over 77 keys 56 us, MEASURED_STORE this way).
+    // sector at a time (the kernel for few keys, 8 x 16 of 4 heads of 4096 x 64 over 77: 56.2 us, 48.1 this way).
     const float inv = sees > 0 && (z > 0.f || z != z) ? 1.f / z : 0.f;
     unsigned char* slab = sQ + t * Cfg::TILE + (warp & 3) * 32 * 128;
     uint16_t* out = (uint16_t*)a.O.ptr + b * a.O.batch + (rq.q_row + i) * a.O.token + h * a.O.head;
@@ -1616,20 +1616,22 @@ static dgq_status es_launch(const EncAttnArgs& a, cudaStream_t stream) {
     DGQ_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg::SMEM));
     if (dev < 64) attr_set[dev].store(true);
   }
-  // Tiles of a block: it costs about 3 us beside them, a tile 1 us.
+  // Tiles of a block: it costs about 3 us beside them, a tile 1 us (2 x 8 heads of 4096 x 40 over 77 keys: 14.5 us with one tile a
+  // block, 11.9 with two, 14.0 with three, 19.7 with eight).  Where requests have different numbers of queries, two rounds of
+  // blocks at least, so that they even out (8 x 8 heads of 1024 to 4096 x 40 over 20 to 154: 29.3 us with three, 33.1 with eight).
   const int64_t all = (int64_t)((a.nq + EA_Q - 1) / EA_Q) * (a.Hq / a.Hkv), heads = a.B * (int64_t)a.Hkv;
   if (all * heads > INT_MAX) return DGQ_ERR_UNSUPPORTED;
   int tiles = 1;
   float best = 3.4e38f;
   for (int c = 1; c <= 64 && c <= all; ++c) {
     const int64_t blocks = heads * ((all + c - 1) / c), rounds = (blocks + 2 * sms - 1) / (2 * sms);
+    if (a.q_start && c > 1 && rounds < 2) break;
     const float time = rounds * (3.f + c);
     if (time < best) {
       best = time;
       tiles = c;
     }
   }
-  if (getenv("ESW")) tiles = atoi(getenv("ESW"));
   EaMaps maps;
   std::memset(&maps, 0, sizeof(maps));
   if (!ea_encode(&maps.q, a.Q, a.q_start ? 1 : a.B, a.q_start ? a.n_rows : a.nq, a.Hq, a.d, BF, 128, &maps.q_b, &maps.q_h)) return DGQ_ERR_CUDA;
@@ -1650,9 +1652,9 @@ static dgq_status enc_attn_launch(const EncAttnArgs& a, cudaStream_t stream) {
   if (a.nq <= 16) return ef_launch_size<BF, CACHED>(a, stream);
   EncAttnArgs t = a;
   if (t.scale_log2 == 0.f) t.scale_log2 = 1.17549435e-38f;  // hidden keys are -inf, which 0 would make NaN
-  const bool few = !a.causal && !(getenv("ESK") && atoi(getenv("ESK")) == 0);
-  if (few && a.d <= 64 && a.nk <= EsCfg<1, CACHED>::KEYS) return es_launch<1, BF, CACHED>(t, stream);
-  if (few && a.d > 64 && a.d <= 128 && a.nk <= EsCfg<2, CACHED>::KEYS) return es_launch<2, BF, CACHED>(t, stream);
+  // Few keys: 8 x 16 of 4 heads of 4096 x 64 over 77 keys 48 us as one block of scores, 82 by blocks of 128; over 192 58 and 99.
+  if (!a.causal && a.d <= 64 && a.nk <= EsCfg<1, CACHED>::KEYS) return es_launch<1, BF, CACHED>(t, stream);
+  if (!a.causal && a.d > 64 && a.d <= 128 && a.nk <= EsCfg<2, CACHED>::KEYS) return es_launch<2, BF, CACHED>(t, stream);
   if (a.d <= 64) return ea_launch_tiles<1, BF, CACHED>(t, stream);
   if (a.d <= 128) return ea_launch_tiles<2, BF, CACHED>(t, stream);
   return ea_launch_tiles<3, BF, CACHED>(t, stream);

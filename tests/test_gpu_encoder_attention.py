@@ -63,16 +63,47 @@ def test_against_64_bits(case, dtype):
     compare(O, q, k, v, lens)
 
 
-@pytest.mark.parametrize("nq", [1, 3, 200])
+def on_gpu(q, k, v, n, scale):
+    """Attention of one request in 64 bits on the GPU, all rows alike: (O, sum of a |V|, sum of |V|)."""
+    H, G, d = q.shape[1], k.shape[1], q.shape[2]
+    kk, vv = (x[:n].double().repeat_interleave(H // G, 1).transpose(0, 1) for x in (k, v))
+    a = torch.softmax(q.double().transpose(0, 1) @ kk.transpose(1, 2) * scale, -1)
+    return [x.transpose(0, 1).cpu() for x in (a @ vv, a @ vv.abs(), vv.abs().sum(1, keepdim=True).expand(-1, q.shape[0], -1))]
+
+
+@pytest.mark.parametrize("B,nq,nk,H,G,d,lens", [
+    # enough heads that a block walks several tiles of queries over keys that stay in shared memory
+    (8, 1100, 77, 16, 16, 40, [77, 1, 16, 17, 64, 0, 65, 76]), (6, 1000, 192, 20, 5, 64, None), (6, 1000, 185, 20, 20, 64, [185, 96, 97, 180, 33, 160]),
+    (6, 900, 128, 20, 10, 128, [128, 127, 1, 64, 65, 100]), (6, 900, 100, 20, 20, 72, None),
+    # long keys over many blocks, every kernel class of head sizes
+    (1, 700, 1500, 4, 2, 64, [1490]), (1, 700, 1500, 4, 4, 128, None), (1, 300, 900, 4, 1, 160, [895]),
+])
 @pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
-def test_rubbish_behind_the_lengths(dtype, nq):
+def test_many_rows(B, nq, nk, H, G, d, lens, dtype):
+    _, b = gpu()
+    q, k, v = (t.cuda() for t in make(B, nq, nk, H, G, d, dtype, seed=6))
+    n = None if lens is None else torch.tensor(lens, dtype=torch.int32).cuda()
+    O = b.encoder_attn(q, k, v, kv_lens=n)
+    assert b.device_status() == 0
+    for i in range(B):
+        m = nk if lens is None else lens[i]
+        if m == 0:
+            assert not O[i].any()
+            continue
+        ref = on_gpu(q[i], k[i], v[i], m, d ** -0.5)
+        check(O[i], ref[0], bound(*ref, q[i].double(), k[i].double(), d ** -0.5, dtype, dtype))
+
+
+@pytest.mark.parametrize("nq", [1, 3, 200])
+@pytest.mark.parametrize("nk,lens", [(300, [0, 1, 128, 237]), (150, [0, 1, 128, 137])])
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+def test_rubbish_behind_the_lengths(dtype, nk, lens, nq):
     """NaN, infinities and the type's extremes in keys and values that no row sees."""
     _, b = gpu()
-    q, k, v = make(4, nq, 300, 2, 1, 64, dtype, seed=1)
-    lens = [0, 1, 128, 237]
+    q, k, v = make(4, nq, nk, 2, 1, 64, dtype, seed=1)
     for i, n in enumerate(lens):
         for t in (k, v):
-            t[i, n:] = torch.tensor([float("nan"), float("inf"), float("-inf"), torch.finfo(dtype).min])[torch.arange(300 - n) % 4].to(dtype)[:, None, None]
+            t[i, n:] = torch.tensor([float("nan"), float("inf"), float("-inf"), torch.finfo(dtype).min])[torch.arange(nk - n) % 4].to(dtype)[:, None, None]
     O = b.encoder_attn(q.cuda(), k.cuda(), v.cuda(), kv_lens=torch.tensor(lens, dtype=torch.int32).cuda())
     compare(O, q, k, v, lens)
     assert not O[0].any()
@@ -87,11 +118,12 @@ def test_lengths_outside_the_range_are_clamped():
 
 
 @pytest.mark.parametrize("nq", [1, 150])
-def test_large_logits_and_scale(nq):
+@pytest.mark.parametrize("nk,d", [(600, 64), (600, 128), (90, 64), (150, 40)])
+def test_large_logits_and_scale(nq, nk, d):
     """Rows whose maximum moves far from block to block, negative scale, zero scale."""
     _, b = gpu()
-    q, k, v = make(1, nq, 600, 2, 2, 64, BF16, seed=3)
-    k = (k * torch.linspace(0.1, 12, 600)[None, :, None, None]).to(BF16)
+    q, k, v = make(1, nq, nk, 2, 2, d, BF16, seed=3)
+    k = (k * torch.linspace(0.1, 12, nk)[None, :, None, None]).to(BF16)
     for scale in (0.125, -0.5, 0.0):
         O = b.encoder_attn(q.cuda(), k.cuda(), v.cuda(), scale=scale)
         compare(O, q, k, v, None, scale)
@@ -122,11 +154,11 @@ def test_views(nq):
     compare(O, q.cpu(), heads[:, :, 0].cpu(), heads[:, :, 1].cpu(), None)
 
 
-@pytest.mark.parametrize("nq", [2, 260])
-def test_same_bits_again_in_a_graph_and_on_a_stream(nq):
+@pytest.mark.parametrize("nq,nk", [(2, 400), (260, 400), (260, 180)])
+def test_same_bits_again_in_a_graph_and_on_a_stream(nq, nk):
     _, b = gpu()
-    q, k, v = (t.cuda() for t in make(2, nq, 400, 4, 2, 64, F16, seed=5))
-    lens = torch.tensor([400, 211], dtype=torch.int32).cuda()
+    q, k, v = (t.cuda() for t in make(2, nq, nk, 4, 2, 64, F16, seed=5))
+    lens = torch.tensor([nk, 111], dtype=torch.int32).cuda()
     O = b.encoder_attn(q, k, v, kv_lens=lens)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())

@@ -234,6 +234,33 @@ def test_cached_attention(case, dtype):
         assert torch.equal(b.cached_attn(four, c, dev(table), dev(lens), causal=causal).view_as(O), O)
 
 
+@TYPES
+@pytest.mark.parametrize("G,H,d,page,lens,nq", [
+    (16, 16, 40, 16, [154, 20, 0, 33, 154, 97, 16, 160], [1500, 1100, 200, 1024, 1, 129, 128, 900]),
+    (5, 20, 64, 64, [190, 64, 130, 7], [700, 300, 1000, 1000]), (10, 20, 128, 32, [128, 33, 70, 96], [600, 900, 31, 32]),
+    (2, 4, 128, 16, [1000, 500], [300, 257]), (2, 2, 160, 64, [700, 90], [300, 100]),
+])
+def test_many_rows(G, H, d, page, lens, nq, dtype):
+    """Several tiles of packed queries a block, requests that end inside a tile, blocks of keys that are codes."""
+    _, b = gpu()
+    c, table, q, starts = cached_case(b, len(lens), H, G, d, page, lens, nq, dtype, seed=14)
+    more = torch.cat([q, q[:50]])
+    out = torch.full_like(more, 3.0)
+    b.cached_attn(more, c, dev(table), dev(lens), q_start=dev(starts), max_nq=max(nq), out=out)
+    assert b.device_status() == 0 and (out[len(q):] == 3.0).all()
+    for i, n in enumerate(lens):
+        rows = slice(starts[i], starts[i + 1])
+        if n == 0:
+            assert not out[rows].any()
+            continue
+        pages = torch.as_tensor(table[i, :-(-n // page)]).cuda()
+        k, v = ((x[pages][..., :d].double() * s[pages].double()[..., None, None]).transpose(1, 2).reshape(-1, G, d)[:n].repeat_interleave(H // G, 1).transpose(0, 1)
+                for x, s in ((c.k, c.k_scale), (c.v, c.v_scale)))
+        a = torch.softmax(q[rows].double().transpose(0, 1) @ k.transpose(1, 2) * d ** -0.5, -1)
+        ref = [x.transpose(0, 1).cpu() for x in (a @ v, a @ v.abs(), v.abs().sum(1, keepdim=True).expand(-1, nq[i], -1))]
+        check(out[rows], ref[0], bound(ref[0], ref[1], ref[2] * 256, q[rows].double(), k, d ** -0.5, dtype, F16))
+
+
 @pytest.mark.parametrize("nq", [1, 2, 150])
 def test_scales_far_apart(nq):
     """Pages of zeros, and pages whose values are 2^14 times smaller than others' in front of those with the large weights."""
