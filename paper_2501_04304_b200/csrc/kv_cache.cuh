@@ -210,118 +210,149 @@ __device__ __forceinline__ float code_as_float(uint32_t biased_word, int i) {
   return __uint_as_float(__byte_perm(biased_word, 0x4B000000u, 0x7540 + i)) - 8388736.f;  // 2^23 + 128
 }
 
-// THREADS (one warp, or the block for large pages) take the runs of rows of one page that begin among `chunk` tokens, for one
-// head of K or V: largest value, scale, codes.  Most runs fit the registers and are read once.  64 prompts of 20 to 77 rows of
-// 20 x 64 into pages of 16: 43.4 us with a block per run, IEEE divisions and a second read, 18.2 us with the read-back now.
+// THREADS (one warp, or the block for large pages) take the runs of rows of one page that begin among `chunk` tokens, for one head's
+// keys and values at once: largest values, scales, codes.  Most runs fit the registers and are read once.  What bounds it is the
+// chain slots, rows, maximum, codes of a run, so keys and values go through it together and few tokens share a warp only where the
+// GPU is full without.  64 prompts of 20 to 77 rows of 20 x 64 into pages of 16: 43 us with a block per run, IEEE divisions and a
+// second read; 18.8 with a warp for keys and one for values, 13.5 as it is (cold; its floor is 3.7).
 template <bool BF, int THREADS>
 __global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(const __grid_constant__ KvWriteArgs a) {
-  __shared__ uint32_t red[WRITE_THREADS / 32];
+  __shared__ uint32_t red[2][WRITE_THREADS / 32];
   constexpr int GROUPS = WRITE_THREADS / THREADS;
   const int tid = threadIdx.x % THREADS, lane = threadIdx.x & 31;
-  const int h = blockIdx.y, which = blockIdx.z;
+  const int h = blockIdx.y;
   const int row_bytes = kv_row_bytes(a.d), units = a.d / 8;
   const int n_slots = a.n_pages << a.page_log2;
   pdl_launch_dependents();
   pdl_wait();
   const int64_t t0 = ((int64_t)blockIdx.x * GROUPS + threadIdx.x / THREADS) * a.chunk;
   // which of the tokens begin a run: those whose predecessor is not the slot before, and those in row 0 of a page
-  unsigned begins = 0;
+  unsigned begins;
+  int mine = -1;
   {
     const int64_t t = t0 + lane;
+    bool first = false;
     if (lane < a.chunk && t < a.T) {
-      const int slot = a.slots[t];
-      const bool real = slot >= 0 && slot < n_slots;
-      if (slot >= n_slots) record_error(DGQ_ERR_INVALID_ARG);
-      if (real && ((slot & (a.page - 1)) == 0 || t == 0 || a.slots[t - 1] != slot - 1)) begins = 1;
+      mine = a.slots[t];
+      const int before = t > 0 ? a.slots[t - 1] : -1;
+      if (mine >= n_slots && h == 0) record_error(DGQ_ERR_INVALID_ARG);
+      first = mine >= 0 && mine < n_slots && ((mine & (a.page - 1)) == 0 || t == 0 || before != mine - 1);
     }
-    begins = __ballot_sync(0xFFFFFFFFu, begins != 0);
+    begins = __ballot_sync(0xFFFFFFFFu, first);
   }
   // a thread has the same piece of rows tid / units, + step, ...
   const int step = THREADS / units, r_first = tid / units, c = tid - r_first * units;
   const bool works = r_first < step;
-  const uint16_t* x = a.x[which] + (int64_t)h * a.head[which] + c * 8;
   for (; begins; begins &= begins - 1) {
-    const int64_t t = t0 + (__ffs(begins) - 1);
-    const int slot = a.slots[t], r0 = slot & (a.page - 1);
+    const int at = __ffs(begins) - 1;
+    const int64_t t = t0 + at;
+    const int slot = __shfl_sync(0xFFFFFFFFu, mine, at), r0 = slot & (a.page - 1);
+    const int64_t ph = (int64_t)(slot >> a.page_log2) * a.n_heads + h;
+    float held[2] = {0.f, 0.f};
+    if (r0 > 0) {
+      held[0] = a.scale[0][ph];
+      held[1] = a.scale[1][ph];
+    }
     int n = 0;
-    for (int more = a.page - r0; n < more; n += 32) {
+    for (const int most = a.page - r0; n < most; n += 32) {
       const int i = n + lane;
-      const bool in = i < more && t + i < a.T && a.slots[t + i] == slot + i;
+      const bool in = i < most && t + i < a.T && a.slots[t + i] == slot + i;
       const unsigned ball = __ballot_sync(0xFFFFFFFFu, in);
       if (ball != 0xFFFFFFFFu) {
         n += __ffs(~ball) - 1;
         break;
       }
     }
-    const int64_t ph = (int64_t)(slot >> a.page_log2) * a.n_heads + h;
-    float* scale = a.scale[which] + ph;
-    const float held = r0 > 0 ? *scale : 0.f;
-    const uint16_t* rows = x + t * a.token[which];
-    uint4 q[WRITE_HELD];
-    uint32_t top2 = 0;
+    const uint16_t* rows[2];
+    uint4 q[2][WRITE_HELD];
+    uint32_t top2[2] = {0, 0};
 #pragma unroll
-    for (int k = 0; k < WRITE_HELD; ++k) {
-      const int r = r_first + k * step;
-      q[k] = make_uint4(0, 0, 0, 0);
-      if (works && r < n) q[k] = __ldg(reinterpret_cast<const uint4*>(rows + r * a.token[which]));
+    for (int w = 0; w < 2; ++w) {
+      rows[w] = a.x[w] + (int64_t)h * a.head[w] + c * 8 + t * a.token[w];
+#pragma unroll
+      for (int k = 0; k < WRITE_HELD; ++k) {
+        if (k * step >= n) break;
+        const int r = r_first + k * step;
+        q[w][k] = make_uint4(0, 0, 0, 0);
+        if (works && r < n) q[w][k] = __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w]));
+      }
     }
 #pragma unroll
-    for (int k = 0; k < WRITE_HELD; ++k)
-      top2 = absmax16<BF>(absmax16<BF>(absmax16<BF>(absmax16<BF>(top2, q[k].x), q[k].y), q[k].z), q[k].w);
-    if (works)
-#pragma unroll 4
-      for (int r = r_first + WRITE_HELD * step; r < n; r += step) {
-        const uint4 y = __ldg(reinterpret_cast<const uint4*>(rows + r * a.token[which]));
-        top2 = absmax16<BF>(absmax16<BF>(absmax16<BF>(absmax16<BF>(top2, y.x), y.y), y.z), y.w);
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int k = 0; k < WRITE_HELD; ++k) {
+        if (k * step >= n) break;
+        top2[w] = absmax16<BF>(absmax16<BF>(absmax16<BF>(absmax16<BF>(top2[w], q[w][k].x), q[w][k].y), q[w][k].z), q[w][k].w);
       }
+    if (works)
+#pragma unroll 2
+      for (int r = r_first + WRITE_HELD * step; r < n; r += step)
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top2 = absmax16<BF>(top2, __shfl_xor_sync(0xFFFFFFFFu, top2, o));
+        for (int w = 0; w < 2; ++w) {
+          const uint4 y = __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w]));
+          top2[w] = absmax16<BF>(absmax16<BF>(absmax16<BF>(absmax16<BF>(top2[w], y.x), y.y), y.z), y.w);
+        }
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top2[w] = absmax16<BF>(top2[w], __shfl_xor_sync(0xFFFFFFFFu, top2[w], o));
     if (THREADS > 32) {
-      if (lane == 0) red[threadIdx.x >> 5] = top2;
-      __syncthreads();  // also: everyone has read the old scale
+      if (lane == 0) {
+        red[0][threadIdx.x >> 5] = top2[0];
+        red[1][threadIdx.x >> 5] = top2[1];
+      }
+      __syncthreads();  // also: everyone has read the old scales
 #pragma unroll
-      for (int w = 0; w < THREADS / 32; ++w) top2 = absmax16<BF>(top2, red[w]);
+      for (int i = 0; i < THREADS / 32; ++i) {
+        top2[0] = absmax16<BF>(top2[0], red[0][i]);
+        top2[1] = absmax16<BF>(top2[1], red[1][i]);
+      }
     } else {
       __syncwarp();
     }
-    const float2 top = unpack16<BF>(top2);
-    // a scale below the smallest normal number would have no inverse
-    float s = fmaxf(top.x, top.y);
-    s = s > 0.f ? fmaxf(__fmul_rn(s, 1.0f / 127.0f), 1.17549435e-38f) : 0.f;
-    s = fmaxf(s, held);
-    const float inv = s > 0.f ? __fdiv_rn(1.0f, s) : 0.f;
-    int8_t* page = a.codes[which] + (ph << a.page_log2) * row_bytes;
-    if (r0 > 0 && s > held) {
-      const float ratio = __fmul_rn(held, inv);
-      for (int u = tid; u < r0 * (row_bytes / 16); u += THREADS) {
-        uint4* p = reinterpret_cast<uint4*>(page) + u;
-        const uint4 y = *p;
-        uint32_t w4[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t w = w4[i] ^ 0x80808080u;
-          uint32_t f[4];
+    for (int w = 0; w < 2; ++w) {
+      const float2 top = unpack16<BF>(top2[w]);
+      // a scale below the smallest normal number would have no inverse
+      float s = fmaxf(top.x, top.y);
+      s = s > 0.f ? fmaxf(__fmul_rn(s, 1.0f / 127.0f), 1.17549435e-38f) : 0.f;
+      s = fmaxf(s, held[w]);
+      const float inv = s > 0.f ? __fdiv_rn(1.0f, s) : 0.f;
+      int8_t* page = a.codes[w] + (ph << a.page_log2) * row_bytes;
+      if (r0 > 0 && s > held[w]) {
+        const float ratio = __fmul_rn(held[w], inv);
+        for (int u = tid; u < r0 * (row_bytes / 16); u += THREADS) {
+          uint4* p = reinterpret_cast<uint4*>(page) + u;
+          const uint4 y = *p;
+          uint32_t w4[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-          for (int k = 0; k < 4; ++k) f[k] = __float_as_uint(fmaf(code_as_float(w, k), ratio, 12582912.f));
-          w4[i] = __byte_perm(__byte_perm(f[0], f[1], 0x0040), __byte_perm(f[2], f[3], 0x0040), 0x5410);
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t x = w4[i] ^ 0x80808080u;
+            uint32_t f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[k] = __float_as_uint(fmaf(code_as_float(x, k), ratio, 12582912.f));
+            w4[i] = __byte_perm(__byte_perm(f[0], f[1], 0x0040), __byte_perm(f[2], f[3], 0x0040), 0x5410);
+          }
+          *p = make_uint4(w4[0], w4[1], w4[2], w4[3]);
         }
-        *p = make_uint4(w4[0], w4[1], w4[2], w4[3]);
       }
-    }
-    int8_t* dst = page + r0 * row_bytes + c * 8;
-    const auto put = [&](int r, const uint4& y) {
-      int8_t* at = dst + r * row_bytes;
-      *reinterpret_cast<uint2*>(at) = make_uint2(codes_of4<BF>(y.x, y.y, inv), codes_of4<BF>(y.z, y.w, inv));
-      if (c == units - 1 && (a.d & 8)) *reinterpret_cast<uint2*>(at + 8) = make_uint2(0, 0);
-    };
-    if (works) {
+      int8_t* dst = page + r0 * row_bytes + c * 8;
+      const auto put = [&](int r, const uint4& y) {
+        int8_t* to = dst + r * row_bytes;
+        *reinterpret_cast<uint2*>(to) = make_uint2(codes_of4<BF>(y.x, y.y, inv), codes_of4<BF>(y.z, y.w, inv));
+        if (c == units - 1 && (a.d & 8)) *reinterpret_cast<uint2*>(to + 8) = make_uint2(0, 0);
+      };
+      if (works) {
 #pragma unroll
-      for (int k = 0; k < WRITE_HELD; ++k)
-        if (r_first + k * step < n) put(r_first + k * step, q[k]);
+        for (int k = 0; k < WRITE_HELD; ++k) {
+          if (k * step >= n) break;
+          if (r_first + k * step < n) put(r_first + k * step, q[w][k]);
+        }
 #pragma unroll 2
-      for (int r = r_first + WRITE_HELD * step; r < n; r += step) put(r, __ldg(reinterpret_cast<const uint4*>(rows + r * a.token[which])));
+        for (int r = r_first + WRITE_HELD * step; r < n; r += step) put(r, __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w])));
+      }
+      if (tid == 0) a.scale[w][ph] = s;
     }
-    if (tid == 0) *scale = s;
     if (THREADS > 32) __syncthreads();  // red is free again
   }
 }
@@ -333,10 +364,12 @@ struct KvReadArgs {
   const int8_t* codes[2];
   const float* scale[2];
   const int32_t* slots;
-  int64_t n_units;                 // T * heads * d / 8
-  uint64_t per_units, per_heads;   // 2^64 / n rounded up: the high half of a product with it is the quotient
-  int n_pages, n_heads, page, page_log2, d;
+  int64_t T;
+  uint32_t per_row, per_units;   // 2^32 / n rounded up: the high half of a product with it is the quotient
+  int n_pages, n_heads, page, page_log2, d, tokens;
 };
+
+constexpr int READ_UNITS = 512;  // most pieces of a block's tokens (a token may have more)
 
 // Two codes (bytes i, i + 1 of a biased word) as values.
 template <bool BF>
@@ -344,26 +377,27 @@ __device__ __forceinline__ uint32_t values_of2(uint32_t w, int i, float s) {
   return pack16<BF>(__fmul_rn(code_as_float(w, i), s), __fmul_rn(code_as_float(w, i + 1), s));
 }
 
-// One thread: eight values of K and the same eight of V.  Quotients of indices below 2^32 by numbers below 2^16 come from one
-// multiplication.
+// A block has `tokens` tokens, a thread a piece of eight codes of K and the same of V at a time: sixteen bytes out, next to its
+// neighbours' (two pieces a thread wrote halves of sectors and took 14.7 us instead of 12.0 for 256 requests' last pages of 8 x
+// 128).  The index arithmetic stays in 32 bits: quotients of a block's piece numbers come from one multiplication.
 template <bool BF>
 __global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ KvReadArgs a) {
   pdl_launch_dependents();
   pdl_wait();
-  const int units = a.d / 8, row_bytes = kv_row_bytes(a.d), n_slots = a.n_pages << a.page_log2;
-  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < a.n_units; i += gridDim.x * 256ll) {
-    const bool small = a.n_units <= 0xFFFFFFFFll;
-    const int64_t th = units == 1 ? i : small ? (int64_t)__umul64hi(i, a.per_units) : i / units;
-    const int64_t t = a.n_heads == 1 ? th : small ? (int64_t)__umul64hi(th, a.per_heads) : th / a.n_heads;
-    const int c = (int)(i - th * units), h = (int)(th - t * a.n_heads);
-    const int slot = a.slots[t];
+  const int row_bytes = kv_row_bytes(a.d), units = a.d / 8, per_token = a.n_heads * units, n_slots = a.n_pages << a.page_log2;
+  const int64_t t0 = (int64_t)blockIdx.x * a.tokens;
+  const int pieces = (int)min((int64_t)a.tokens, a.T - t0) * per_token;
+  for (int u = threadIdx.x; u < pieces; u += 256) {
+    const int tl = per_token == 1 ? u : a.tokens == 1 ? 0 : (int)__umulhi((uint32_t)u, a.per_row), in = u - tl * per_token;
+    const int h = units == 1 ? in : (int)__umulhi((uint32_t)in, a.per_units), c = in - h * units;
+    const int slot = a.slots[t0 + tl];
     const bool real = slot >= 0 && slot < n_slots;
     if (slot >= n_slots) record_error(DGQ_ERR_INVALID_ARG);
-    const int64_t ph = real ? (int64_t)(slot >> a.page_log2) * a.n_heads + h : 0;
-    const int64_t at = ((ph << a.page_log2) + (slot & (a.page - 1))) * row_bytes + c * 8;
     uint2 q[2] = {make_uint2(0, 0), make_uint2(0, 0)};
     float s[2] = {0.f, 0.f};
     if (real) {
+      const int64_t ph = (int64_t)(slot >> a.page_log2) * a.n_heads + h;
+      const int64_t at = ((ph << a.page_log2) + (slot & (a.page - 1))) * row_bytes + c * 8;
 #pragma unroll
       for (int w = 0; w < 2; ++w) {
         q[w] = __ldg(reinterpret_cast<const uint2*>(a.codes[w] + at));
@@ -372,9 +406,9 @@ __global__ void __launch_bounds__(256) kv_read_kernel(const __grid_constant__ Kv
     }
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      const uint32_t u = q[w].x ^ 0x80808080u, v = q[w].y ^ 0x80808080u;
-      *reinterpret_cast<uint4*>(a.y[w] + t * a.token[w] + h * a.head[w] + c * 8) =
-          make_uint4(values_of2<BF>(u, 0, s[w]), values_of2<BF>(u, 2, s[w]), values_of2<BF>(v, 0, s[w]), values_of2<BF>(v, 2, s[w]));
+      const uint32_t x = q[w].x ^ 0x80808080u, y = q[w].y ^ 0x80808080u;
+      *reinterpret_cast<uint4*>(a.y[w] + (t0 + tl) * a.token[w] + h * a.head[w] + c * 8) =
+          make_uint4(values_of2<BF>(x, 0, s[w]), values_of2<BF>(x, 2, s[w]), values_of2<BF>(y, 0, s[w]), values_of2<BF>(y, 2, s[w]));
     }
   }
 }
@@ -433,12 +467,12 @@ extern "C" dgq_status dgq_kv_write(const dgq_kv_cache* cache, const dgq_rows* K,
   DGQ_CUDA_OK(sm_count(&sms));
   const int group = cache->page > 32 ? WRITE_THREADS : 32;
   a.chunk = 16;
-  while (a.chunk > 1 && T * cache->n_heads * 2 / a.chunk * group < (int64_t)sms * 2048) a.chunk /= 4;
+  while (a.chunk > 1 && T * cache->n_heads / a.chunk * group < (int64_t)sms * 768) a.chunk /= 4;
   const int64_t per_block = (int64_t)a.chunk * (WRITE_THREADS / group), blocks = (T + per_block - 1) / per_block;
   if (blocks > INT_MAX) return DGQ_ERR_UNSUPPORTED;
   const auto kernel = dtype == DGQ_BF16 ? (group == 32 ? kv_write_kernel<true, 32> : kv_write_kernel<true, WRITE_THREADS>)
                                         : (group == 32 ? kv_write_kernel<false, 32> : kv_write_kernel<false, WRITE_THREADS>);
-  DGQ_CUDA_OK(launch_pdl(kernel, dim3((unsigned)blocks, (unsigned)cache->n_heads, 2), dim3(WRITE_THREADS), 0, (cudaStream_t)stream, a));
+  DGQ_CUDA_OK(launch_pdl(kernel, dim3((unsigned)blocks, (unsigned)cache->n_heads), dim3(WRITE_THREADS), 0, (cudaStream_t)stream, a));
   g_launches += 1;
   DGQ_CUDA_OK(cudaGetLastError());
   return DGQ_OK;
@@ -463,17 +497,18 @@ extern "C" dgq_status dgq_kv_read(const dgq_kv_cache* cache, const int32_t* slot
     a.scale[i] = i ? cache->v_scale : cache->k_scale;
   }
   a.slots = slots;
-  a.n_units = T * cache->n_heads * (cache->d / 8);
-  a.per_units = ~0ull / (uint64_t)(cache->d / 8) + 1;
-  a.per_heads = ~0ull / (uint64_t)cache->n_heads + 1;
-  a.page_log2 = kv_log2(cache->page);
+  const int units = cache->d / 8, per_token = units * cache->n_heads;
+  a.T = T;
+  a.tokens = (int)std::min<int64_t>(std::max(1, READ_UNITS / per_token), T);
+  a.per_row = (uint32_t)((1ull << 32) / per_token + 1);
+  a.per_units = (uint32_t)((1ull << 32) / units + 1);
   a.n_pages = cache->n_pages;
   a.n_heads = cache->n_heads;
   a.page = cache->page;
+  a.page_log2 = kv_log2(cache->page);
   a.d = cache->d;
-  int sms = 0;
-  DGQ_CUDA_OK(sm_count(&sms));
-  const int64_t blocks = std::min<int64_t>((a.n_units + 255) / 256, (int64_t)sms * 32);
+  const int64_t blocks = (T + a.tokens - 1) / a.tokens;
+  if (blocks > INT_MAX) return DGQ_ERR_UNSUPPORTED;
   DGQ_CUDA_OK(launch_pdl(dtype == DGQ_BF16 ? kv_read_kernel<true> : kv_read_kernel<false>, dim3((unsigned)blocks), dim3(256), 0,
                          (cudaStream_t)stream, a));
   g_launches += 1;
