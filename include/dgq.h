@@ -272,8 +272,8 @@ dgq_status dgq_kv_plan(const int32_t* lens, const int32_t* n_new, int B, const i
  * stand next to each other in ascending order, as dgq_kv_plan gives them, and no slot comes twice in a call.  For each page and
  * head, in fp32: top = max |x| over the page's rows of this call, s = max(top * (1 / 127), 2^-126), 0 where top is 0; a page whose
  * row 0 is among them forgets what it held, any other one keeps its rows below the first new one: s = max(s, scale), and where s has
- * grown, their codes become rint(code * (scale * inv)), inv = 1 / s.  New codes are rint(x * inv), the product rounded once (to
- * the nearest whole number, ties to even), 0 where s is 0.  Rows behind the
+ * grown, their codes become rint((code * scale) / s).  New codes are rint(x / s), 0 where s is 0.  Each operation is rounded to
+ * fp32, rint to the nearest whole number, ties to even.  Rows behind the
  * new ones stay as they are.  Inputs must be finite.  A slot beyond the cache is skipped and recorded as
  * DGQ_ERR_INVALID_ARG in the status word.
  * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED, CUDA. */

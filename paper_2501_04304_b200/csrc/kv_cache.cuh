@@ -197,14 +197,34 @@ __device__ __forceinline__ uint32_t absmax16(uint32_t top, uint32_t x) {
   const __half2 r = __hmax2(*reinterpret_cast<const __half2*>(&top), *reinterpret_cast<const __half2*>(&x));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-// Codes of four 16-bit numbers: adding 1.5 * 2^23 to the exact product rounds it to a whole number, whose low byte is the code.  (No
-// clamp: |x| <= 127 s up to the last bit of s, so |x * inv| < 127.5.)
+// Codes of four 16-bit numbers: rint(x / s), the quotient rounded to fp32.  x * inv is within 127 * 2^-23 of it, so the two round to the
+// same whole number unless a border of two codes is that near; `near` then tells that these (a few in 10^5, half the largest value
+// among them) have to be divided.  Adding 1.5 * 2^23 rounds to a whole number, whose low byte is the code; no clamp is needed:
+// |x| <= 127 s up to the last bit of s.
+__device__ __forceinline__ uint32_t low_bytes(const float (&t)[4]) {
+  return __byte_perm(__byte_perm(__float_as_uint(t[0]), __float_as_uint(t[1]), 0x0040),
+                     __byte_perm(__float_as_uint(t[2]), __float_as_uint(t[3]), 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint32_t codes_by_division(float4 x, float s) {
+  const float t[4] = {__fadd_rn(__fdiv_rn(x.x, s), 12582912.f), __fadd_rn(__fdiv_rn(x.y, s), 12582912.f),
+                      __fadd_rn(__fdiv_rn(x.z, s), 12582912.f), __fadd_rn(__fdiv_rn(x.w, s), 12582912.f)};
+  return low_bytes(t);
+}
 template <bool BF>
-__device__ __forceinline__ uint32_t codes_of4(uint32_t a, uint32_t b, float inv) {
+__device__ __forceinline__ uint32_t codes_of4(uint32_t a, uint32_t b, float inv, float& near) {
+  const unsigned long long magic = pack_f32x2(12582912.f, 12582912.f), minus = pack_f32x2(-12582912.f, -12582912.f);
+  const unsigned long long inv2 = pack_f32x2(inv, inv), one = pack_f32x2(-1.f, -1.f), zero = 0ull;
   const float2 lo = unpack16<BF>(a), hi = unpack16<BF>(b);
-  const uint32_t y0 = __float_as_uint(fmaf(lo.x, inv, 12582912.f)), y1 = __float_as_uint(fmaf(lo.y, inv, 12582912.f));
-  const uint32_t y2 = __float_as_uint(fmaf(hi.x, inv, 12582912.f)), y3 = __float_as_uint(fmaf(hi.y, inv, 12582912.f));
-  return __byte_perm(__byte_perm(y0, y1, 0x0040), __byte_perm(y2, y3, 0x0040), 0x5410);
+  float t[4], d[4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const unsigned long long y = fma_f32x2(i ? pack_f32x2(hi.x, hi.y) : pack_f32x2(lo.x, lo.y), inv2, zero);
+    const unsigned long long u = add_f32x2(y, magic);
+    unpack_f32x2(u, t[2 * i], t[2 * i + 1]);
+    unpack_f32x2(fma_f32x2(add_f32x2(u, minus), one, y), d[2 * i], d[2 * i + 1]);
+  }
+  near = fmaxf(near, fmaxf(fmaxf(fabsf(d[0]), fabsf(d[1])), fmaxf(fabsf(d[2]), fabsf(d[3]))));
+  return low_bytes(t);
 }
 __device__ __forceinline__ float code_as_float(uint32_t biased_word, int i) {
   return __uint_as_float(__byte_perm(biased_word, 0x4B000000u, 0x7540 + i)) - 8388736.f;  // 2^23 + 128
@@ -213,8 +233,8 @@ __device__ __forceinline__ float code_as_float(uint32_t biased_word, int i) {
 // THREADS (one warp, or the block for large pages) take the runs of rows of one page that begin among `chunk` tokens, for one head's
 // keys and values at once: largest values, scales, codes.  Most runs fit the registers and are read once.  What bounds it is the
 // chain slots, rows, maximum, codes of a run, so keys and values go through it together and few tokens share a warp only where the
-// GPU is full without.  64 prompts of 20 to 77 rows of 20 x 64 into pages of 16: 43 us with a block per run, IEEE divisions and a
-// second read; 18.8 with a warp for keys and one for values, 13.5 as it is (cold; its floor is 3.7).
+// GPU is full without.  64 prompts of 20 to 77 rows of 20 x 64 into pages of 16 and out again: 43 us with a block per run, a division
+// per value and a second read; 18.2 with a warp for keys and one for values; 16.6 as it is (floor of both directions 6.1).
 template <bool BF, int THREADS>
 __global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(const __grid_constant__ KvWriteArgs a) {
   __shared__ uint32_t red[2][WRITE_THREADS / 32];
@@ -320,36 +340,45 @@ __global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(const __grid_co
       const float inv = s > 0.f ? __fdiv_rn(1.0f, s) : 0.f;
       int8_t* page = a.codes[w] + (ph << a.page_log2) * row_bytes;
       if (r0 > 0 && s > held[w]) {
-        const float ratio = __fmul_rn(held[w], inv);
         for (int u = tid; u < r0 * (row_bytes / 16); u += THREADS) {
           uint4* p = reinterpret_cast<uint4*>(page) + u;
           const uint4 y = *p;
           uint32_t w4[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
+#pragma unroll 1
           for (int i = 0; i < 4; ++i) {
             const uint32_t x = w4[i] ^ 0x80808080u;
-            uint32_t f[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) f[k] = __float_as_uint(fmaf(code_as_float(x, k), ratio, 12582912.f));
-            w4[i] = __byte_perm(__byte_perm(f[0], f[1], 0x0040), __byte_perm(f[2], f[3], 0x0040), 0x5410);
+            w4[i] = codes_by_division(make_float4(__fmul_rn(code_as_float(x, 0), held[w]), __fmul_rn(code_as_float(x, 1), held[w]),
+                                                  __fmul_rn(code_as_float(x, 2), held[w]), __fmul_rn(code_as_float(x, 3), held[w])), s);
           }
           *p = make_uint4(w4[0], w4[1], w4[2], w4[3]);
         }
       }
       int8_t* dst = page + r0 * row_bytes + c * 8;
-      const auto put = [&](int r, const uint4& y) {
+      float near = 0.f;
+      const auto put = [&](int r, uint32_t lo, uint32_t hi) {
         int8_t* to = dst + r * row_bytes;
-        *reinterpret_cast<uint2*>(to) = make_uint2(codes_of4<BF>(y.x, y.y, inv), codes_of4<BF>(y.z, y.w, inv));
+        *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
         if (c == units - 1 && (a.d & 8)) *reinterpret_cast<uint2*>(to + 8) = make_uint2(0, 0);
       };
       if (works) {
 #pragma unroll
         for (int k = 0; k < WRITE_HELD; ++k) {
           if (k * step >= n) break;
-          if (r_first + k * step < n) put(r_first + k * step, q[w][k]);
+          if (r_first + k * step < n) put(r_first + k * step, codes_of4<BF>(q[w][k].x, q[w][k].y, inv, near), codes_of4<BF>(q[w][k].z, q[w][k].w, inv, near));
         }
-#pragma unroll 2
-        for (int r = r_first + WRITE_HELD * step; r < n; r += step) put(r, __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w])));
+#pragma unroll 1
+        for (int r = r_first + WRITE_HELD * step; r < n; r += step) {
+          const uint4 y = __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w]));
+          put(r, codes_of4<BF>(y.x, y.y, inv, near), codes_of4<BF>(y.z, y.w, inv, near));
+        }
+        if (near > 0.49998f) {
+#pragma unroll 1
+          for (int r = r_first; r < n; r += step) {
+            const uint4 y = __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w]));
+            const float2 f0 = unpack16<BF>(y.x), f1 = unpack16<BF>(y.y), f2 = unpack16<BF>(y.z), f3 = unpack16<BF>(y.w);
+            put(r, codes_by_division(make_float4(f0.x, f0.y, f1.x, f1.y), s), codes_by_division(make_float4(f2.x, f2.y, f3.x, f3.y), s));
+          }
+        }
       }
       if (tid == 0) a.scale[w][ph] = s;
     }

@@ -74,12 +74,10 @@ def quantize_reference(x, slots, codes, scale, page):
         s = torch.where(top > 0, torch.clamp(top * torch.tensor(1.0 / 127.0), min=2.0 ** -126), torch.zeros(()))
         if first:
             s = torch.maximum(s, scale[p])
-        inv = torch.where(s > 0, 1 / s, torch.zeros(()))
         if first:
             old = codes[p, :, :first].float()
-            ratio = (scale[p] * inv).double()  # products of 24 and fewer bits are exact in 64
-            codes[p, :, :first] = torch.where((s > scale[p])[:, None, None], (old.double() * ratio[:, None, None]).round().float(), old).to(torch.int8)
-        q = (new.double() * inv.double()[None, :, None]).round().to(torch.int8)
+            codes[p, :, :first] = torch.where((s > scale[p])[:, None, None], (old * scale[p][:, None, None] / s[:, None, None]).round(), old).to(torch.int8)
+        q = torch.where(s[None, :, None] > 0, new / s[None, :, None], torch.zeros(())).round().to(torch.int8)
         for i, r in enumerate(at):
             codes[p, :, r, :d] = q[i]
             codes[p, :, r, d:] = 0
@@ -116,7 +114,7 @@ def test_write_and_read(heads, d, page, slots, dtype):
     k, v = (torch.randn(len(slots), heads, d, generator=g).to(dtype) * f for f in (1.0, 3.0))
     want = [quantize_reference(x, slots, codes.cpu(), scale.cpu(), page) for x, codes, scale in ((k, c.k, c.k_scale), (v, c.v, c.v_scale))]
     b.kv_write(c, k.cuda(), v.cuda(), dev(slots))
-    # bit for bit: both sides round the same products
+    # bit for bit: both sides round the same 32-bit quotients
     assert torch.equal(c.k.cpu(), want[0][0]) and torch.equal(c.k_scale.cpu(), want[0][1])
     assert torch.equal(c.v.cpu(), want[1][0]) and torch.equal(c.v_scale.cpu(), want[1][1])
     rk, rv = b.kv_read(c, dev(slots), dtype)
@@ -149,6 +147,20 @@ def test_write_zeros_and_views():
     # a page whose rows are all zero takes the scale of what comes next
     b.kv_write(c, fused[:4, 1], fused[:4, 1], dev([36, 37, 38, 39]))
     assert (c.v_scale[2, 1] > 0).item()
+
+
+@TYPES
+def test_codes_near_borders(dtype):
+    """Rows full of odd multiples of half a scale, up to the type's rounding: the quotient in 32 bits decides."""
+    _, b = gpu()
+    c = b.KvCache.empty(300, 1, 16, 64)
+    top = (torch.rand(300, generator=torch.Generator().manual_seed(15)) * 60 + 0.01).to(dtype)
+    x = (top.float()[:, None] * (2 * torch.arange(64) + 1) / 254).to(dtype)
+    x[:, 63], x[:, 31], x[:, 30] = top, top / 2, -top / 2
+    slots = [16 * i for i in range(300)]
+    b.kv_write(c, x[:, None].cuda(), (-x[:, None]).cuda(), dev(slots))
+    codes, scale = quantize_reference(x[:, None], slots, torch.zeros(300, 1, 16, 64, dtype=torch.int8), torch.zeros(300, 1), 16)
+    assert torch.equal(c.k.cpu(), codes) and torch.equal(c.v.cpu(), -codes) and torch.equal(c.k_scale.cpu(), scale)
 
 
 def test_slots_beyond_the_cache():
