@@ -273,6 +273,22 @@ def test_many_rows(G, H, d, page, lens, nq, dtype):
         check(out[rows], ref[0], bound(ref[0], ref[1], ref[2] * 256, q[rows].double(), k, d ** -0.5, dtype, F16))
 
 
+@pytest.mark.parametrize("nq,lens", [(1, [200, 77]), (140, [200, 77]), (140, [160, 77])])
+def test_queries_of_any_size(nq, lens):
+    """bf16 queries far outside fp16's range: a power of two in the queries and its inverse in the scale change no bit."""
+    _, b = gpu()
+    c, table, q, starts = cached_case(b, 2, 4, 2, 64, 16, lens, [nq, nq], BF16, seed=16)
+    four = q.view(2, nq, 4, 64)
+    O = b.cached_attn(four, c, dev(table), dev(lens), scale=0.125)
+    compare(O.view(-1, 4, 64), q, c, table, lens, starts, False)
+    for e in (60, -60):
+        assert torch.equal(b.cached_attn((four.float() * 2.0 ** e).bfloat16(), c, dev(table), dev(lens), scale=0.125 * 2.0 ** -e), O)
+    # the outputs in the queries' place
+    same = four.clone()
+    b.cached_attn(same, c, dev(table), dev(lens), scale=0.125, out=same)
+    assert torch.equal(same, O)
+
+
 @pytest.mark.parametrize("nq", [1, 2, 150])
 def test_scales_far_apart(nq):
     """Pages of zeros, and pages whose values are 2^14 times smaller than others' in front of those with the large weights."""
