@@ -24,6 +24,7 @@ struct EncAttnArgs {
   int64_t n_rows;
   int causal;
   int bf;                       // Q and O are bf16
+  int by_length;                // blocks take the requests longest first (at most EA_SORTED of them)
 };
 
 // What a block needs to know of its request.
@@ -49,6 +50,23 @@ __device__ __forceinline__ EncRequest enc_request(const EncAttnArgs& a, int b) {
 // Keys that query i of the request sees.
 __device__ __forceinline__ int enc_sees(const EncAttnArgs& a, const EncRequest& r, int i) {
   return a.causal ? max(r.len - r.nq + i + 1, 0) : r.len;
+}
+
+// The request of a given rank by length, for all threads of a block: where blocks run in several rounds, the last ones to start
+// should be short.
+constexpr int EA_SORTED = 128;
+__device__ __forceinline__ int enc_request_of_rank(const EncAttnArgs& a, int rank) {
+  __shared__ int lens[EA_SORTED], found;
+  const int j = threadIdx.x;
+  if (j < a.B) lens[j] = a.kv_lens[j];
+  __syncthreads();
+  if (j < a.B) {
+    int r = 0;
+    for (int k = 0; k < a.B; ++k) r += lens[k] > lens[j] || (lens[k] == lens[j] && k < j);
+    if (r == rank) found = j;
+  }
+  __syncthreads();
+  return found;
 }
 
 // ------------------------------------------------------------------ many query rows: tcgen05
@@ -202,7 +220,8 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
   const int n_tiles = (a.nq + EA_Q * NT - 1) / (EA_Q * NT);
   // the tiles that see most come first where that differs
   const int tile = a.causal ? n_tiles - 1 - (int)(blockIdx.x % n_tiles) : (int)(blockIdx.x % n_tiles);
-  const int h = (int)(blockIdx.x / n_tiles) % a.Hq, b = (int)(blockIdx.x / n_tiles) / a.Hq;
+  const int h = (int)(blockIdx.x / n_tiles) % a.Hq;
+  int b = (int)(blockIdx.x / n_tiles) / a.Hq;
   const int g = h / (a.Hq / a.Hkv);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -232,6 +251,7 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
   pdl_launch_dependents();  // not before this block has its tensor memory: a block of the next kernel could take it and wait for this one
   const uint32_t tmem_base = sh->tmem_base;
 
+  if (a.by_length) b = enc_request_of_rank(a, b);
   const EncRequest rq = enc_request(a, b);
   const int row0 = tile * (EA_Q * NT);
   // keys and key blocks that each tile walks: as many as its last row sees
@@ -675,7 +695,11 @@ static dgq_status ea_launch_tiles(const EncAttnArgs& a, cudaStream_t stream) {
                   !ea_encode(&maps.v, a.V, a.B, a.nk, a.Hkv, a.d, BF, 128, &maps.v_b, &maps.v_h)))
     return DGQ_ERR_CUDA;
   if (!ea_encode(&maps.o, a.O, a.q_start ? 1 : a.B, a.q_start ? a.n_rows : a.nq, a.Hq, a.d, BF, 32, &maps.o_b, &maps.o_h)) return DGQ_ERR_CUDA;
-  DGQ_CUDA_OK(launch_pdl(enc_attn_tiles_kernel<NP, BF, CACHED>, dim3((unsigned)grid), dim3(Cfg::THREADS), (size_t)Cfg::SMEM, stream, maps, a));
+  int sms = 0;
+  DGQ_CUDA_OK(sm_count(&sms));
+  EncAttnArgs aa = a;
+  aa.by_length = a.kv_lens && a.B > 1 && a.B <= EA_SORTED && grid > Cfg::BLOCKS * sms;
+  DGQ_CUDA_OK(launch_pdl(enc_attn_tiles_kernel<NP, BF, CACHED>, dim3((unsigned)grid), dim3(Cfg::THREADS), (size_t)Cfg::SMEM, stream, maps, aa));
   g_launches += 1;
   DGQ_CUDA_OK(cudaGetLastError());
   return DGQ_OK;
@@ -690,7 +714,6 @@ static dgq_status ea_launch_tiles(const EncAttnArgs& a, cudaStream_t stream) {
 // the blocks of a request in the shared memory of their cluster, in a fixed order.
 enum { EF_I8 = 0, EF_F16 = 1, EF_BF16 = 2 };
 constexpr int EF_SPLITS = 16;   // most blocks of a cluster
-constexpr int EF_SORTED = 128;  // most requests that are taken in the order of their lengths
 
 template <int SRC, int DC, int NTL>
 struct EfCfg {
@@ -751,7 +774,7 @@ __device__ __forceinline__ uint2 ld_stream8(const void* p) {
 }
 
 template <int SRC, int DC, int NTL>
-__global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant__ EncAttnArgs a, int splits, int by_length) {
+__global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant__ EncAttnArgs a, int splits) {
   using Cfg = EfCfg<SRC, DC, NTL>;
   constexpr bool I8 = Cfg::I8;
   constexpr bool M_BF = SRC == EF_BF16;       // type of both products' operands; codes: fp16
@@ -774,20 +797,7 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
   int b = (int)(blockIdx.x / splits) / a.Hkv;
   pdl_launch_dependents();
   pdl_wait();
-  if (by_length) {
-    // longest first, so that the last blocks to start are short ones: the request whose rank is this block's number
-    __shared__ int lens[EF_SORTED], mine;
-    const int j = threadIdx.x;
-    if (j < a.B) lens[j] = a.kv_lens[j];
-    __syncthreads();
-    if (j < a.B) {
-      int rank = 0;
-      for (int k = 0; k < a.B; ++k) rank += lens[k] > lens[j] || (lens[k] == lens[j] && k < j);
-      if (rank == b) mine = j;
-    }
-    __syncthreads();
-    b = mine;
-  }
+  if (a.by_length) b = enc_request_of_rank(a, b);
   const EncRequest rq = enc_request(a, b);
 
   // this block's keys: whole steps, the same number for every block of the cluster but the last ones
@@ -1218,7 +1228,8 @@ static dgq_status ef_launch(const EncAttnArgs& a, cudaStream_t stream) {
     splits *= 2;
   const int64_t blocks = base / blocks_z * splits;
   if (blocks > INT_MAX || blocks_z > 65535) return DGQ_ERR_UNSUPPORTED;
-  const int by_length = a.kv_lens && a.B > 1 && a.B <= EF_SORTED && blocks > 2 * sms;
+  EncAttnArgs aa = a;
+  aa.by_length = a.kv_lens && a.B > 1 && a.B <= EA_SORTED && blocks > 4 * sms;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks, (unsigned)blocks_z);
   cfg.blockDim = dim3(128);
@@ -1232,7 +1243,7 @@ static dgq_status ef_launch(const EncAttnArgs& a, cudaStream_t stream) {
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = pdl_enabled() ? 2 : 1;
-  DGQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a, splits, by_length));
+  DGQ_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, aa, splits));
   g_launches += 1;
   DGQ_CUDA_OK(cudaGetLastError());
   return DGQ_OK;
