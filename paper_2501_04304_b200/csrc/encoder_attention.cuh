@@ -1297,13 +1297,6 @@ __device__ __forceinline__ void pin16(uint32_t (&r)[16]) {
   asm volatile("" : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
                "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]));
 }
-// 32 lanes x 8 consecutive 32-bit columns: thread i of the warp writes row (lane base + i).
-__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
-               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-               : "memory");
-}
-
 template <int NP, bool BF, bool CACHED>
 __global__ void __launch_bounds__(EsCfg<NP, CACHED>::THREADS, 2)
 enc_attn_short_kernel(const __grid_constant__ EaMaps maps, const __grid_constant__ EncAttnArgs a, int chunk_tiles) {
