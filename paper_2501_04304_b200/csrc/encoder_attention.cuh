@@ -795,7 +795,6 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
   const int split = (int)blockIdx.x % splits;  // heads lie in x too, so that a request's blocks are dealt out together
   const int g = (int)(blockIdx.x / splits) % a.Hkv, col0 = (int)blockIdx.y * N;
   int b = (int)(blockIdx.x / splits) / a.Hkv;
-  pdl_launch_dependents();
   pdl_wait();
   if (a.by_length) b = enc_request_of_rank(a, b);
   const EncRequest rq = enc_request(a, b);
@@ -1097,6 +1096,7 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
     find_pages(step + 2 * Cfg::WARPS);
   }
 
+  pdl_launch_dependents();  // blocks of the next kernel that wait from the start take 0.6 us of 16 x 16 x 1 x 64 over 1000 keys (12.4 us)
   // ------------------------------------------------------------ the warps of the block
 #pragma unroll
   for (int nt = 0; nt < NTL; ++nt)
