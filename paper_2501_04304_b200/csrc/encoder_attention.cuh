@@ -806,7 +806,8 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
 
   // ------------------------------------------------------------ loads of a step
   // Nothing here is conditional on a lane: a piece beyond a row is another one's instead (Q is zero there, or the feature is not
-  // written), a group of absent keys is page 0's (their weights are 0), and a 16-bit row beyond the keys is the last one's.
+  // written; a 16-bit key's, which may hold an infinity, becomes zero), a group of absent keys is page 0's (their weights are 0), and
+  // a 16-bit row beyond the keys is the last one's.
   const int row_bytes = I8 ? kv_row_bytes(a.d) : a.d * 2;
   uint4 kx[GR][2][KR];
   uint4 vx[GR][4][VR];
@@ -818,6 +819,7 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
   for (int r = 0; r < KR; ++r) kc[r] = (lt + 4 * r) * 16 < row_bytes ? (lt + 4 * r) * 16 : 0;
 #pragma unroll
   for (int r = 0; r < VR; ++r) vc[r] = (lg + 8 * r) * Cfg::VB < row_bytes ? (lg + 8 * r) * Cfg::VB : 0;
+  const bool short_rows = !I8 && row_bytes < KR * 64;
   const uint8_t* k_rows = I8 ? nullptr : (const uint8_t*)a.K.ptr + 2 * (b * a.K.batch + g * a.K.head);
   const uint8_t* v_rows = I8 ? nullptr : (const uint8_t*)a.V.ptr + 2 * (b * a.V.batch + g * a.V.head);
   auto find_pages = [&](int st) {
@@ -825,7 +827,7 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
 #pragma unroll
     for (int i = 0; i < GR; ++i) {
       const int key = st * Cfg::CH + i * 16;
-      page_next[i] = key < rq.len ? __ldg(table + (key >> a.page_log2)) : -2;
+      page_next[i] = key < rq.len ? __ldg(table + (key >> a.page_log2)) : -1;
     }
   };
   auto load_k = [&](int st) {
@@ -836,7 +838,7 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
       if (I8) {
         const int p = page_next[i];
         const bool real = p >= 0 && p < a.n_pages;
-        if (!real && p != -2) record_error(DGQ_ERR_INVALID_ARG);
+        if (!real && key < rq.len) record_error(DGQ_ERR_INVALID_ARG);
         const int64_t ph = real ? (int64_t)p * a.Hkv + g : 0;
         ks[i] = __ldg(a.k_scale + ph);
         vs[i] = real ? __ldg(a.v_scale + ph) : -1.f;  // negative: absent
@@ -850,7 +852,10 @@ __global__ void __launch_bounds__(128) enc_attn_few_kernel(const __grid_constant
         for (int hh = 0; hh < 2; ++hh) {
           const uint8_t* base = k_rows + 2 * a.K.token * min(key + lg + 8 * hh, rq.len - 1);
 #pragma unroll
-          for (int r = 0; r < KR; ++r) kx[i][hh][r] = ld_stream16(base + kc[r]);
+          for (int r = 0; r < KR; ++r) {
+            kx[i][hh][r] = ld_stream16(base + kc[r]);
+            if (short_rows && (lt + 4 * r) * 16 >= row_bytes) kx[i][hh][r] = make_uint4(0, 0, 0, 0);
+          }
         }
       }
     }

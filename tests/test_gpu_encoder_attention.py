@@ -109,6 +109,19 @@ def test_rubbish_behind_the_lengths(dtype, nk, lens, nq):
     assert not O[0].any()
 
 
+@pytest.mark.parametrize("nq", [1, 12, 150])
+@pytest.mark.parametrize("nk,d", [(90, 40), (300, 40), (90, 64), (260, 24), (300, 104), (200, 144)])
+def test_a_key_that_scores_minus_infinity(nk, d, nq):
+    """One feature of one key is -inf where every query is positive: its weight is 0, whichever pieces of a row a lane has."""
+    _, b = gpu()
+    q, k, v = make(1, nq, nk, 2, 1, d, F16, seed=7)
+    q[..., 0] = 1.0
+    k[0, 5, :, 0] = float("-inf")
+    O = b.encoder_attn(q.cuda(), k.cuda(), v.cuda())
+    rest = [i for i in range(nk) if i != 5]
+    compare(O, q, k[:, rest], v[:, rest], None)
+
+
 def test_lengths_outside_the_range_are_clamped():
     _, b = gpu()
     q, k, v = make(3, 20, 50, 1, 1, 40, F16, seed=2)
