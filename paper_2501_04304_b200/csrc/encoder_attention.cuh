@@ -1226,10 +1226,11 @@ static dgq_status ef_launch(const EncAttnArgs& a, cudaStream_t stream) {
   const int64_t columns = (int64_t)a.nq * (a.Hq / a.Hkv), blocks_z = (columns + Cfg::N - 1) / Cfg::N;
   // Blocks that share a head's keys: two to four rounds of the GPU while every warp keeps four steps, and at least one block an
   // SM while every warp has a step (64 requests of 300 to 8000 keys, 8 heads of 128: 147 us with one block a head,
-  // 131 with two, 136 with four, 169 with eight; longest first 108 with two; a block costs about 7 us beside its keys).
+  // 131 with two, 136 with four, 169 with eight; longest first 108 with two; a block costs about 7 us beside its keys).  Clusters of sixteen take long to start and have
+  // to be worth it (1 x 8 heads of 64 rows over 600 keys of 128: 31.7 us with sixteen, 17.5 with eight).
   const int64_t steps = ((int64_t)a.nk + Cfg::CH - 1) / Cfg::CH, base = a.B * (int64_t)a.Hkv * blocks_z;
   int splits = 1;
-  while (splits < EF_SPLITS && ((base * splits < 6 * sms && steps >= splits * 2 * Cfg::WARPS * 4) || (base * splits < sms && steps > splits * Cfg::WARPS)))
+  while (splits < EF_SPLITS && ((base * splits < 6 * sms && steps >= splits * 2 * Cfg::WARPS * 4) || (base * splits < sms && steps > splits * Cfg::WARPS && splits < 8)))
     splits *= 2;
   const int64_t blocks = base / blocks_z * splits;
   if (blocks > INT_MAX || blocks_z > 65535) return DGQ_ERR_UNSUPPORTED;
@@ -1656,6 +1657,21 @@ static dgq_status es_launch(const EncAttnArgs& a, cudaStream_t stream) {
 }
 
 // ------------------------------------------------------------------ launch
+// Whether a few tiles of query rows, which leave most SMs without work, take longer than the kernel that splits keys.  Fitted to 72
+// shapes of 8 to 128 key heads, 17 to 128 rows, 600 and 4000 keys (time in us): a block of 128 keys for a tile, sixteen keys for
+// thirty-two rows of one head over the whole GPU.  1 x 8 heads of 64 rows over 4000 keys of 64: 44 by tiles, 16 split; codes of
+// 128: 90 and 27; 8 x 16 heads: 46 and 115, 100 and 160.
+static bool ef_is_faster(const EncAttnArgs& a, bool cached, int sms) {
+  if (a.nq > 256) return false;
+  const int rows = cached && a.d <= 128 ? 2 * EA_Q : EA_Q, columns = a.d <= 128 ? 32 : 16;
+  const double blocks = (double)a.B * a.Hq * ((a.nq + rows - 1) / rows), places = sms * (cached || a.d > 128 ? 1.0 : 2.0);
+  const double block_us = cached ? 2.6 : a.d <= 64 ? 1.25 : a.d <= 128 ? 1.8 : 2.3;
+  const double tiles_us = std::ceil(blocks / places) * (6.0 + std::ceil((double)a.nk / EA_K) * block_us);
+  const double unit_us = 1e-3 * (cached ? (a.d <= 64 ? 1.1 : 2.1) : a.d <= 64 ? 1.5 : 3.6);
+  const double units = (double)a.B * a.Hkv * std::ceil((double)a.nq * (a.Hq / a.Hkv) / columns) * (a.nk / 16.0);
+  return 11.0 + 1.1 * units * unit_us < 0.9 * tiles_us;
+}
+
 template <bool BF, bool CACHED>
 static dgq_status enc_attn_launch(const EncAttnArgs& a, cudaStream_t stream) {
   if (a.nq <= 16) return ef_launch_size<BF, CACHED>(a, stream);
@@ -1664,6 +1680,9 @@ static dgq_status enc_attn_launch(const EncAttnArgs& a, cudaStream_t stream) {
   // Few keys: 8 x 16 of 4 heads of 4096 x 64 over 77 keys 48 us as one block of scores, 82 by blocks of 128; over 192 58 and 99.
   if (!a.causal && a.d <= 64 && a.nk <= EsCfg<1, CACHED>::KEYS) return es_launch<1, BF, CACHED>(t, stream);
   if (!a.causal && a.d > 64 && a.d <= 128 && a.nk <= EsCfg<2, CACHED>::KEYS) return es_launch<2, BF, CACHED>(t, stream);
+  int sms = 0;
+  DGQ_CUDA_OK(sm_count(&sms));
+  if (ef_is_faster(a, CACHED, sms)) return ef_launch_size<BF, CACHED>(a, stream);
   if (a.d <= 64) return ea_launch_tiles<1, BF, CACHED>(t, stream);
   if (a.d <= 128) return ea_launch_tiles<2, BF, CACHED>(t, stream);
   return ea_launch_tiles<3, BF, CACHED>(t, stream);
