@@ -240,11 +240,13 @@ enc_attn_tiles_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
     sh->abort_flag = 0;
     fence_barrier_init();
   }
+  // Tensor memory is taken once the kernel before has ended: a block that held it while it waits could keep a block of that one from
+  // its own.
+  pdl_wait();
   if (warp == Cfg::WARP_MMA) {
     tmem_alloc(&sh->tmem_base, Cfg::TMEM);
     tmem_relinquish();
   }
-  pdl_wait();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -1337,11 +1339,13 @@ enc_attn_short_kernel(const __grid_constant__ EaMaps maps, const __grid_constant
     sh->abort_flag = 0;
     fence_barrier_init();
   }
+  // Tensor memory is taken once the kernel before has ended: a block that held it while it waits could keep a block of that one from
+  // its own.
+  pdl_wait();
   if (warp == Cfg::WARP_MMA) {
     tmem_alloc(&sh->tmem_base, 256);
     tmem_relinquish();
   }
-  pdl_wait();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
