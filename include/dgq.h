@@ -269,13 +269,16 @@ dgq_status dgq_kv_plan(const int32_t* lens, const int32_t* n_new, int B, const i
                        int n_slots, int32_t* used, void* stream);
 
 /* Rows K[t], V[t] (t < T; [1, T, n_heads, d]) into slots[t] (dev int32 [T]; negative: the row is skipped).  The rows of one page
- * stand next to each other in ascending order, as dgq_kv_plan gives them, and no slot comes twice in a call.  For each page and
+ * stand next to each other in ascending order, as dgq_kv_plan gives them; there may be rows of the page between them that get
+ * nothing, and any number of skipped ones.  For each page and
  * head, in fp32: top = max |x| over the page's rows of this call, s = max(top * (1 / 127), 2^-126), 0 where top is 0; a page whose
  * row 0 is among them forgets what it held, any other one keeps its rows below the first new one: s = max(s, scale), and where s has
  * grown, their codes become rint((code * scale) / s).  New codes are rint(x / s), 0 where s is 0.  Each operation is rounded to
- * fp32, rint to the nearest whole number, ties to even.  Rows behind the
- * new ones stay as they are.  Inputs must be finite.  A slot beyond the cache is skipped and recorded as
- * DGQ_ERR_INVALID_ARG in the status word.
+ * fp32, rint to the nearest whole number, ties to even.  Rows behind the first
+ * new one that get nothing stay as they are.  Inputs must be finite.  A slot beyond the cache is skipped and recorded as
+ * DGQ_ERR_INVALID_ARG in the status word, as is one that is not above all of its page's before it.  Of a page whose rows stand in
+ * several places of a call, with another page's rows between them, or to which two calls write at the same time, the codes and scales
+ * are not defined afterwards.
  * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED, CUDA. */
 dgq_status dgq_kv_write(const dgq_kv_cache* cache, const dgq_rows* K, const dgq_rows* V, int dtype, int64_t T,
                         const int32_t* slots, void* stream);

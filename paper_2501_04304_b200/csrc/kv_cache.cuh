@@ -231,39 +231,213 @@ __device__ __forceinline__ float code_as_float(uint32_t biased_word, int i) {
   return __uint_as_float(__byte_perm(biased_word, 0x4B000000u, 0x7540 + i)) - 8388736.f;  // 2^23 + 128
 }
 
-// THREADS (one warp, or the block for large pages) take the runs of rows of one page that begin among `chunk` tokens, for one head's
-// keys and values at once: largest values, scales, codes.  Most runs fit the registers and are read once.  What bounds it is the
-// chain slots, rows, maximum, codes of a run, so keys and values go through it together and few tokens share a warp only where the
-// GPU is full without.  64 prompts of 20 to 77 rows of 20 x 64 into pages of 16 and out again: 43 us with a block per run, a division
-// per value and a second read; 18.2 with a warp for keys and one for values; 16.6 as it is (floor of both directions 6.1).
+// Largest magnitude of sixteen bytes of a row against `top`.
+template <bool BF>
+__device__ __forceinline__ uint32_t absmax_piece(uint32_t top, const uint4& y) {
+  return absmax16<BF>(absmax16<BF>(absmax16<BF>(absmax16<BF>(top, y.x), y.y), y.z), y.w);
+}
+// The same over THREADS threads, keys and values; all have then read what they needed of the page's old scales.
 template <bool BF, int THREADS>
-__global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(const __grid_constant__ KvWriteArgs a) {
+__device__ __forceinline__ void absmax_all(uint32_t (&top2)[2], uint32_t (*red)[WRITE_THREADS / 32]) {
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top2[w] = absmax16<BF>(top2[w], __shfl_xor_sync(0xFFFFFFFFu, top2[w], o));
+  if (THREADS > 32) {
+    if ((threadIdx.x & 31) == 0) {
+      red[0][threadIdx.x >> 5] = top2[0];
+      red[1][threadIdx.x >> 5] = top2[1];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < THREADS / 32; ++i) {
+      top2[0] = absmax16<BF>(top2[0], red[0][i]);
+      top2[1] = absmax16<BF>(top2[1], red[1][i]);
+    }
+  } else {
+    __syncwarp();
+  }
+}
+// A page's scale from its largest new magnitude and the one it has (0: none).
+template <bool BF>
+__device__ __forceinline__ float page_scale(uint32_t top2, float held) {
+  const float2 top = unpack16<BF>(top2);
+  // a scale below the smallest normal number would have no inverse
+  float s = fmaxf(top.x, top.y);
+  s = s > 0.f ? fmaxf(__fmul_rn(s, 1.0f / 127.0f), 1.17549435e-38f) : 0.f;
+  return fmaxf(s, held);
+}
+// The codes of a page's first rows from one scale to a larger one.
+template <int THREADS>
+__device__ __forceinline__ void round_old_codes(int8_t* page, int rows, int row_bytes, float held, float s) {
+#pragma unroll 1
+  for (int u = threadIdx.x % THREADS; u < rows * (row_bytes / 16); u += THREADS) {
+    uint4* p = reinterpret_cast<uint4*>(page) + u;
+    const uint4 y = *p;
+    uint32_t w4[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll 1
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = w4[i] ^ 0x80808080u;
+      w4[i] = codes_by_division(make_float4(__fmul_rn(code_as_float(x, 0), held), __fmul_rn(code_as_float(x, 1), held),
+                                            __fmul_rn(code_as_float(x, 2), held), __fmul_rn(code_as_float(x, 3), held)), s);
+    }
+    *p = make_uint4(w4[0], w4[1], w4[2], w4[3]);
+  }
+}
+// Eight codes; the last ones of a row with the zeros that fill it up.
+__device__ __forceinline__ void put_codes(int8_t* to, uint32_t lo, uint32_t hi, bool fill) {
+  *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
+  if (fill) *reinterpret_cast<uint2*>(to + 8) = make_uint2(0, 0);
+}
+template <bool BF>
+__device__ __forceinline__ void put_divided(int8_t* to, const uint4& y, float s, bool fill) {
+  const float2 f0 = unpack16<BF>(y.x), f1 = unpack16<BF>(y.y), f2 = unpack16<BF>(y.z), f3 = unpack16<BF>(y.w);
+  put_codes(to, codes_by_division(make_float4(f0.x, f0.y, f1.x, f1.y), s), codes_by_division(make_float4(f2.x, f2.y, f3.x, f3.y), s), fill);
+}
+
+// The tokens of a call seen from a run, which goes on to the next usable slot of another page.
+struct KvRun {
+  const KvWriteArgs& a;
+  int64_t t;  // its first token
+  int slot;
+  __device__ __forceinline__ bool usable(int s) const { return s >= 0 && s < a.n_pages << a.page_log2; }
+  // Slot s of token i + lane and which of the 32 are the run's; true: it ends among them.
+  __device__ __forceinline__ bool look(int64_t i, int& s, unsigned& in) const {
+    i += threadIdx.x & 31;
+    s = i < a.T ? a.slots[i] : INT_MIN;
+    const bool here = usable(s) && (s >> a.page_log2) == (slot >> a.page_log2);
+    const unsigned end = __ballot_sync(0xFFFFFFFFu, s == INT_MIN || (usable(s) && !here));
+    in = __ballot_sync(0xFFFFFFFFu, here) & (end ? (1u << (__ffs(end) - 1)) - 1u : 0xFFFFFFFFu);
+    return end != 0;
+  }
+  // Past tokens from i on that are skipped, 256 at a time.
+  __device__ __forceinline__ int64_t pass_skipped(int64_t i) const {
+    for (; i + 256 <= a.T; i += 256) {
+      bool any = false;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) any |= usable(a.slots[i + k * 32 + (threadIdx.x & 31)]);
+      if (__any_sync(0xFFFFFFFFu, any)) break;
+    }
+    return i;
+  }
+};
+
+// A run with rows left out or skipped tokens between its rows: first the token of every row of the page, then two passes over them.
+template <bool BF, int THREADS>
+__device__ __forceinline__ void kv_write_gaps(const KvWriteArgs& a, const KvRun& run, int h, long long* token_of, uint32_t (*red)[WRITE_THREADS / 32]) {
+  const int lane = threadIdx.x & 31, tid = threadIdx.x % THREADS;
+  const int row_bytes = kv_row_bytes(a.d), units = a.d / 8, r0 = run.slot & (a.page - 1);
+  const int step = THREADS / units, r_first = tid / units, c = tid - r_first * units;
+  const int64_t ph = (int64_t)(run.slot >> a.page_log2) * a.n_heads + h;
+  float held[2] = {0.f, 0.f};
+  if (r0 > 0) {
+    held[0] = a.scale[0][ph];
+    held[1] = a.scale[1][ph];
+  }
+  if (THREADS == 32 || threadIdx.x < 32) {
+    __syncwarp();
+    for (int r = lane; r < a.page; r += 32) token_of[r] = -1;
+    __syncwarp();
+    int top = -1;
+    for (int64_t i = run.t; top < a.page - 1;) {
+      int s;
+      unsigned in;
+      const bool end = run.look(i, s, in);
+      const int row = in >> lane & 1u ? s & (a.page - 1) : -1;
+      int most = row;  // of the lanes up to this one
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xFFFFFFFFu, most, o);
+        if (lane >= o) most = max(most, y);
+      }
+      const int before = __shfl_up_sync(0xFFFFFFFFu, most, 1);
+      if (row > (lane ? max(before, top) : top)) token_of[row] = i + lane;  // one that is not above all before it is skipped
+      top = max(top, __shfl_sync(0xFFFFFFFFu, most, 31));
+      if (end) break;
+      i += 32;
+      if (!in) i = run.pass_skipped(i);
+    }
+    __syncwarp();
+  }
+  if (THREADS > 32) __syncthreads();
+  const auto piece = [&](int w, long long token) {
+    return __ldg(reinterpret_cast<const uint4*>(a.x[w] + (int64_t)h * a.head[w] + c * 8 + token * a.token[w]));
+  };
+  uint32_t top2[2] = {0, 0};
+  if (r_first < step)
+#pragma unroll 1
+    for (int r = r0 + r_first; r < a.page; r += step) {
+      const long long token = token_of[r];
+      if (token < 0) continue;
+#pragma unroll
+      for (int w = 0; w < 2; ++w) top2[w] = absmax_piece<BF>(top2[w], piece(w, token));
+    }
+  absmax_all<BF, THREADS>(top2, red);
+#pragma unroll 1
+  for (int w = 0; w < 2; ++w) {
+    const float s = page_scale<BF>(top2[w], held[w]);
+    int8_t* page = a.codes[w] + (ph << a.page_log2) * row_bytes;
+    if (r0 > 0 && s > held[w]) round_old_codes<THREADS>(page, r0, row_bytes, held[w], s);
+    if (r_first < step)
+#pragma unroll 1
+      for (int r = r0 + r_first; r < a.page; r += step) {
+        const long long token = token_of[r];
+        if (token >= 0) put_divided<BF>(page + r * row_bytes + c * 8, piece(w, token), s > 0.f ? s : 1.f, c == units - 1 && (a.d & 8));
+      }
+    if (tid == 0) a.scale[w][ph] = s;
+  }
+}
+
+// THREADS (one warp, or the block for large pages) take the runs that begin among `chunk` tokens, for one head's keys and values at
+// once: largest values, scales, codes.  A run is all that a call brings for one page, whatever tokens are skipped and rows left out in
+// it: one scale has to come out of it, and the old codes are rounded to it once.  Most runs' rows follow one another, fit the registers
+// and are read once.  What bounds it is the chain slots, rows, maximum, codes of a run, so keys and values go through it together and
+// few tokens share a warp only where the GPU is full without.  64 prompts of 20 to 77 rows of 20 x 64 into pages of 16 and out again:
+// 43 us with a block per run, a division per value and a second read; 18.2 with a warp for keys and one for values; 16.6 with one
+// warp for both.  Looking for a run's end behind gaps costs 1.2 us of that case with changing inputs (19.6 -> 20.9; 256 single tokens
+// 19.5 -> 20.2).  Without the bound on registers the compiler takes 120 for runs with gaps and fewer blocks share an SM (22.2 us for the tokens).
+template <bool BF, int THREADS>
+__global__ void __launch_bounds__(WRITE_THREADS, 5) kv_write_kernel(const __grid_constant__ KvWriteArgs a) {
   __shared__ uint32_t red[2][WRITE_THREADS / 32];
+  __shared__ long long row_token[WRITE_THREADS];  // of a run with gaps: 32 rows for each warp (pages up to 32) or 128 for the block
   constexpr int GROUPS = WRITE_THREADS / THREADS;
   const int tid = threadIdx.x % THREADS, lane = threadIdx.x & 31;
   const int h = blockIdx.y;
   const int row_bytes = kv_row_bytes(a.d), units = a.d / 8;
-  const int n_slots = a.n_pages << a.page_log2;
+  KvRun run{a, 0, 0};
   pdl_launch_dependents();
   pdl_wait();
   const int64_t t0 = ((int64_t)blockIdx.x * GROUPS + threadIdx.x / THREADS) * a.chunk;
-  // which of the tokens begin a run: those whose predecessor is not the slot before, and those in row 0 of a page
+  // Which of the tokens begin a run: those whose page is not that of the nearest usable slot before them, however far back that is.
   unsigned begins;
   int mine = -1;
   {
     const int64_t t = t0 + lane;
-    bool first = false;
+    int64_t back = t0 - 32;
+    int before = back + lane >= 0 && back + lane < a.T ? a.slots[back + lane] : -1;
     if (lane < a.chunk && t < a.T) {
       mine = a.slots[t];
-      const int before = t > 0 ? a.slots[t - 1] : -1;
-      if (mine >= n_slots && h == 0) record_error(DGQ_ERR_INVALID_ARG);
-      first = mine >= 0 && mine < n_slots && ((mine & (a.page - 1)) == 0 || t == 0 || before != mine - 1);
+      if (mine >= 0 && !run.usable(mine) && h == 0) record_error(DGQ_ERR_INVALID_ARG);
     }
-    begins = __ballot_sync(0xFFFFFFFFu, first);
+    const unsigned real = __ballot_sync(0xFFFFFFFFu, run.usable(mine));
+    unsigned seen = __ballot_sync(0xFFFFFFFFu, run.usable(before));
+    while (real && !seen && back > 0) {
+      back -= 32;
+      before = back + lane >= 0 ? a.slots[back + lane] : -1;
+      seen = __ballot_sync(0xFFFFFFFFu, run.usable(before));
+    }
+    before = __shfl_sync(0xFFFFFFFFu, before, seen ? 31 - __clz(seen) : 0);
+    const unsigned lower = real & ((1u << lane) - 1u);
+    const int inside = __shfl_sync(0xFFFFFFFFu, mine, lower ? 31 - __clz(lower) : 0);
+    const int prev = lower ? inside : seen ? before : -1;
+    const bool same = run.usable(mine) && prev >= 0 && (prev >> a.page_log2) == (mine >> a.page_log2);
+    if (same && prev >= mine && h == 0) record_error(DGQ_ERR_INVALID_ARG);
+    begins = __ballot_sync(0xFFFFFFFFu, run.usable(mine) && !same);
   }
   // a thread has the same piece of rows tid / units, + step, ...
   const int step = THREADS / units, r_first = tid / units, c = tid - r_first * units;
-  const bool works = r_first < step;
+  const bool works = r_first < step, fill = c == units - 1 && (a.d & 8);
+  unsigned gapped = 0;  // runs with gaps, which come last
   for (; begins; begins &= begins - 1) {
     const int at = __ffs(begins) - 1;
     const int64_t t = t0 + at;
@@ -274,15 +448,30 @@ __global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(const __grid_co
       held[0] = a.scale[0][ph];
       held[1] = a.scale[1][ph];
     }
+    // n rows follow one another, row r0 + i being token t + i; `gaps`: there are more
+    run.t = t;
+    run.slot = slot;
     int n = 0;
-    for (const int most = a.page - r0; n < most; n += 32) {
-      const int i = n + lane;
-      const bool in = i < most && t + i < a.T && a.slots[t + i] == slot + i;
-      const unsigned ball = __ballot_sync(0xFFFFFFFFu, in);
-      if (ball != 0xFFFFFFFFu) {
-        n += __ffs(~ball) - 1;
-        break;
+    bool gaps = false;
+    for (int64_t i = t;;) {
+      int s;
+      unsigned in;
+      const bool end = run.look(i, s, in);
+      unsigned rest = in;
+      if (i - t == n) {
+        const unsigned direct = __ballot_sync(0xFFFFFFFFu, (unsigned)s - (unsigned)slot == (unsigned)(n + lane)) & in;
+        const int more = direct == 0xFFFFFFFFu ? 32 : __ffs(~direct) - 1;
+        n += more;
+        rest = more == 32 ? 0u : in >> more;
       }
+      gaps = rest != 0;
+      if (gaps || end || r0 + n == a.page) break;
+      i += 32;
+      if (!in) i = run.pass_skipped(i);
+    }
+    if (gaps) {
+      gapped |= 1u << at;
+      continue;
     }
     const uint16_t* rows[2];
     uint4 q[2][WRITE_HELD];
@@ -303,87 +492,49 @@ __global__ void __launch_bounds__(WRITE_THREADS) kv_write_kernel(const __grid_co
 #pragma unroll
       for (int k = 0; k < WRITE_HELD; ++k) {
         if (k * step >= n) break;
-        top2[w] = absmax16<BF>(absmax16<BF>(absmax16<BF>(absmax16<BF>(top2[w], q[w][k].x), q[w][k].y), q[w][k].z), q[w][k].w);
+        top2[w] = absmax_piece<BF>(top2[w], q[w][k]);
       }
     if (works)
 #pragma unroll 2
       for (int r = r_first + WRITE_HELD * step; r < n; r += step)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const uint4 y = __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w]));
-          top2[w] = absmax16<BF>(absmax16<BF>(absmax16<BF>(absmax16<BF>(top2[w], y.x), y.y), y.z), y.w);
-        }
-#pragma unroll
-    for (int w = 0; w < 2; ++w)
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top2[w] = absmax16<BF>(top2[w], __shfl_xor_sync(0xFFFFFFFFu, top2[w], o));
-    if (THREADS > 32) {
-      if (lane == 0) {
-        red[0][threadIdx.x >> 5] = top2[0];
-        red[1][threadIdx.x >> 5] = top2[1];
-      }
-      __syncthreads();  // also: everyone has read the old scales
-#pragma unroll
-      for (int i = 0; i < THREADS / 32; ++i) {
-        top2[0] = absmax16<BF>(top2[0], red[0][i]);
-        top2[1] = absmax16<BF>(top2[1], red[1][i]);
-      }
-    } else {
-      __syncwarp();
-    }
+        for (int w = 0; w < 2; ++w) top2[w] = absmax_piece<BF>(top2[w], __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w])));
+    absmax_all<BF, THREADS>(top2, red);
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      const float2 top = unpack16<BF>(top2[w]);
-      // a scale below the smallest normal number would have no inverse
-      float s = fmaxf(top.x, top.y);
-      s = s > 0.f ? fmaxf(__fmul_rn(s, 1.0f / 127.0f), 1.17549435e-38f) : 0.f;
-      s = fmaxf(s, held[w]);
+      const float s = page_scale<BF>(top2[w], held[w]);
       const float inv = s > 0.f ? __fdiv_rn(1.0f, s) : 0.f;
       int8_t* page = a.codes[w] + (ph << a.page_log2) * row_bytes;
-      if (r0 > 0 && s > held[w]) {
-        for (int u = tid; u < r0 * (row_bytes / 16); u += THREADS) {
-          uint4* p = reinterpret_cast<uint4*>(page) + u;
-          const uint4 y = *p;
-          uint32_t w4[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll 1
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t x = w4[i] ^ 0x80808080u;
-            w4[i] = codes_by_division(make_float4(__fmul_rn(code_as_float(x, 0), held[w]), __fmul_rn(code_as_float(x, 1), held[w]),
-                                                  __fmul_rn(code_as_float(x, 2), held[w]), __fmul_rn(code_as_float(x, 3), held[w])), s);
-          }
-          *p = make_uint4(w4[0], w4[1], w4[2], w4[3]);
-        }
-      }
+      if (r0 > 0 && s > held[w]) round_old_codes<THREADS>(page, r0, row_bytes, held[w], s);
       int8_t* dst = page + r0 * row_bytes + c * 8;
       float near = 0.f;
-      const auto put = [&](int r, uint32_t lo, uint32_t hi) {
-        int8_t* to = dst + r * row_bytes;
-        *reinterpret_cast<uint2*>(to) = make_uint2(lo, hi);
-        if (c == units - 1 && (a.d & 8)) *reinterpret_cast<uint2*>(to + 8) = make_uint2(0, 0);
-      };
       if (works) {
 #pragma unroll
         for (int k = 0; k < WRITE_HELD; ++k) {
           if (k * step >= n) break;
-          if (r_first + k * step < n) put(r_first + k * step, codes_of4<BF>(q[w][k].x, q[w][k].y, inv, near), codes_of4<BF>(q[w][k].z, q[w][k].w, inv, near));
+          if (r_first + k * step < n)
+            put_codes(dst + (r_first + k * step) * row_bytes, codes_of4<BF>(q[w][k].x, q[w][k].y, inv, near), codes_of4<BF>(q[w][k].z, q[w][k].w, inv, near), fill);
         }
 #pragma unroll 1
         for (int r = r_first + WRITE_HELD * step; r < n; r += step) {
           const uint4 y = __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w]));
-          put(r, codes_of4<BF>(y.x, y.y, inv, near), codes_of4<BF>(y.z, y.w, inv, near));
+          put_codes(dst + r * row_bytes, codes_of4<BF>(y.x, y.y, inv, near), codes_of4<BF>(y.z, y.w, inv, near), fill);
         }
         if (near > 0.49998f) {
 #pragma unroll 1
-          for (int r = r_first; r < n; r += step) {
-            const uint4 y = __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w]));
-            const float2 f0 = unpack16<BF>(y.x), f1 = unpack16<BF>(y.y), f2 = unpack16<BF>(y.z), f3 = unpack16<BF>(y.w);
-            put(r, codes_by_division(make_float4(f0.x, f0.y, f1.x, f1.y), s), codes_by_division(make_float4(f2.x, f2.y, f3.x, f3.y), s));
-          }
+          for (int r = r_first; r < n; r += step) put_divided<BF>(dst + r * row_bytes, __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w])), s, fill);
         }
       }
       if (tid == 0) a.scale[w][ph] = s;
     }
     if (THREADS > 32) __syncthreads();  // red is free again
+  }
+  for (; gapped; gapped &= gapped - 1) {
+    const int at = __ffs(gapped) - 1;
+    run.t = t0 + at;
+    run.slot = __shfl_sync(0xFFFFFFFFu, mine, at);
+    kv_write_gaps<BF, THREADS>(a, run, h, row_token + threadIdx.x / THREADS * (WRITE_THREADS / GROUPS), red);
+    if (THREADS > 32) __syncthreads();
   }
 }
 
