@@ -50,9 +50,14 @@ PyObject* wrap(const at::Tensor& t) {
   return THPVariable_Wrap(t);
 }
 
+// An integer argument; one that 32 bits do not hold is refused, not cut.
 bool integer(PyObject* o, int* v) {
   const long x = PyLong_AsLong(o);
   if (x == -1 && PyErr_Occurred()) return false;
+  if (x < INT32_MIN || x > INT32_MAX) {
+    PyErr_SetString(PyExc_ValueError, "an integer argument does not fit 32 bits");
+    return false;
+  }
   *v = static_cast<int>(x);
   return true;
 }
