@@ -261,8 +261,8 @@ typedef struct {
  * packed batch), kv_lens[B] = lens + n_new, slots[n_slots] (the slot of every new token in that order; -1 behind the last
  * one) and used[1] = free pages taken.
  * What does not fit is found on the device, which records DGQ_ERR_INVALID_ARG in the status word: negative lengths count
- * as 0, lengths beyond max_pages * page as that, a page that free_pages has no more entry for becomes -1, as do the slots of the
- * tokens concerned and of those beyond n_slots or the table.
+ * as 0, lengths beyond max_pages * page as that, a page that free_pages has no more entry for becomes -1, as do the slots of its
+ * tokens, of tokens on a page that is negative or whose slots do not fit 31 bits, and of those beyond n_slots or the table.
  * The outputs may not overlap lens and n_new.  Errors: INVALID_ARG, UNSUPPORTED (page), CUDA. */
 dgq_status dgq_kv_plan(const int32_t* lens, const int32_t* n_new, int B, const int32_t* free_pages, int n_free,
                        int32_t* block_table, int max_pages, int page, int32_t* token_start, int32_t* kv_lens, int32_t* slots,

@@ -144,23 +144,29 @@ __global__ void __launch_bounds__(PLAN_WARPS * 32) kv_plan_kernel(const KvPlanAr
       a.token_start[b] = (int32_t)min(start, (long long)INT_MAX);
       a.kv_lens[b] = len + add;
     }
+    // a page whose slots 31 bits hold: a larger number's would be those of another page
+    const auto page_ok = [&](int p) { return p >= 0 && p <= INT_MAX >> a.page_log2; };
     // the page of the tokens that the request has already begun
     int first = -1;
     if (have > 0 && (len & (a.page - 1))) {
       first = row[have - 1];
-      if (first < 0) bad = true;
+      bad |= !page_ok(first);
     }
     const auto new_page = [&](int i) {
       const long long at = taken + i;
       return at < a.n_free ? a.free_pages[at] : -1;
     };
-    for (int i = lane; i < need - have; i += 32) row[have + i] = new_page(i);
+    for (int i = lane; i < need - have; i += 32) {
+      const int p = new_page(i);
+      bad |= !page_ok(p);
+      row[have + i] = p;
+    }
     for (int i = lane; i < add; i += 32) {
       const long long t = start + i;
       if (t >= a.n_slots) break;
       const int pos = len + i, pi = pos >> a.page_log2;
       const int page = pi < have ? first : new_page(pi - have);
-      a.slots[t] = page < 0 ? -1 : (page << a.page_log2) + (pos & (a.page - 1));
+      a.slots[t] = !page_ok(page) ? -1 : (page << a.page_log2) + (pos & (a.page - 1));
     }
   }
   for (long long t = min(total, (long long)a.n_slots) + blockIdx.x * (PLAN_WARPS * 32) + threadIdx.x; t < a.n_slots;
