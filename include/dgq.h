@@ -275,8 +275,9 @@ dgq_status dgq_kv_plan(const int32_t* lens, const int32_t* n_new, int B, const i
  * row 0 is among them forgets what it held, any other one keeps its rows below the first new one: s = max(s, scale), and where s has
  * grown, their codes become rint((code * scale) / s).  New codes are rint(x / s), 0 where s is 0.  Each operation is rounded to
  * fp32, rint to the nearest whole number, ties to even.  Rows behind the first
- * new one that get nothing stay as they are.  Inputs must be finite.  A slot beyond the cache is skipped and recorded as
- * DGQ_ERR_INVALID_ARG in the status word, as is one that is not above all of its page's before it.  Of a page whose rows stand in
+ * new one that get nothing stay as they are.  A value that is not finite counts as 0 and is recorded as DGQ_ERR_INVALID_ARG in the
+ * status word; rows that are skipped may hold anything.  A slot beyond the cache is skipped and recorded too, as is one that is not
+ * above all of its page's before it.  Of a page whose rows stand in
  * several places of a call, with another page's rows between them, or to which two calls write at the same time, the codes and scales
  * are not defined afterwards.
  * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED, CUDA. */

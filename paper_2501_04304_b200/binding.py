@@ -343,7 +343,7 @@ def kv_plan(lens, n_new, free_pages, block_table, page, n_tokens, stream=None):
 
 def kv_write(cache: KvCache, K, V, slots, stream=None):
     """dgq_kv_write: rows K, V [T, heads, d] (fp16 or bf16) into the cache's slots [T] (int32), as kv_plan lays them out: the rows of a
-    page next to each other, their slots ascending; rows with negative slots are skipped."""
+    page next to each other, their slots ascending; rows with negative slots are skipped, values that are not finite count as 0."""
     r = (_native or native()).kv_write(cache.k, cache.v, cache.k_scale, cache.v_scale, cache.d, K, V, slots, stream)
     if type(r) is int:
         _check(r, "dgq_kv_write")

@@ -193,16 +193,24 @@ struct KvWriteArgs {
 constexpr int WRITE_THREADS = 128;
 constexpr int WRITE_HELD = 4;  // sixteen-byte pieces of a thread that stay in registers between the two passes
 
-// Largest magnitude of two 16-bit numbers against `top`, in the type itself (exact).
+// Largest magnitude of two 16-bit numbers against `top`, in the type itself (exact); NaN stays NaN.
 template <bool BF>
 __device__ __forceinline__ uint32_t absmax16(uint32_t top, uint32_t x) {
   x &= 0x7FFF7FFFu;
   if (BF) {
-    const __nv_bfloat162 r = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&top), *reinterpret_cast<const __nv_bfloat162*>(&x));
+    const __nv_bfloat162 r = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&top), *reinterpret_cast<const __nv_bfloat162*>(&x));
     return *reinterpret_cast<const uint32_t*>(&r);
   }
-  const __half2 r = __hmax2(*reinterpret_cast<const __half2*>(&top), *reinterpret_cast<const __half2*>(&x));
+  const __half2 r = __hmax2_nan(*reinterpret_cast<const __half2*>(&top), *reinterpret_cast<const __half2*>(&x));
   return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Two 16-bit numbers with 0 for those that are not finite: all bits of their exponent are set.
+template <bool BF>
+__device__ __forceinline__ uint32_t finite16(uint32_t x) {
+  constexpr uint32_t E = BF ? 0x7F80u : 0x7C00u;
+  if ((x & E) == E) x &= 0xFFFF0000u;
+  if ((x >> 16 & E) == E) x &= 0x0000FFFFu;
+  return x;
 }
 // Codes of four 16-bit numbers: rint(x / s), the quotient rounded to fp32.  x * inv is within 127 * 2^-23 of it, so the two round to the
 // same whole number unless a border of two codes is that near; `near` then tells that these (a few in 10^5, half the largest value
@@ -328,7 +336,8 @@ struct KvRun {
   }
 };
 
-// A run with rows left out or skipped tokens between its rows: first the token of every row of the page, then two passes over them.
+// A run with rows left out or skipped tokens between its rows, or with values that are not finite, which count as 0: first the token of
+// every row of the page, then two passes over them.
 template <bool BF, int THREADS>
 __device__ __forceinline__ void kv_write_gaps(const KvWriteArgs& a, const KvRun& run, int h, long long* token_of, uint32_t (*red)[WRITE_THREADS / 32]) {
   const int lane = threadIdx.x & 31, tid = threadIdx.x % THREADS;
@@ -366,8 +375,12 @@ __device__ __forceinline__ void kv_write_gaps(const KvWriteArgs& a, const KvRun&
     __syncwarp();
   }
   if (THREADS > 32) __syncthreads();
+  bool odd = false;
   const auto piece = [&](int w, long long token) {
-    return __ldg(reinterpret_cast<const uint4*>(a.x[w] + (int64_t)h * a.head[w] + c * 8 + token * a.token[w]));
+    const uint4 y = __ldg(reinterpret_cast<const uint4*>(a.x[w] + (int64_t)h * a.head[w] + c * 8 + token * a.token[w]));
+    const uint4 f = make_uint4(finite16<BF>(y.x), finite16<BF>(y.y), finite16<BF>(y.z), finite16<BF>(y.w));
+    odd |= f.x != y.x || f.y != y.y || f.z != y.z || f.w != y.w;
+    return f;
   };
   uint32_t top2[2] = {0, 0};
   if (r_first < step)
@@ -378,6 +391,7 @@ __device__ __forceinline__ void kv_write_gaps(const KvWriteArgs& a, const KvRun&
 #pragma unroll
       for (int w = 0; w < 2; ++w) top2[w] = absmax_piece<BF>(top2[w], piece(w, token));
     }
+  if (odd) record_error(DGQ_ERR_INVALID_ARG);
   absmax_all<BF, THREADS>(top2, red);
 #pragma unroll 1
   for (int w = 0; w < 2; ++w) {
@@ -400,8 +414,8 @@ __device__ __forceinline__ void kv_write_gaps(const KvWriteArgs& a, const KvRun&
 // and are read once.  What bounds it is the chain slots, rows, maximum, codes of a run, so keys and values go through it together and
 // few tokens share a warp only where the GPU is full without.  64 prompts of 20 to 77 rows of 20 x 64 into pages of 16 and out again:
 // 43 us with a block per run, a division per value and a second read; 18.2 with a warp for keys and one for values; 16.6 with one
-// warp for both.  Looking for a run's end behind gaps costs 1.2 us of that case with changing inputs (19.6 -> 20.9; 256 single tokens
-// 19.5 -> 20.2).  Without the bound on registers the compiler takes 120 for runs with gaps and fewer blocks share an SM (22.2 us for the tokens).
+// warp for both.  Looking for a run's end behind gaps and for values that are not finite costs 1.5 us of that case with changing inputs
+// (19.6 -> 21.1; 256 single tokens 19.5 -> 20.6).  Without the bound on registers the compiler takes 120 for runs with gaps and fewer blocks share an SM (22.2 us for the tokens).
 template <bool BF, int THREADS>
 __global__ void __launch_bounds__(WRITE_THREADS, 5) kv_write_kernel(const __grid_constant__ KvWriteArgs a) {
   __shared__ uint32_t red[2][WRITE_THREADS / 32];
@@ -443,7 +457,7 @@ __global__ void __launch_bounds__(WRITE_THREADS, 5) kv_write_kernel(const __grid
   // a thread has the same piece of rows tid / units, + step, ...
   const int step = THREADS / units, r_first = tid / units, c = tid - r_first * units;
   const bool works = r_first < step, fill = c == units - 1 && (a.d & 8);
-  unsigned gapped = 0;  // runs with gaps, which come last
+  unsigned gapped = 0;  // runs with gaps or values that are not finite, which come last
   for (; begins; begins &= begins - 1) {
     const int at = __ffs(begins) - 1;
     const int64_t t = t0 + at;
@@ -506,6 +520,11 @@ __global__ void __launch_bounds__(WRITE_THREADS, 5) kv_write_kernel(const __grid
 #pragma unroll
         for (int w = 0; w < 2; ++w) top2[w] = absmax_piece<BF>(top2[w], __ldg(reinterpret_cast<const uint4*>(rows[w] + r * a.token[w])));
     absmax_all<BF, THREADS>(top2, red);
+    if (finite16<BF>(top2[0]) != top2[0] || finite16<BF>(top2[1]) != top2[1]) {
+      gapped |= 1u << at;
+      if (THREADS > 32) __syncthreads();  // red is free again
+      continue;
+    }
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
       const float s = page_scale<BF>(top2[w], held[w]);

@@ -71,3 +71,43 @@ def test_rows_with_gaps(heads, d, page, slots, dtype):
     assert torch.equal(c.k.cpu(), want[0][0]) and torch.equal(c.k_scale.cpu(), want[0][1])
     assert torch.equal(c.v.cpu(), want[1][0]) and torch.equal(c.v_scale.cpu(), want[1][1])
     assert b.device_status() == int(recorded)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("d,page,slots", [
+    (64, 16, list(range(16, 60))), (40, 32, list(range(5, 90))), (128, 64, [70, 71, 128, 200]), (160, 128, list(range(1, 128)) + list(range(256, 300))),
+    (64, 16, [33, 35, 36, 48, 50]), (64, 128, list(range(7, 120, 2))),
+], ids=lambda x: None if isinstance(x, list) else str(x))
+def test_values_that_are_not_finite(d, page, slots, dtype):
+    """Such a value counts as 0 and is recorded; other rows, pages and heads are as without it."""
+    _, b = gpu()
+    g = torch.Generator().manual_seed(2)
+    k, v = (torch.randn(len(slots), 3, d, generator=g).to(dtype) for _ in range(2))
+    clean = [k.clone(), v.clone()]
+    for x, z, places in ((k, clean[0], [(1, 0, 0, "nan"), (3, 0, d - 1, "inf")]), (v, clean[1], [(2, 1, 5, "-inf"), (0, 1, 1, "-nan")])):
+        for t, h, i, value in places:
+            x[t, h, i], z[t, h, i] = float(value), 0.0
+    v[:, 2], clean[1][:, 2] = float("nan"), 0.0  # a head without a finite value
+    c = random_cache(b, 40, 3, page, d, seed=d)
+    want = [quantize_reference(x, slots, codes.cpu(), scale.cpu(), page) for x, codes, scale in zip(clean, (c.k, c.v), (c.k_scale, c.v_scale))]
+    b.kv_write(c, k.cuda(), v.cuda(), dev(slots))
+    assert b.device_status() == 1
+    assert torch.equal(c.k.cpu(), want[0][0]) and torch.equal(c.k_scale.cpu(), want[0][1])
+    assert torch.equal(c.v.cpu(), want[1][0]) and torch.equal(c.v_scale.cpu(), want[1][1])
+
+
+@pytest.mark.parametrize("page", [16, 128])
+def test_skipped_rows_hold_anything(page):
+    _, b = gpu()
+    slots = [16, 17, -1, 19, -2, 40 * page, page * 3 - 1]
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn(len(slots), 2, 64, generator=g).half()
+    x[[2, 4, 5]] = torch.tensor([float("nan"), float("inf"), float("-inf")]).half()[:, None, None]
+    c = random_cache(b, 40, 2, page, 64, seed=4)
+    want = quantize_reference(x, [s if s < 40 * page else -1 for s in slots], c.k.cpu(), c.k_scale.cpu(), page)
+    b.kv_write(c, x[:5].cuda(), x[:5].cuda(), dev(slots[:5]))
+    assert b.device_status() == 0
+    c = random_cache(b, 40, 2, page, 64, seed=4)
+    b.kv_write(c, x.cuda(), x.cuda(), dev(slots))
+    assert b.device_status() == 1  # the slot beyond the cache
+    assert torch.equal(c.k.cpu(), want[0]) and torch.equal(c.k_scale.cpu(), want[1])
