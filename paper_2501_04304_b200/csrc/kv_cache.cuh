@@ -88,8 +88,8 @@ __device__ __forceinline__ void plan_lengths(const KvPlanArgs& a, int b, int& le
 
 // A warp has one request, a block eight in a row.  Every block adds up the tokens and pages of all requests before its own by
 // itself (at most a few reads a thread, from L2), so that one launch does it all; the totals it gets on the way say where the
-// unused end of the slot map begins.  The largest case writes 1.8 MB; what bounds it is the launch and two dependent
-// rounds of loads.
+// unused end of the slot map begins.  That reads B * B / 8 lengths in all: 2048 requests, which write 1.25 MB, are bound by the launch
+// and two dependent rounds of loads.
 __global__ void __launch_bounds__(PLAN_WARPS * 32) kv_plan_kernel(const KvPlanArgs a) {
   __shared__ long long part[PLAN_WARPS][4];
   __shared__ long long own[PLAN_WARPS][2];
@@ -287,15 +287,14 @@ __device__ __forceinline__ void round_old_codes(int8_t* page, int rows, int row_
 #pragma unroll 1
   for (int u = threadIdx.x % THREADS; u < rows * (row_bytes / 16); u += THREADS) {
     uint4* p = reinterpret_cast<uint4*>(page) + u;
-    const uint4 y = *p;
-    uint32_t w4[4] = {y.x, y.y, y.z, y.w};
+    uint4 y = *p;
 #pragma unroll 1
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t x = w4[i] ^ 0x80808080u;
-      w4[i] = codes_by_division(make_float4(__fmul_rn(code_as_float(x, 0), held), __fmul_rn(code_as_float(x, 1), held),
-                                            __fmul_rn(code_as_float(x, 2), held), __fmul_rn(code_as_float(x, 3), held)), s);
+    for (int i = 0; i < 4; ++i) {  // the words move up: four divisions of code instead of sixteen
+      const uint32_t x = y.x ^ 0x80808080u;
+      y = make_uint4(y.y, y.z, y.w, codes_by_division(make_float4(__fmul_rn(code_as_float(x, 0), held), __fmul_rn(code_as_float(x, 1), held),
+                                                                  __fmul_rn(code_as_float(x, 2), held), __fmul_rn(code_as_float(x, 3), held)), s));
     }
-    *p = make_uint4(w4[0], w4[1], w4[2], w4[3]);
+    *p = y;
   }
 }
 // Eight codes; the last ones of a row with the zeros that fill it up.
@@ -318,21 +317,57 @@ struct KvRun {
   // Slot s of token i + lane and which of the 32 are the run's; true: it ends among them.
   __device__ __forceinline__ bool look(int64_t i, int& s, unsigned& in) const {
     i += threadIdx.x & 31;
-    s = i < a.T ? a.slots[i] : INT_MIN;
+    s = i < a.T ? a.slots[i] : -1;
     const bool here = usable(s) && (s >> a.page_log2) == (slot >> a.page_log2);
-    const unsigned end = __ballot_sync(0xFFFFFFFFu, s == INT_MIN || (usable(s) && !here));
+    const unsigned end = __ballot_sync(0xFFFFFFFFu, i >= a.T || (usable(s) && !here));
     in = __ballot_sync(0xFFFFFFFFu, here) & (end ? (1u << (__ffs(end) - 1)) - 1u : 0xFFFFFFFFu);
     return end != 0;
   }
-  // Past tokens from i on that are skipped, 256 at a time.
-  __device__ __forceinline__ int64_t pass_skipped(int64_t i) const {
-    for (; i + 256 <= a.T; i += 256) {
-      bool any = false;
+  // The first token from i on whose slot is usable, T if none is left.  Stretches of skipped tokens may be long (the end of a slot map with
+  // room for more): 1024 at a time where that many are left, all loads in front of the first use.
+  __device__ __forceinline__ int64_t next_usable(int64_t i) const {
+    const int lane = threadIdx.x & 31;
+    for (bool first = true; i < a.T; first = false) {
+      const bool wide = !first && i + 1024 <= a.T;
+      unsigned at = 1024;
+      if (wide) {
+        // from a sixteen-byte boundary, at most three tokens back, which are skipped ones
+        i -= (int64_t)(((reinterpret_cast<uintptr_t>(a.slots) >> 2) + (uint64_t)i) & 3);
+        int4 s[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) any |= usable(a.slots[i + k * 32 + (threadIdx.x & 31)]);
-      if (__any_sync(0xFFFFFFFFu, any)) break;
+        for (int k = 0; k < 8; ++k) s[k] = reinterpret_cast<const int4*>(a.slots + i)[k * 32 + lane];
+#pragma unroll
+        for (int k = 7; k >= 0; --k) {
+          const unsigned j = k * 128 + lane * 4;
+          at = usable(s[k].x) ? j : usable(s[k].y) ? j + 1 : usable(s[k].z) ? j + 2 : usable(s[k].w) ? j + 3 : at;
+        }
+      } else {
+        int s[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k] = i + k * 32 + lane < a.T ? a.slots[i + k * 32 + lane] : -1;
+#pragma unroll
+        for (int k = 7; k >= 0; --k) at = usable(s[k]) ? k * 32 + lane : at;
+      }
+      at = __reduce_min_sync(0xFFFFFFFFu, at);
+      if (at < 1024) return i + at;
+      i += wide ? 1024 : 256;
     }
-    return i;
+    return a.T;
+  }
+  // The last usable slot of the tokens in front of i, -1 if there is none.
+  __device__ __forceinline__ int last_before(int64_t i) const {
+    const int lane = threadIdx.x & 31;
+    for (; i > 0; i -= 256) {
+      int s[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s[k] = i > k * 32 + lane ? a.slots[i - 1 - k * 32 - lane] : -1;
+      unsigned back = 256;
+#pragma unroll
+      for (int k = 7; k >= 0; --k) back = usable(s[k]) ? k * 32 + lane : back;
+      back = __reduce_min_sync(0xFFFFFFFFu, back);
+      if (back < 256) return a.slots[i - 1 - back];
+    }
+    return -1;
   }
 };
 
@@ -370,7 +405,7 @@ __device__ __forceinline__ void kv_write_gaps(const KvWriteArgs& a, const KvRun&
       top = max(top, __shfl_sync(0xFFFFFFFFu, most, 31));
       if (end) break;
       i += 32;
-      if (!in) i = run.pass_skipped(i);
+      if (!in) i = run.next_usable(i);
     }
     __syncwarp();
   }
@@ -415,7 +450,7 @@ __device__ __forceinline__ void kv_write_gaps(const KvWriteArgs& a, const KvRun&
 // few tokens share a warp only where the GPU is full without.  64 prompts of 20 to 77 rows of 20 x 64 into pages of 16 and out again:
 // 43 us with a block per run, a division per value and a second read; 18.2 with a warp for keys and one for values; 16.6 with one
 // warp for both.  Looking for a run's end behind gaps and for values that are not finite costs 1.5 us of that case with changing inputs
-// (19.6 -> 21.1; 256 single tokens 19.5 -> 20.6).  Without the bound on registers the compiler takes 120 for runs with gaps and fewer blocks share an SM (22.2 us for the tokens).
+// (19.6 -> 21.1; 256 single tokens 19.5 -> 20.7), a slot map with room for 64, 960 and 8128 more tokens 0.2, 0.8 and 8 us.  Without the bound on registers the compiler takes 120 for runs with gaps and fewer blocks share an SM (22.2 us for the tokens).
 template <bool BF, int THREADS>
 __global__ void __launch_bounds__(WRITE_THREADS, 5) kv_write_kernel(const __grid_constant__ KvWriteArgs a) {
   __shared__ uint32_t red[2][WRITE_THREADS / 32];
@@ -433,23 +468,19 @@ __global__ void __launch_bounds__(WRITE_THREADS, 5) kv_write_kernel(const __grid
   int mine = -1;
   {
     const int64_t t = t0 + lane;
-    int64_t back = t0 - 32;
-    int before = back + lane >= 0 && back + lane < a.T ? a.slots[back + lane] : -1;
+    const int64_t back = t0 - 32 + lane;
+    int before = back >= 0 && back < a.T ? a.slots[back] : -1;
     if (lane < a.chunk && t < a.T) {
       mine = a.slots[t];
       if (mine >= 0 && !run.usable(mine) && h == 0) record_error(DGQ_ERR_INVALID_ARG);
     }
-    const unsigned real = __ballot_sync(0xFFFFFFFFu, run.usable(mine));
-    unsigned seen = __ballot_sync(0xFFFFFFFFu, run.usable(before));
-    while (real && !seen && back > 0) {
-      back -= 32;
-      before = back + lane >= 0 ? a.slots[back + lane] : -1;
-      seen = __ballot_sync(0xFFFFFFFFu, run.usable(before));
-    }
-    before = __shfl_sync(0xFFFFFFFFu, before, seen ? 31 - __clz(seen) : 0);
+    const unsigned real = __ballot_sync(0xFFFFFFFFu, run.usable(mine)), seen = __ballot_sync(0xFFFFFFFFu, run.usable(before));
+    if (!real) return;
+    if (seen) before = __shfl_sync(0xFFFFFFFFu, before, 31 - __clz(seen));
+    else before = run.last_before(t0 - 32);
     const unsigned lower = real & ((1u << lane) - 1u);
     const int inside = __shfl_sync(0xFFFFFFFFu, mine, lower ? 31 - __clz(lower) : 0);
-    const int prev = lower ? inside : seen ? before : -1;
+    const int prev = lower ? inside : before;
     const bool same = run.usable(mine) && prev >= 0 && (prev >> a.page_log2) == (mine >> a.page_log2);
     if (same && prev >= mine && h == 0) record_error(DGQ_ERR_INVALID_ARG);
     begins = __ballot_sync(0xFFFFFFFFu, run.usable(mine) && !same);
@@ -487,7 +518,8 @@ __global__ void __launch_bounds__(WRITE_THREADS, 5) kv_write_kernel(const __grid
       gaps = rest != 0;
       if (gaps || end || r0 + n == a.page) break;
       i += 32;
-      if (!in) i = run.pass_skipped(i);
+      if (i - t != n) i = run.next_usable(i);  // the rows that follow one another have ended
+      if (i >= a.T) break;
     }
     if (gaps) {
       gapped |= 1u << at;

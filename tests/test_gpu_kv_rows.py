@@ -38,6 +38,8 @@ GAPS = [
     (2, 8, 16, [0, 2, 4, 33, 47]),
     # a page of zeros' rows between, more skipped tokens than a warp looks at in one read, in the run and behind it
     (2, 128, 16, [3] + [-1] * 300 + [9] + [-3] * 1000 + [64, 65] + [-1] * 700),
+    (1, 40, 16, [-1, 3, -2 ** 31, 4, 5] + [-2 ** 31] * 2500 + [7] + [-1] * 1024 + [48, 50] + [-1] * 5001),
+    (1, 64, 64, [70] + [-1] * 1087 + [71] + [-1] * 4096 + [73, 74] + [-1] * 127 + [75] + [-1] * 300),
     (2, 64, 32, [-1] * 1500 + [40] + [-1] * 31 + [41, 43] + [-1] * 600 + [64]),
     (1, 160, 32, every(2, 33, 128)),
     (5, 104, 16, every(3, 1, 600)),
@@ -67,10 +69,14 @@ def test_rows_with_gaps(heads, d, page, slots, dtype):
     v[:, 0] = 0  # one head's pages keep their scale, or get none
     real, recorded = accepted(slots, page, pages * page)
     want = [quantize_reference(x, real, codes.cpu(), scale.cpu(), page) for x, codes, scale in ((k, c.k, c.k_scale), (v, c.v, c.v_scale))]
-    b.kv_write(c, k.cuda(), v.cuda(), dev(slots))
-    assert torch.equal(c.k.cpu(), want[0][0]) and torch.equal(c.k_scale.cpu(), want[0][1])
-    assert torch.equal(c.v.cpu(), want[1][0]) and torch.equal(c.v_scale.cpu(), want[1][1])
-    assert b.device_status() == int(recorded)
+    before = [x.clone() for x in (c.k, c.v, c.k_scale, c.v_scale)]
+    for offset in range(4 if -1 in slots else 1):  # a slot map may begin at any multiple of four bytes
+        for x, y in zip((c.k, c.v, c.k_scale, c.v_scale), before):
+            x.copy_(y)
+        b.kv_write(c, k.cuda(), v.cuda(), dev([5] * offset + slots)[offset:])
+        assert torch.equal(c.k.cpu(), want[0][0]) and torch.equal(c.k_scale.cpu(), want[0][1])
+        assert torch.equal(c.v.cpu(), want[1][0]) and torch.equal(c.v_scale.cpu(), want[1][1])
+        assert b.device_status() == int(recorded)
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
