@@ -263,7 +263,8 @@ typedef struct {
  * What does not fit is found on the device, which records DGQ_ERR_INVALID_ARG in the status word: negative lengths count
  * as 0, lengths beyond max_pages * page as that, a page that free_pages has no more entry for becomes -1, as do the slots of its
  * tokens, of tokens on a page that is negative or whose slots do not fit 31 bits, and of those beyond n_slots or the table.
- * The outputs may not overlap lens and n_new.  Errors: INVALID_ARG, UNSUPPORTED (page), CUDA. */
+ * The outputs may not overlap lens and n_new.  B is at least 1; each eight requests read all lengths, which is meant for thousands of
+ * requests, not for millions.  Errors: INVALID_ARG, UNSUPPORTED (page), CUDA. */
 dgq_status dgq_kv_plan(const int32_t* lens, const int32_t* n_new, int B, const int32_t* free_pages, int n_free,
                        int32_t* block_table, int max_pages, int page, int32_t* token_start, int32_t* kv_lens, int32_t* slots,
                        int n_slots, int32_t* used, void* stream);
@@ -295,7 +296,9 @@ dgq_status dgq_kv_read(const dgq_kv_cache* cache, const int32_t* slots, int64_t 
  * q_start NULL: Q, O [B, max_nq, Hq, d].  Else Q, O [1, n_rows, Hq, d] packed: request b has rows q_start[b] .. q_start[b + 1] - 1
  * (dev int32 [B + 1], ascending), at most max_nq of them; other rows of O stay as they are.  causal != 0: row i of n sees the first
  * kv_lens[b] - n + i + 1 tokens (the n queries belong to the last n tokens).  Hq a multiple of cache->n_heads.  Pages may be
- * shared by requests.  max_pages * page, max_nq and n_rows are at most 2^30.  Weights are rounded to fp16 for the product with the codes, whatever `dtype` is.
+ * shared by requests.  max_pages * page, max_nq and n_rows are at most 2^30.  Weights are rounded to fp16 for the product with the codes,
+ * whatever `dtype` is.  The value scales of the pages that a row sees are within 2^80 of one another (a page of zeros counts as one of
+ * 2^-40, scales below 2^-100 as 2^-100); a weight on a page of far smaller values than that would be lost from the row's sum.
  * Found on the device and recorded as DGQ_ERR_INVALID_ARG in the status word: table entries outside the cache (their tokens
  * count as absent), more than max_nq rows or rows beyond n_rows (left out).  n_rows is ignored where q_start is NULL.
  * Errors: INVALID_ARG, ALIGNMENT, UNSUPPORTED, CUDA. */

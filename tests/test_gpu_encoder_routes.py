@@ -180,3 +180,19 @@ def test_codes_within_the_roundings(H, G, d, page, lens, rows, dtype):
     O = b.cached_attn(q, c, dev(table), dev(lens), q_start=dev(starts), max_nq=max(rows))
     assert b.device_status() == 0
     check_cached(O, q, c, table, lens, starts, False)
+
+
+@pytest.mark.parametrize("nq,n", [(1, 300), (1, 40), (150, 90), (300, 300)])
+def test_value_scales_far_apart(nq, n):
+    """Pages of values 2^78 and more from one another, and pages of zeros: the row's sum has the weights of all of them.  Every row sees
+    the zeros' keys about as much as the others', so that a weight that is lost from the sum shows."""
+    _, b = gpu()
+    c, table, q, starts = cached_case(b, 1, 2, 2, 64, 16, [n], [nq], BF16, seed=11)
+    pages = torch.as_tensor(table[0, :-(-n // 16)]).cuda()
+    c.k_scale.mul_(0.02)
+    scales = torch.tensor([2.0 ** -40, 2.0 ** 38, 0.0, 2.0 ** 38]).cuda()
+    c.v_scale[pages] = scales[torch.arange(len(pages), device="cuda") % 4][:, None]
+    c.v[pages[2::4]] = 0
+    O = b.cached_attn(q, c, dev(table), dev([n]), q_start=dev(starts), max_nq=nq)
+    assert b.device_status() == 0
+    check_cached(O, q, c, table, [n], starts, False)
