@@ -333,7 +333,7 @@ class KvCache:
 
 def kv_plan(lens, n_new, free_pages, block_table, page, n_tokens, stream=None):
     """dgq_kv_plan: enters the pages that the new tokens need into `block_table` (int32 [B, max_pages], in place), taken from the front
-    of `free_pages`.  Returns (token_start [B + 1], kv_lens [B], slots [n_tokens], used [1]), all int32 on the GPU; slots
+    of `free_pages`.  B and max_pages are at least 1.  Returns (token_start [B + 1], kv_lens [B], slots [n_tokens], used [1]), all int32 on the GPU; slots
     behind the last new token are -1."""
     r = (_native or native()).kv_plan(lens, n_new, free_pages, block_table, page, n_tokens, stream)
     if type(r) is int:
@@ -363,8 +363,10 @@ def kv_read(cache: KvCache, slots, dtype=torch.float16, out=None, stream=None):
 
 def cached_attn(Q, cache: KvCache, block_table, kv_lens, q_start=None, max_nq=None, causal=False, scale=None, out=None, stream=None):
     """dgq_cached_attn: attention over the first kv_lens[b] (int32 [B]) tokens of each request's pages (block_table int32
-    [B, max_pages]).  Q [B, nq, Hq, d], or packed [rows, Hq, d] with q_start (int32 [B + 1]) and at most max_nq rows a request
-    (default: as many as there are; rows outside every request are not written).  causal: the queries are the last tokens.
+    [B, max_pages], max_pages at least 1).  Q [B, nq, Hq, d], or packed [rows, Hq, d] with q_start (int32 [B + 1]) and at most max_nq
+    rows a request; rows outside every request are not written.  Without max_nq the call goes out as if one request might have all
+    rows: right, but slower where each has few.  The table's width, too, counts as the longest request may be.  causal: the queries
+    are the last tokens.
     Returns O like Q."""
     r = (_native or native()).cached_attn(cache.k, cache.v, cache.k_scale, cache.v_scale, cache.d, Q, block_table, kv_lens, q_start,
                                           max_nq, bool(causal), scale, out, stream)

@@ -201,8 +201,10 @@ __device__ __forceinline__ int quantize_code(float x, float inv_s, float Zf, flo
 // ------------------------------------------------------------------ programmatic dependent launch
 // Kernels of the hot path are launched so that the next kernel in the stream may be scheduled while
 // the current one drains (its blocks become resident as this one's exit, without the launch gap):
-// every such kernel calls pdl_launch_dependents() at its top and pdl_wait() before its first access
-// to global memory that an earlier kernel may have written.  pdl_wait() returns once every
+// every such kernel calls pdl_wait() before its first access to global memory that an earlier kernel
+// may have written, and pdl_launch_dependents() where the next kernel's blocks may come in: most at their
+// top, kernels that take their tensor memory after the wait behind that (a block of the next kernel
+// could take it and wait for this one), others behind the reads that those blocks would slow down.  pdl_wait() returns once every
 // preceding kernel has completed and its writes are visible; without the launch attribute both
 // are no-ops.
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }

@@ -1,8 +1,9 @@
 // Attention with full-precision scores over an encoder's states and over a paged 8-bit cache:
 //
-//     O_i = sum_j w_ij V_j / sum_j w_ij,   w_ij = 2^(t_ij - m_i),   t_ij = log2(e) scale Q_i . K_j,   m_i >= max_j t_ij
+//     O_i = sum_j w_ij V_j / sum_j w_ij,   w_ij = 2^(t_ij - m_i),   t_ij = log2(e) scale Q_i . K_j
 //
-// over the keys that row i sees; a row that sees none gives zeros.
+// over the keys that row i sees; a row that sees none gives zeros.  Any m_i gives the same quotient; the kernels keep one that the
+// largest t_ij so far exceeds by 8 at most.
 #pragma once
 
 #include "kv_cache.cuh"
@@ -53,7 +54,8 @@ __device__ __forceinline__ int enc_sees(const EncAttnArgs& a, const EncRequest& 
 }
 
 // The request of a given rank by length, for all threads of a block: where blocks run in several rounds, the last ones to start
-// should be short.
+// should be short.  A thread counts one request's rank, so this goes up to as many requests as the smallest block has threads; more
+// are taken in their order.
 constexpr int EA_SORTED = 128;
 __device__ __forceinline__ int enc_request_of_rank(const EncAttnArgs& a, int rank) {
   __shared__ int lens[EA_SORTED], found;
@@ -78,7 +80,8 @@ constexpr float EA_LAZY = 8.0f;           // a row's reference follows its maxim
 
 // NT: query tiles of a block.  Over 16-bit keys one, and two blocks to an SM, whose starts, products and softmaxes then drift apart
 // and run under each other (2 x 10 x 4096 x 64 over 4173 keys: 153 us, with two tiles in one block 191; 128 features 214 and 277).
-// Over a cache two, which share the work of widening every code (2 x 16 of 4 x 2048 x 128 over 6000 codes: 283 us, with one 489).
+// Over a cache two, which share the work of widening every code (2 x 16 of 4 x 2048 x 128 over 6000 codes: 283 us, with one 489); their
+// 608 threads have 96 registers each and spill 76 bytes for heads to 128 and 8 to 64, the 448 for heads to 160 (128 registers) 52.
 template <int NP, bool CACHED>
 struct EaCfg {
   static constexpr int NT = CACHED && NP <= 2 ? 2 : 1;
@@ -709,11 +712,13 @@ static dgq_status ea_launch_tiles(const EncAttnArgs& a, cudaStream_t stream) {
 
 // ------------------------------------------------------------------ few query rows: keys split over warps and blocks
 // The n x G rows of a request's queries that share a key head are columns of S^T = K Q^T (mma.m16n8k16: sixteen keys, eight
-// columns), so that a key or value is read once for all of them, straight from memory into the operand's registers: which
+// columns), so that a key or value is read once for up to 32 of them (16 for heads beyond 128), straight from memory into the operand's
+// registers; more columns are blocks of their own, which read the keys again, for a request with fewer queries than others too.  Which
 // features a lane's sixteen bytes hold is the lane's choice as long as Q's fragment follows it.  Weights turn into the second
 // product's operand O^T = V^T P by transposing 8 x 8 tiles between lanes.  Codes become fp16 in registers (1.25 instructions a
 // code for keys, 1.5 for values).  Each warp has its own running maximum and sums; the warps of a block meet in shared memory,
-// the blocks of a request in the shared memory of their cluster, in a fixed order.
+// the blocks of a request in the shared memory of their cluster, in a fixed order.  Beyond 16 columns heads of 72 to 128 take all 255
+// registers and spill 436 bytes (over codes 268), heads beyond 128 with 16 columns 44 (over codes none).
 enum { EF_I8 = 0, EF_F16 = 1, EF_BF16 = 2 };
 constexpr int EF_SPLITS = 16;   // most blocks of a cluster
 
