@@ -450,7 +450,9 @@ __device__ __forceinline__ void kv_write_gaps(const KvWriteArgs& a, const KvRun&
 // few tokens share a warp only where the GPU is full without.  64 prompts of 20 to 77 rows of 20 x 64 into pages of 16 and out again:
 // 43 us with a block per run, a division per value and a second read; 18.2 with a warp for keys and one for values; 16.6 with one
 // warp for both.  Looking for a run's end behind gaps and for values that are not finite costs 1.5 us of that case with changing inputs
-// (19.6 -> 21.1; 256 single tokens 19.5 -> 20.7), a slot map with room for 64, 960 and 8128 more tokens 0.2, 0.8 and 8 us.  Without the bound on registers the compiler takes 120 for runs with gaps and fewer blocks share an SM (22.2 us for the tokens).
+// (19.6 -> 21.1; 256 single tokens 19.5 -> 20.7); 64 tokens in a slot map with room for 64, 960 and 8128 more 0.2, 0.8 and 8 us.
+// Without the bound on registers the compiler takes 120 for runs with gaps and fewer blocks share an SM (22.2 us for the tokens); a
+// bound for six blocks spills (23.0 us for the prompts).
 template <bool BF, int THREADS>
 __global__ void __launch_bounds__(WRITE_THREADS, 5) kv_write_kernel(const __grid_constant__ KvWriteArgs a) {
   __shared__ uint32_t red[2][WRITE_THREADS / 32];
