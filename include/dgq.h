@@ -306,6 +306,59 @@ dgq_status dgq_cached_attn(const dgq_kv_cache* cache, const dgq_rows* Q, const d
                            int64_t n_rows, const int32_t* q_start, int max_nq, const int32_t* block_table, int max_pages,
                            const int32_t* kv_lens, int causal, float scale, void* stream);
 
+/* ---------------------------------------------------------------- group norm, and products of few rows with 4-bit weights
+ * (What stands around the convolutions of a UNet's residual block; the paper leaves it in 16 bits.  The calls of this section are this
+ * library's own.  dgq_group_norm, dgq_group_norm_quantize and dgq_linear_few only enqueue work on `stream`, allocate nothing and do
+ * not synchronise.  Work goes to the current device, where all memory and objects have to be.) */
+
+enum { DGQ_ACT_NONE = 0, DGQ_ACT_SILU = 1 }; /* SiLU: y / (1 + e^-y) */
+
+/* Group norm of channels-last maps X [B, P, C] (P pixels; `head` of the strides is ignored) of type `dtype`, with an addend per
+ * image and channel (dev [B, C] of the same type, rows ld_add elements apart, 0 for one that all images share; NULL: none):
+ *   u = x + add[b, c];  y = (u - mean) / sqrt(var + eps) * gamma[c] + beta[c];  Y = act(y), rounded once,
+ * mean and (biased) variance over the P pixels and C / n_groups neighbouring channels of a group.  gamma, beta: dev fp32 [C], NULL for 1
+ * and 0.  Statistics are held in 64 bits, the rest in 32.  A group that holds a value that is not finite gives NaN.  Y may be X (the
+ * same pointer and strides); it may not overlap X otherwise.
+ * C a multiple of 8 up to 4096, any n_groups that divides it, eps positive.
+ * workspace: dev, 256-byte aligned, at least dgq_group_norm_workspace_bytes(); contents undefined on entry and exit; calls that may
+ * overlap on the GPU need separate ones.
+ * Errors: INVALID_ARG (also: pixel rows of Y that overlap), ALIGNMENT, UNSUPPORTED (also: B > 65535, P > 2^30), WORKSPACE, CUDA. */
+dgq_status dgq_group_norm(const dgq_rows* X, const void* add, int64_t ld_add, const float* gamma, const float* beta,
+                          const dgq_rows* Y, int dtype, int B, int P, int C, int n_groups, float eps, int act, void* workspace,
+                          size_t workspace_bytes, void* stream);
+/* The same, straight into the codes of a layer: Xq dev bytes [B * P, K_pad] as dgq_quantize_act lays them out, with the static table
+ * of `timestep` (row i = b * P + p is pixel position i mod the grouping's own P), C channels of the grouping.  The value that is
+ * quantized is act(y) itself, not its rounding to 16 bits:
+ *   q = clamp(rint(act(y) * inv_s) + Z, 0, 2^b - 1)   as 64-bit arithmetic on the 16-bit inputs gives it (inv_s is the table's fp32
+ * number): the codes do not depend on how the sums were split.  NaN gives code 0.
+ * DGQ_CODES_S8_CENTRED has the limits of dgq_quantize_act.  Xq is 16-byte aligned and does not overlap X.
+ * Errors: as above, NOT_CALIBRATED, INVALID_ARG also for a grouping of another device than the current one. */
+dgq_status dgq_group_norm_quantize(const dgq_groups* g, int timestep, int layout, const dgq_rows* X, const void* add,
+                                   int64_t ld_add, const float* gamma, const float* beta, int dtype, int B, int P, int n_groups,
+                                   float eps, int act, void* Xq, void* workspace, size_t workspace_bytes, void* stream);
+dgq_status dgq_group_norm_workspace_bytes(int B, int P, int C, int n_groups, size_t* bytes);
+
+/* A 4-bit weight whose scales each serve one output and `group` (32, 64 or 128) neighbouring input channels, for products with few
+ * 16-bit rows (time embeddings, single tokens).  Library-owned; every call but _destroy synchronises with the host. */
+typedef struct dgq_few_weight dgq_few_weight;
+/* W dev fp16 [N, K], rounded to nearest: s = max |w| / 7 of the group rounded up to fp16, q = rint(w / s).  K a multiple of 8 (the last
+ * group may be short), K and N up to 2^20 - 16.  Errors: INVALID_ARG (also: a weight that is not finite), UNSUPPORTED, CUDA. */
+dgq_status dgq_few_weight_prepare(const void* W, int N, int K, int group, dgq_few_weight** out, void* stream);
+/* The same from codes quantized elsewhere: wq dev int8 [N, K], -8 .. 7; scales dev fp16 [N, ceil(K / group)], finite.
+ * Errors: INVALID_ARG (also: a code or scale outside these), UNSUPPORTED, CUDA. */
+dgq_status dgq_few_weight_from_codes(const int8_t* wq, const void* scales, int N, int K, int group, dgq_few_weight** out,
+                                     void* stream);
+dgq_status dgq_few_weight_destroy(dgq_few_weight* w);
+/* Host copies of the codes (int8 [N, K]) and of the scales' fp16 bits [N, ceil(K / group)]; either may be NULL. */
+dgq_status dgq_few_weight_export(const dgq_few_weight* w, int8_t* wq, uint16_t* scales);
+/* Y[m, n] = bias[n] + sum_g s[n, g] * sum over the channels k of group g of q[n, k] * act(X[m, k]), summed in fp32 and rounded once.
+ * X dev [M, K], Y dev [M, N], bias dev [N] or NULL, all of type `dtype`; X 16-byte aligned, its rows ldx elements apart (a multiple of 8,
+ * 0 allowed), those of Y ldy.  SiLU's results are rounded to `dtype` for the product.  Any M; the weight is read once for every 32 rows,
+ * so that for many rows dgq_linear is the better call.
+ * Errors: INVALID_ARG (also: a weight of another device than the current one), ALIGNMENT, UNSUPPORTED (M > 2^21 - 32), CUDA. */
+dgq_status dgq_linear_few(const dgq_few_weight* w, const void* X, int64_t ldx, int dtype, int M, int act, const void* bias, void* Y,
+                          int64_t ldy, void* stream);
+
 /* ---------------------------------------------------------------- cross-attention without a caller workspace
  * (The paper has no counterpart: this is a deployment convenience of this library.)
  * Same computation, arguments and results as dgq_cross_attn_logq, for callers that

@@ -23,13 +23,16 @@ OUTLIER_KMEANS, OUTLIER_EXPLICIT = 0, 1
 MODE_STATIC, MODE_DYNAMIC_TOKEN = 0, 1
 CODES_U8, CODES_S8_CENTRED = 0, 1
 SCALE_PER_PROMPT, SCALE_PER_PROMPT_HEAD, SCALE_PER_CALL = 0, 1, 2
+ACT_NONE, ACT_SILU = 0, 1
 
 EXPORTS = [
     "dgq_calibrate_groups", "dgq_groups_from_host", "dgq_groups_destroy", "dgq_groups_info",
     "dgq_groups_export", "dgq_quantize_act", "dgq_weight_prepare", "dgq_weight_from_codes",
     "dgq_weight_destroy", "dgq_weight_export", "dgq_linear", "dgq_linear_workspace_bytes", "dgq_cross_attn_logq", "dgq_cross_attn_logq_qv", "dgq_self_attn_logq",
     "dgq_cross_attn_workspace_bytes", "dgq_cross_attn_logq_noalloc",
-    "dgq_encoder_attn", "dgq_kv_plan", "dgq_kv_write", "dgq_kv_read", "dgq_cached_attn", "dgq_selftest_wait_timeout", "dgq_device_status", "dgq_status_string", "dgq_launch_count",
+    "dgq_encoder_attn", "dgq_kv_plan", "dgq_kv_write", "dgq_kv_read", "dgq_cached_attn",
+    "dgq_group_norm", "dgq_group_norm_quantize", "dgq_group_norm_workspace_bytes", "dgq_few_weight_prepare", "dgq_few_weight_from_codes",
+    "dgq_few_weight_destroy", "dgq_few_weight_export", "dgq_linear_few", "dgq_selftest_wait_timeout", "dgq_device_status", "dgq_status_string", "dgq_launch_count",
 ]
 
 
@@ -372,6 +375,93 @@ def cached_attn(Q, cache: KvCache, block_table, kv_lens, q_start=None, max_nq=No
                                           max_nq, bool(causal), scale, out, stream)
     if type(r) is int:
         _check(r, "dgq_cached_attn")
+    return r
+
+
+def group_norm_workspace_bytes(B, P, C_, n_groups) -> int:
+    n = C.c_size_t(0)
+    _check(lib().dgq_group_norm_workspace_bytes(C.c_int(B), C.c_int(P), C.c_int(C_), C.c_int(n_groups), C.byref(n)), "dgq_group_norm_workspace_bytes")
+    return n.value
+
+
+def group_norm(X, n_groups, gamma=None, beta=None, eps=1e-5, act=ACT_NONE, add=None, out=None, workspace=None, stream=None):
+    """dgq_group_norm: X a CUDA fp16 or bf16 map [B, P, C] or [B, H, W, C] (channels contiguous, pixels evenly spaced), gamma and beta fp32
+    [C], add [B, C] of X's type (added to every pixel before the norm), act ACT_NONE or ACT_SILU.  `out` may be X.  `workspace` (CUDA
+    tensor) is taken from torch where it is None.  Returns the normalised map."""
+    r = (_native or native()).group_norm(X, n_groups, gamma, beta, eps, act, add, out, workspace, stream)
+    if type(r) is int:
+        _check(r, "dgq_group_norm")
+    return r
+
+
+def group_norm_quantize(groups: Groups, X, n_groups, gamma=None, beta=None, eps=1e-5, act=ACT_NONE, add=None, timestep=0, layout=CODES_U8,
+                        out=None, workspace=None, stream=None):
+    """dgq_group_norm_quantize: the same into the codes of the layer whose static table `groups` holds, as `quantize_act` lays them out.
+    Returns Xq uint8 [B * P, K_pad]."""
+    r = (_native or native()).group_norm_quantize(_raw(groups.h), groups.C, groups.K_pad, timestep, layout, X, n_groups, gamma, beta, eps, act, add,
+                                                  out, workspace, stream)
+    if type(r) is int:
+        _check(r, "dgq_group_norm_quantize")
+    return r
+
+
+class FewWeight:
+    """Owns a dgq_few_weight handle: 4-bit codes [N, K] with an fp16 scale for each output and `group` input channels."""
+
+    def __init__(self, handle, N, K, group):
+        self.h, self.N, self.K, self.group = handle, N, K, group
+
+    def export(self):
+        """Codes int8 [N, K] and scales fp16 [N, ceil(K / group)] as numpy arrays."""
+        wq = np.empty((self.N, self.K), np.int8)
+        scales = np.empty((self.N, -(-self.K // self.group)), np.float16)
+        _check(lib().dgq_few_weight_export(self.h, _ptr(wq), _ptr(scales)), "dgq_few_weight_export")
+        return wq, scales
+
+    def close(self):
+        if self.h:
+            lib().dgq_few_weight_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def few_weight_prepare(W, group=64, stream=None) -> FewWeight:
+    """dgq_few_weight_prepare: W is a CUDA fp16 [N, K] tensor, rounded to nearest with a scale per output and `group` input channels."""
+    if not (W.is_cuda and W.dtype == torch.float16 and W.dim() == 2 and W.is_contiguous()):
+        raise ValueError("W is a contiguous CUDA fp16 matrix [N, K]")
+    h = C.c_void_p(None)
+    with torch.cuda.device(W.device):
+        st = lib().dgq_few_weight_prepare(_ptr(W), C.c_int(W.shape[0]), C.c_int(W.shape[1]), C.c_int(group), C.byref(h), _stream(stream))
+    _check(st, "dgq_few_weight_prepare")
+    return FewWeight(h, W.shape[0], W.shape[1], group)
+
+
+def few_weight_from_codes(wq, scales, group=64, stream=None) -> FewWeight:
+    """dgq_few_weight_from_codes: wq CUDA int8 [N, K] with values -8 .. 7, scales CUDA fp16 [N, ceil(K / group)]."""
+    if not (wq.is_cuda and wq.dtype == torch.int8 and wq.dim() == 2 and wq.is_contiguous()):
+        raise ValueError("wq is a contiguous CUDA int8 matrix [N, K]")
+    N, K = wq.shape
+    if group not in (32, 64, 128):
+        raise ValueError("group is 32, 64 or 128")
+    if not (scales.device == wq.device and scales.dtype == torch.float16 and tuple(scales.shape) == (N, -(-K // group)) and scales.is_contiguous()):
+        raise ValueError("scales is a contiguous fp16 matrix [N, ceil(K / group)] on wq's device")
+    h = C.c_void_p(None)
+    with torch.cuda.device(wq.device):
+        st = lib().dgq_few_weight_from_codes(_ptr(wq), _ptr(scales), C.c_int(N), C.c_int(K), C.c_int(group), C.byref(h), _stream(stream))
+    _check(st, "dgq_few_weight_from_codes")
+    return FewWeight(h, N, K, group)
+
+
+def linear_few(weight: FewWeight, X, bias=None, act=ACT_NONE, out=None, stream=None):
+    """dgq_linear_few: act(X) times the weight, X CUDA fp16 or bf16 [M, K], bias [N] of its type.  Returns Y [M, N]."""
+    r = (_native or native()).linear_few(_raw(weight.h), weight.N, weight.K, X, act, bias, out, stream)
+    if type(r) is int:
+        _check(r, "dgq_linear_few")
     return r
 
 

@@ -560,6 +560,181 @@ PyObject* kv_plan(PyObject* const* a, Py_ssize_t n) {
   return tuple({wrap(start), wrap(out_lens), wrap(slots), wrap(used)});
 }
 
+// ---------------------------------------------------------------- group norm and products of few rows
+bool floats(const at::Tensor& t, const at::Tensor& like, int64_t n, const char* what) {
+  if (t.defined() && (!t.is_cuda() || t.device() != like.device() || t.scalar_type() != at::kFloat || !t.is_contiguous() || t.numel() != n))
+    return fail(what);
+  return true;
+}
+
+// A map [B, P, C] or [B, H, W, C] whose pixels lie at one distance from each other.
+bool map16(const at::Tensor& t, const at::Tensor& like, const char* what, dgq_rows* r, int64_t* pixels) {
+  const int64_t dims = t.defined() ? t.dim() : 0;
+  if (!t.defined() || !t.is_cuda() || t.device() != like.device() || t.scalar_type() != like.scalar_type() || (dims != 3 && dims != 4) ||
+      (t.scalar_type() != at::kHalf && t.scalar_type() != at::kBFloat16) || (t.size(dims - 1) > 1 && t.stride(dims - 1) != 1))
+    return fail(what);
+  int64_t step = t.stride(dims - 2);
+  *pixels = t.size(1);
+  if (dims == 4) {
+    *pixels *= t.size(2);
+    if (t.size(2) == 1) step = t.stride(1);
+    else if (t.size(1) > 1 && t.stride(1) != t.size(2) * step) return fail(what);
+  }
+  *r = dgq_rows{t.data_ptr(), t.stride(0), step, 0};
+  return true;
+}
+
+struct NormArgs {
+  at::Tensor x, gamma, beta, add;
+  dgq_rows rx;
+  int B, P, C, n_groups, act;
+  float eps;
+  int64_t ld_add;
+};
+// (X, n_groups, gamma | None, beta | None, eps, act, add | None)
+bool norm_args(PyObject* const* a, NormArgs* n) {
+  if (!tensor(a[0], &n->x) || !integer(a[1], &n->n_groups) || !tensor(a[2], &n->gamma) || !tensor(a[3], &n->beta) || !integer(a[5], &n->act) ||
+      !tensor(a[6], &n->add))
+    return false;
+  const double eps = PyFloat_AsDouble(a[4]);
+  if (eps == -1.0 && PyErr_Occurred()) return false;
+  n->eps = static_cast<float>(eps);
+  int64_t pixels;
+  if (!map16(n->x, n->x, "X is a CUDA fp16 or bf16 map [B, P, C] or [B, H, W, C] with contiguous channels and evenly spaced pixels", &n->rx, &pixels))
+    return false;
+  if (!fits(n->x.size(0), &n->B) || !fits(pixels, &n->P) || !fits(n->x.size(n->x.dim() - 1), &n->C)) return false;
+  if (!floats(n->gamma, n->x, n->C, "gamma is a contiguous CUDA fp32 tensor [C]") || !floats(n->beta, n->x, n->C, "beta is a contiguous CUDA fp32 tensor [C]"))
+    return false;
+  n->ld_add = 0;
+  if (n->add.defined()) {
+    if (!n->add.is_cuda() || n->add.device() != n->x.device() || n->add.scalar_type() != n->x.scalar_type() || n->add.dim() != 2 ||
+        n->add.size(0) != n->B || n->add.size(1) != n->C || (n->C > 1 && n->add.stride(1) != 1))
+      return fail("add is a tensor [B, C] of X's type and device with contiguous rows");
+    n->ld_add = n->add.stride(0);
+  }
+  return true;
+}
+// The workspace of a call: the caller's, or one of the size the library asks for.
+bool norm_workspace(PyObject* given, const NormArgs& n, PyObject* stream, void* st, at::Tensor* ws, dgq_status* rc) {
+  *rc = DGQ_OK;
+  if (!tensor(given, ws)) return false;
+  if (ws->defined()) {
+    if (!ws->is_cuda() || ws->device() != n.x.device() || !ws->is_contiguous()) return fail("workspace is a contiguous CUDA tensor on X's device");
+    return true;
+  }
+  size_t need = 0;
+  *rc = dgq_group_norm_workspace_bytes(n.B, n.P, n.C, n.n_groups, &need);
+  if (*rc == DGQ_OK) *ws = scratch(static_cast<int64_t>(need), n.x, stream, st);
+  return true;
+}
+
+// (X, n_groups, gamma, beta, eps, act, add, out | None, workspace | None, stream) -> Y
+PyObject* group_norm(PyObject* const* a, Py_ssize_t n) {
+  void* st;
+  NormArgs x;
+  at::Tensor y, ws;
+  if (!arity(n, 10) || !norm_args(a, &x) || !tensor(a[7], &y)) return nullptr;
+  const c10::cuda::CUDAGuard on(x.x.device());
+  if (!stream_on(a[9], x.x, &st)) return nullptr;
+  if (!y.defined()) {
+    y = x.x.dim() == 3 ? empty({x.x.size(0), x.x.size(1), x.x.size(2)}, x.x.scalar_type(), x.x)
+                       : empty({x.x.size(0), x.x.size(1), x.x.size(2), x.x.size(3)}, x.x.scalar_type(), x.x);
+    on_stream(y, a[9], st);
+  }
+  dgq_rows ry;
+  int64_t pixels;
+  if (!map16(y, x.x, "out is a map like X", &ry, &pixels) || (y.sizes() != x.x.sizes() && !fail("out is a map like X"))) return nullptr;
+  if (y.numel() == 0) return output(a[7], y);
+  dgq_status rc;
+  if (!norm_workspace(a[8], x, a[9], st, &ws, &rc)) return nullptr;
+  if (rc != DGQ_OK) return status(rc);
+  const int type = dtype_of(x.x);
+  void *p_add = ptr(x.add), *p_ws = ptr(ws);
+  const float *p_gamma = ptr<float>(x.gamma), *p_beta = ptr<float>(x.beta);
+  const size_t bytes = ws.nbytes();
+  Py_BEGIN_ALLOW_THREADS
+  rc = dgq_group_norm(&x.rx, p_add, x.ld_add, p_gamma, p_beta, &ry, type, x.B, x.P, x.C, x.n_groups, x.eps, x.act, p_ws, bytes, st);
+  Py_END_ALLOW_THREADS
+  if (rc != DGQ_OK) return status(rc);
+  return output(a[7], y);
+}
+
+// (groups, C of the grouping, K_pad, timestep, layout, X, n_groups, gamma, beta, eps, act, add, out | None, workspace | None, stream) -> Xq
+PyObject* group_norm_quantize(PyObject* const* a, Py_ssize_t n) {
+  void *st, *g;
+  int channels, k_pad, timestep, layout;
+  NormArgs x;
+  at::Tensor xq, ws;
+  if (!arity(n, 15) || !handle(a[0], &g) || !integer(a[1], &channels) || !integer(a[2], &k_pad) || !integer(a[3], &timestep) ||
+      !integer(a[4], &layout) || !norm_args(a + 5, &x) || !tensor(a[12], &xq))
+    return nullptr;
+  if (x.C != channels && !fail("X has the grouping's channels")) return nullptr;
+  const c10::cuda::CUDAGuard on(x.x.device());
+  if (!stream_on(a[14], x.x, &st)) return nullptr;
+  const int64_t rows = static_cast<int64_t>(x.B) * x.P;
+  if (!xq.defined()) {
+    xq = empty({rows, k_pad}, at::kByte, x.x);
+    on_stream(xq, a[14], st);
+  }
+  if ((!xq.is_cuda() || xq.device() != x.x.device() || xq.scalar_type() != at::kByte || xq.dim() != 2 || xq.size(0) != rows ||
+       xq.size(1) != k_pad || !xq.is_contiguous()) &&
+      !fail("out is a contiguous uint8 tensor [B * P, K_pad] on X's device"))
+    return nullptr;
+  if (rows == 0) return output(a[12], xq);
+  dgq_status rc;
+  if (!norm_workspace(a[13], x, a[14], st, &ws, &rc)) return nullptr;
+  if (rc != DGQ_OK) return status(rc);
+  const int type = dtype_of(x.x);
+  void *p_add = ptr(x.add), *p_ws = ptr(ws), *p_xq = ptr(xq);
+  const float *p_gamma = ptr<float>(x.gamma), *p_beta = ptr<float>(x.beta);
+  const size_t bytes = ws.nbytes();
+  Py_BEGIN_ALLOW_THREADS
+  rc = dgq_group_norm_quantize(static_cast<const dgq_groups*>(g), timestep, layout, &x.rx, p_add, x.ld_add, p_gamma, p_beta, type, x.B, x.P,
+                               x.n_groups, x.eps, x.act, p_xq, p_ws, bytes, st);
+  Py_END_ALLOW_THREADS
+  if (rc != DGQ_OK) return status(rc);
+  return output(a[12], xq);
+}
+
+// (weight, N, K, X, act, bias | None, out | None, stream) -> Y
+PyObject* linear_few(PyObject* const* a, Py_ssize_t n) {
+  void *st, *w;
+  int n_out, k, act, m;
+  at::Tensor x, bias, y;
+  if (!arity(n, 8) || !handle(a[0], &w) || !integer(a[1], &n_out) || !integer(a[2], &k) || !tensor(a[3], &x) || !integer(a[4], &act) ||
+      !tensor(a[5], &bias) || !tensor(a[6], &y))
+    return nullptr;
+  if ((!x.defined() || !x.is_cuda() || x.dim() != 2 || (x.scalar_type() != at::kHalf && x.scalar_type() != at::kBFloat16) || x.size(1) != k ||
+       (k > 1 && x.stride(1) != 1)) &&
+      !fail("X is a CUDA fp16 or bf16 matrix [M, K] with contiguous rows and the weight's K"))
+    return nullptr;
+  if (bias.defined() && (!bias.is_cuda() || bias.device() != x.device() || bias.scalar_type() != x.scalar_type() || !bias.is_contiguous() ||
+                         bias.numel() != n_out) &&
+      !fail("bias is a contiguous tensor [N] of X's type and device"))
+    return nullptr;
+  if (!fits(x.size(0), &m)) return nullptr;
+  const c10::cuda::CUDAGuard on(x.device());
+  if (!stream_on(a[7], x, &st)) return nullptr;
+  if (!y.defined()) {
+    y = empty({m, n_out}, x.scalar_type(), x);
+    on_stream(y, a[7], st);
+  }
+  if ((!y.is_cuda() || y.device() != x.device() || y.scalar_type() != x.scalar_type() || y.dim() != 2 || y.size(0) != m || y.size(1) != n_out ||
+       (n_out > 1 && y.stride(1) != 1)) &&
+      !fail("out is a matrix [M, N] of X's type and device with contiguous rows"))
+    return nullptr;
+  if (m == 0) return output(a[6], y);
+  const int type = dtype_of(x);
+  const int64_t ldx = x.stride(0), ldy = y.stride(0);
+  void *p_x = ptr(x), *p_bias = ptr(bias), *p_y = ptr(y);
+  dgq_status rc;
+  Py_BEGIN_ALLOW_THREADS
+  rc = dgq_linear_few(static_cast<const dgq_few_weight*>(w), p_x, ldx, type, m, act, p_bias, p_y, ldy, st);
+  Py_END_ALLOW_THREADS
+  if (rc != DGQ_OK) return status(rc);
+  return output(a[6], y);
+}
+
 template <PyObject* (*BODY)(PyObject* const*, Py_ssize_t)>
 PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(entry<BODY>)), METH_FASTCALL, nullptr};
@@ -567,7 +742,8 @@ PyMethodDef method(const char* name) {
 PyMethodDef methods[] = {method<quantize_act>("quantize_act"), method<linear>("linear"),
                          method<cross_attn_logq>("cross_attn_logq"), method<self_attn_logq>("self_attn_logq"),
                          method<encoder_attn>("encoder_attn"), method<cached_attn>("cached_attn"), method<kv_plan>("kv_plan"),
-                         method<kv_write>("kv_write"), method<kv_read>("kv_read"),
+                         method<kv_write>("kv_write"), method<kv_read>("kv_read"), method<group_norm>("group_norm"),
+                         method<group_norm_quantize>("group_norm_quantize"), method<linear_few>("linear_few"),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

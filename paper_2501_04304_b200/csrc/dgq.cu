@@ -11,6 +11,8 @@
 #include "self_attention.cuh"
 #include "kv_cache.cuh"
 #include "encoder_attention.cuh"
+#include "group_norm.cuh"
+#include "few.cuh"
 
 // ---------------------------------------------------------------------------------------------
 // Cross-attention for callers that cannot allocate a workspace: the scratch is this fixed array

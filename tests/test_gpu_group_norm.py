@@ -1,0 +1,295 @@
+"""Group norm of channels-last maps, as values and as codes, against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import norm_testlib as nl
+from dgq_testlib import gpu
+from paper_2501_04304_b200 import binding as b
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+def make(seed, B, P, C, dtype, add=True, shift=0.3):
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((B, P, C)).astype(np.float32) + np.float32(shift)
+    x[:, :, rng.permutation(C)[:max(1, C // 50)]] *= 8
+    t = torch.from_numpy(x).to(dtype).cuda()
+    gamma = torch.from_numpy((1 + 0.2 * rng.standard_normal(C)).astype(np.float32)).cuda()
+    beta = torch.from_numpy((0.2 * rng.standard_normal(C)).astype(np.float32)).cuda()
+    e = torch.from_numpy(rng.standard_normal((B, C)).astype(np.float32)).to(dtype).cuda() if add else None
+    return t, gamma, beta, e
+
+
+def against(x, groups, gamma, beta, eps, silu, e, y):
+    v, u, c = nl.norm(x, groups, gamma, beta, eps, silu, e)
+    nl.check(y, v, nl.norm_bound(v, u, c, x.dtype))
+
+
+# B, P, C, groups: one pixel, one channel a group, one group, groups of 10, 30, 40 and 60 channels, groups that start inside eight
+# channels, the widest, many images, maps that one block holds, that several share and that none does
+SHAPES = [(1, 1, 8, 1), (2, 1, 64, 8), (3, 2, 8, 8), (1, 37, 24, 8), (2, 64, 1280, 32), (1, 4096, 320, 32), (2, 333, 320, 32), (1, 1000, 960, 32),
+          (2, 77, 1920, 32), (1, 257, 72, 24), (1, 129, 40, 40), (2, 50, 4096, 1), (1, 30, 4096, 4096), (1, 300, 2568, 321), (9, 100, 128, 32), (70, 5, 56, 7),
+          (1, 70001, 8, 2), (1, 20000, 128, 32), (1, 5000, 640, 1), (40, 260, 64, 4), (2, 1030, 1000, 5), (1, 16, 3000, 3000)]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("B,P,C,groups", SHAPES)
+def test_values(B, P, C, groups, dtype):
+    gpu()
+    if P * C // groups == 1:
+        pytest.skip("a group of one value")
+    x, gamma, beta, e = make(B + P + C, B, P, C, dtype, add=P % 2 == 0)
+    silu = C % 3 != 0
+    y = b.group_norm(x, groups, gamma, beta, eps=1e-5, act=b.ACT_SILU if silu else b.ACT_NONE, add=e)
+    assert y.dtype == dtype and y.shape == x.shape
+    against(x, groups, gamma, beta, 1e-5, silu, e, y)
+
+
+def test_one_value_a_group():
+    """Its variance is 0: the result is beta."""
+    gpu()
+    x, gamma, beta, _ = make(5, 2, 1, 16, F16, add=False)
+    y = b.group_norm(x, 16, gamma, beta)
+    assert torch.equal(y, beta.half().expand(2, 1, 16))
+
+
+@pytest.mark.parametrize("P", [64, 5000, 40000])
+def test_defaults_and_constant_maps(P):
+    gpu()
+    x = torch.full((2, P, 64), 3.25, dtype=F16, device="cuda")
+    assert (b.group_norm(x, 4).abs() <= 1e-4).all()
+    x[1] = 0
+    assert (b.group_norm(x, 4)[1] == 0).all()
+
+
+@pytest.mark.parametrize("P", [100, 3000, 60000])
+def test_far_mean_and_one_outlier(P):
+    """Values around 1000 of deviation 1, in one image; zeros with one large value in front, in the other."""
+    gpu()
+    rng = np.random.default_rng(P)
+    x = torch.zeros(2, P, 32, dtype=F16)
+    x[0] = torch.from_numpy((1000 + rng.standard_normal((P, 32))).astype(np.float32)).half()
+    x[1, 0, 0] = 1000.0
+    x = x.cuda()
+    y = b.group_norm(x, 4)
+    v, u, c = nl.norm(x, 4, None, None, 1e-5, False)
+    nl.check(y, v, nl.norm_bound(v, u, c, F16))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("P", [60, 4000])
+def test_strides(P, dtype):
+    """Slices of wider rows, in and out, an addend that all images share, images in reverse order of memory left to torch."""
+    gpu()
+    wide, gamma, beta, _ = make(7, 3, P, 960, dtype, add=False)
+    e = torch.randn(1, 320, device="cuda").to(dtype).expand(3, 320)
+    x = wide[:, :, 320:640]
+    out = torch.full((3, P, 400), 7.0, dtype=dtype, device="cuda")
+    y = b.group_norm(x, 32, gamma[:320], beta[:320], act=b.ACT_SILU, add=e, out=out[:, :, 64:384])
+    assert y.data_ptr() == out[:, :, 64:384].data_ptr()
+    against(x, 32, gamma[:320], beta[:320], 1e-5, True, e, y)
+    assert (out[:, :, :64] == 7).all() and (out[:, :, 384:] == 7).all()
+    swapped = wide.transpose(0, 1).contiguous().transpose(0, 1)  # pixels outermost
+    assert torch.equal(b.group_norm(swapped, 32, gamma, beta), b.group_norm(wide, 32, gamma, beta))
+
+
+def test_maps_of_rows_and_columns():
+    gpu()
+    x, gamma, beta, _ = make(8, 2, 15 * 21, 64, F16, add=False)
+    flat = b.group_norm(x, 8, gamma, beta)
+    assert torch.equal(b.group_norm(x.view(2, 15, 21, 64), 8, gamma, beta), flat.view(2, 15, 21, 64))
+    assert torch.equal(b.group_norm(x.view(2, 15, 21, 64)[:, :, :1], 8).view(2, 15, 64), b.group_norm(x.view(2, 15, 21, 64)[:, :, 0].contiguous(), 8))
+    with pytest.raises(ValueError):
+        b.group_norm(x.view(2, 15, 21, 64)[:, :, :20], 8)
+
+
+@pytest.mark.parametrize("shape", [(2, 64, 1280), (2, 4096, 320), (1, 60000, 128)])
+def test_in_place(shape):
+    gpu()
+    x, gamma, beta, e = make(9, *shape, F16)
+    y = b.group_norm(x, 32, gamma, beta, act=b.ACT_SILU, add=e)
+    assert b.group_norm(x, 32, gamma, beta, act=b.ACT_SILU, add=e, out=x) is x
+    assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("shape", [(3, 70, 64), (3, 5000, 320), (2, 60000, 64)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_not_finite(shape, bad):
+    """The group is NaN, the others are what they were."""
+    gpu()
+    x, gamma, beta, _ = make(10, *shape, F16, add=False)
+    clean = b.group_norm(x, 32, gamma, beta)
+    x[1, shape[1] // 2, 5] = bad
+    y = b.group_norm(x, 32, gamma, beta)
+    n = shape[2] // 32
+    at = 5 // n
+    assert torch.isnan(y[1, :, at * n:(at + 1) * n]).all()
+    y[1, :, at * n:(at + 1) * n] = clean[1, :, at * n:(at + 1) * n]
+    assert torch.equal(y, clean)
+
+
+def test_large_and_small_bf16():
+    gpu()
+    x, gamma, beta, _ = make(11, 2, 500, 64, BF16, add=False)
+    for f in (1e30, 1e-12):
+        big = (x.double() * f).to(BF16)
+        against(big, 8, gamma, beta, 1e-30, False, None, b.group_norm(big, 8, gamma, beta, eps=1e-30))
+
+
+# ------------------------------------------------------------------ codes
+def grouping(seed, C, P, bits, G, R, silu, z=None, T=1):
+    rng = np.random.default_rng(seed)
+    col = rng.integers(0, G, C)
+    row = rng.integers(0, R, P)
+    scale = np.exp(rng.uniform(-0.5, 0.5, (T, R, G))).astype(np.float32) * np.float32(8.0 / 2 ** bits)
+    zp = np.full((T, R, G), z) if z is not None else rng.integers(0, 2 ** bits // (4 if silu else 1), (T, R, G))
+    return b.groups_from_host(C, P, bits, col, row, scale, zp)
+
+
+def codes_against(g, x, groups, gamma, beta, silu, e, timestep, centred, got, eps=1e-5):
+    v, _, _ = nl.norm(x, groups, gamma, beta, eps, silu, e)
+    ref = nl.codes(v, g.export(), g.bits, timestep, centred)
+    assert torch.equal(got.cpu().long(), ref)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("B,P,C,groups", [s for s in SHAPES if s[1] * s[2] // s[3] > 1])
+@pytest.mark.parametrize("bits,G,R,centred", [(6, 16, 1, True), (8, 5, 2, False), (4, 1, 1, False), (6, 3, 3, True), (2, 32, 1, True)])
+def test_codes(B, P, C, groups, dtype, bits, G, R, centred):
+    gpu()
+    if B * P * C > 1 << 21 and (bits, R) != (6, 1):
+        pytest.skip("the large maps once")
+    x, gamma, beta, e = make(B + P + C, B, P, C, dtype, add=P % 2 == 0)
+    silu = C % 3 != 0
+    g = grouping(P, C, P, bits, min(G, C), R, silu)
+    q = b.group_norm_quantize(g, x, groups, gamma, beta, act=b.ACT_SILU if silu else b.ACT_NONE, add=e,
+                              layout=b.CODES_S8_CENTRED if centred else b.CODES_U8)
+    codes_against(g, x, groups, gamma, beta, silu, e, 0, centred, q)
+
+
+def test_codes_of_a_timestep_and_another_period():
+    """Row 1 of the table; pixel positions repeat with the grouping's own period, not with the map's."""
+    gpu()
+    x, gamma, beta, _ = make(3, 3, 50, 96, F16, add=False)
+    g = grouping(4, 96, 35, 6, 4, 3, False, T=2)
+    q = b.group_norm_quantize(g, x, 8, gamma, beta, timestep=1, layout=b.CODES_S8_CENTRED)
+    codes_against(g, x, 8, gamma, beta, False, None, 1, True, q)
+
+
+@pytest.mark.parametrize("z", [0, 255, -3, 300, -70000, 70000, 2 ** 21, -2 ** 30])
+def test_codes_of_far_zero_points(z):
+    gpu()
+    x, gamma, beta, e = make(4, 2, 90, 64, F16)
+    beta = beta - 0.05 * z if abs(z) < 1000 else beta
+    g = grouping(5, 64, 90, 8, 3, 1, False, z=z)
+    q = b.group_norm_quantize(g, x, 8, gamma, beta, add=e)
+    codes_against(g, x, 8, gamma, beta, False, e, 0, False, q)
+
+
+def test_codes_next_to_borders():
+    """Scales so fine that a 32-bit value leaves the code open for most values, and tables whose steps are the map's own."""
+    gpu()
+    x, gamma, beta, _ = make(6, 1, 400, 64, F16, add=False)
+    n = 64
+    scale = np.full((1, 1, 2), 2.0 ** -18, np.float32)
+    v, _, _ = nl.norm(x, 8, gamma, beta, 1e-5, True)
+    zp = np.full((1, 1, 2), -int(v.median() * 2 ** 18) + 128)
+    g = b.groups_from_host(n, 400, 8, np.arange(n) % 2, np.zeros(400), scale, zp)
+    q = b.group_norm_quantize(g, x, 8, gamma, beta, act=b.ACT_SILU)
+    codes_against(g, x, 8, gamma, beta, True, None, 0, False, q)
+
+
+@pytest.mark.parametrize("centred", [True, False])
+def test_codes_of_values_that_are_not_finite(centred):
+    gpu()
+    x, gamma, beta, _ = make(12, 2, 300, 64, F16, add=False)
+    x[0, 7, 3], x[1, 8, 40] = float("inf"), float("nan")
+    g = grouping(9, 64, 300, 6, 4, 1, False)
+    q = b.group_norm_quantize(g, x, 8, gamma, beta, layout=b.CODES_S8_CENTRED if centred else b.CODES_U8)
+    codes_against(g, x, 8, gamma, beta, False, None, 0, centred, q)
+
+
+def test_codes_feed_the_layer():
+    """The codes are dgq_quantize_act's on the same values, up to the values' rounding to 16 bits, and in its layout."""
+    gpu()
+    x, gamma, beta, _ = make(13, 2, 256, 320, F16, add=False)
+    g = grouping(10, 320, 256, 8, 6, 2, True)
+    a = b.group_norm_quantize(g, x, 32, gamma, beta, act=b.ACT_SILU)
+    y = b.group_norm(x, 32, gamma, beta, act=b.ACT_SILU)
+    c, _, _ = b.quantize_act(g, y.view(-1, 320))
+    d = (a.int() - c.int()).abs()
+    assert d.max() <= 1 and (d > 0).float().mean() < 0.05
+    pad = torch.from_numpy(g.export()["perm"] < 0)
+    assert torch.equal(a[:, pad.cuda()], c[:, pad.cuda()])
+
+
+# ------------------------------------------------------------------ streams, graphs, memory
+@pytest.mark.parametrize("shape", [(2, 64, 1280), (2, 4096, 320), (1, 60000, 128)])
+def test_another_stream_and_graphs(shape):
+    """On a side stream, then as two graphs with workspaces of their own replayed in turn, with other inputs in the same place."""
+    gpu()
+    x, gamma, beta, e = make(14, *shape, F16)
+    g = grouping(11, shape[2], shape[1], 6, 8, 1, True)
+    want = [b.group_norm(x, 32, gamma, beta, add=e), b.group_norm_quantize(g, x, 32, gamma, beta, act=b.ACT_SILU, add=e)]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = [b.group_norm(x, 32, gamma, beta, add=e, stream=side), b.group_norm_quantize(g, x, 32, gamma, beta, act=b.ACT_SILU, add=e, stream=side)]
+    side.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(want, got))
+    graphs = []
+    for k in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = b.group_norm(x, 32, gamma, beta, add=e) if k == 0 else b.group_norm_quantize(g, x, 32, gamma, beta, act=b.ACT_SILU, add=e)
+        graphs.append((graph, out))
+    x.copy_(torch.flip(x, (1,)) * 0.5)
+    want = [b.group_norm(x, 32, gamma, beta, add=e), b.group_norm_quantize(g, x, 32, gamma, beta, act=b.ACT_SILU, add=e)]
+    for _ in range(3):
+        for graph, _ in graphs:
+            graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, (_, q) in zip(want, graphs))
+
+
+def test_many_calls_in_a_row_and_a_workspace_of_the_callers():
+    gpu()
+    shapes = [(2, 64, 1280), (1, 300, 64), (2, 4096, 320), (1, 30000, 128), (3, 7, 24)]
+    made = [make(20 + i, *s, F16) for i, s in enumerate(shapes)]
+    n_groups = [32, 8, 32, 32, 3]
+    size = max(b.group_norm_workspace_bytes(*s, n) for s, n in zip(shapes, n_groups))
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+    want = [b.group_norm(x, n, g, c, add=e) for (x, g, c, e), n in zip(made, n_groups)]
+    for _ in range(5):
+        ws.fill_(255)
+        got = [b.group_norm(x, n, g, c, add=e, workspace=ws) for (x, g, c, e), n in zip(made, n_groups)]
+        assert all(torch.equal(p, q) for p, q in zip(want, got))
+
+
+def test_more_elements_than_31_bits():
+    """Two images 2^31 elements apart."""
+    gpu()
+    x, gamma, beta, _ = make(15, 2, 100, 64, F16, add=False)
+    far = torch.empty((1 << 31) + 64 * 100, dtype=F16, device="cuda").as_strided((2, 100, 64), (1 << 31, 64, 1))
+    far.copy_(x)
+    assert torch.equal(b.group_norm(far, 8, gamma, beta), b.group_norm(x, 8, gamma, beta))
+    g = grouping(12, 64, 100, 6, 4, 1, False)
+    assert torch.equal(b.group_norm_quantize(g, far, 8, gamma, beta), b.group_norm_quantize(g, x, 8, gamma, beta))
+
+
+def test_refusals_of_the_binding():
+    gpu()
+    x, gamma, beta, e = make(16, 2, 10, 64, F16)
+    for call in (lambda: b.group_norm(x.float(), 8), lambda: b.group_norm(x[0], 8), lambda: b.group_norm(x, 8, gamma[:32]),
+                 lambda: b.group_norm(x, 8, gamma.half()), lambda: b.group_norm(x, 8, add=e[:1]), lambda: b.group_norm(x, 8, add=e.float()),
+                 lambda: b.group_norm(x, 8, out=x[:, :5]), lambda: b.group_norm(x.transpose(1, 2), 8), lambda: b.group_norm(x.cpu(), 8),
+                 lambda: b.group_norm_quantize(grouping(1, 32, 10, 6, 2, 1, False), x, 8)):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: b.group_norm(x, 7), lambda: b.group_norm(x, 8, eps=0.0), lambda: b.group_norm(x, 8, act=2),
+                 lambda: b.group_norm(x, 8, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(b.DgqError):
+            call()
+    empty = b.group_norm(x[:0], 8)
+    assert empty.shape == (0, 10, 64) and b.group_norm(x[:, :0], 8).shape == (2, 0, 64)
