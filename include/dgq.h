@@ -317,9 +317,9 @@ enum { DGQ_ACT_NONE = 0, DGQ_ACT_SILU = 1 }; /* SiLU: y / (1 + e^-y) */
  * image and channel (dev [B, C] of the same type, rows ld_add elements apart, 0 for one that all images share; NULL: none):
  *   u = x + add[b, c];  y = (u - mean) / sqrt(var + eps) * gamma[c] + beta[c];  Y = act(y), rounded once,
  * mean and (biased) variance over the P pixels and C / n_groups neighbouring channels of a group.  gamma, beta: dev fp32 [C], NULL for 1
- * and 0.  Statistics are held in 64 bits, the rest in 32.  A group that holds a value that is not finite gives NaN.  Y may be X (the
+ * and 0.  Sums are held in 32 bits or more.  A group that holds a value that is not finite gives NaN.  Y may be X (the
  * same pointer and strides); it may not overlap X otherwise.
- * C a multiple of 8 up to 4096, any n_groups that divides it, eps positive.
+ * C a multiple of 8 up to 4096, any n_groups that divides it, eps at least 2^-126.
  * workspace: dev, 256-byte aligned, at least dgq_group_norm_workspace_bytes(); contents undefined on entry and exit; calls that may
  * overlap on the GPU need separate ones.
  * Errors: INVALID_ARG (also: pixel rows of Y that overlap), ALIGNMENT, UNSUPPORTED (also: B > 65535, P > 2^30), WORKSPACE, CUDA. */
@@ -336,7 +336,8 @@ dgq_status dgq_group_norm(const dgq_rows* X, const void* add, int64_t ld_add, co
 dgq_status dgq_group_norm_quantize(const dgq_groups* g, int timestep, int layout, const dgq_rows* X, const void* add,
                                    int64_t ld_add, const float* gamma, const float* beta, int dtype, int B, int P, int n_groups,
                                    float eps, int act, void* Xq, void* workspace, size_t workspace_bytes, void* stream);
-dgq_status dgq_group_norm_workspace_bytes(int B, int P, int C, int n_groups, size_t* bytes);
+/* Bytes for dgq_group_norm (quantize 0; 0 where the map is held on the chip: workspace may be NULL then) or dgq_group_norm_quantize. */
+dgq_status dgq_group_norm_workspace_bytes(int B, int P, int C, int n_groups, int quantize, size_t* bytes);
 
 /* A 4-bit weight whose scales each serve one output and `group` (32, 64 or 128) neighbouring input channels, for products with few
  * 16-bit rows (time embeddings, single tokens).  Library-owned; every call but _destroy synchronises with the host. */

@@ -378,9 +378,10 @@ def cached_attn(Q, cache: KvCache, block_table, kv_lens, q_start=None, max_nq=No
     return r
 
 
-def group_norm_workspace_bytes(B, P, C_, n_groups) -> int:
+def group_norm_workspace_bytes(B, P, C_, n_groups, quantize=False) -> int:
     n = C.c_size_t(0)
-    _check(lib().dgq_group_norm_workspace_bytes(C.c_int(B), C.c_int(P), C.c_int(C_), C.c_int(n_groups), C.byref(n)), "dgq_group_norm_workspace_bytes")
+    _check(lib().dgq_group_norm_workspace_bytes(C.c_int(B), C.c_int(P), C.c_int(C_), C.c_int(n_groups), C.c_int(bool(quantize)), C.byref(n)),
+           "dgq_group_norm_workspace_bytes")
     return n.value
 
 

@@ -615,7 +615,7 @@ bool norm_args(PyObject* const* a, NormArgs* n) {
   return true;
 }
 // The workspace of a call: the caller's, or one of the size the library asks for.
-bool norm_workspace(PyObject* given, const NormArgs& n, PyObject* stream, void* st, at::Tensor* ws, dgq_status* rc) {
+bool norm_workspace(PyObject* given, const NormArgs& n, int quantize, PyObject* stream, void* st, at::Tensor* ws, dgq_status* rc) {
   *rc = DGQ_OK;
   if (!tensor(given, ws)) return false;
   if (ws->defined()) {
@@ -623,8 +623,8 @@ bool norm_workspace(PyObject* given, const NormArgs& n, PyObject* stream, void* 
     return true;
   }
   size_t need = 0;
-  *rc = dgq_group_norm_workspace_bytes(n.B, n.P, n.C, n.n_groups, &need);
-  if (*rc == DGQ_OK) *ws = scratch(static_cast<int64_t>(need), n.x, stream, st);
+  *rc = dgq_group_norm_workspace_bytes(n.B, n.P, n.C, n.n_groups, quantize, &need);
+  if (*rc == DGQ_OK && need) *ws = scratch(static_cast<int64_t>(need), n.x, stream, st);
   return true;
 }
 
@@ -646,12 +646,12 @@ PyObject* group_norm(PyObject* const* a, Py_ssize_t n) {
   if (!map16(y, x.x, "out is a map like X", &ry, &pixels) || (y.sizes() != x.x.sizes() && !fail("out is a map like X"))) return nullptr;
   if (y.numel() == 0) return output(a[7], y);
   dgq_status rc;
-  if (!norm_workspace(a[8], x, a[9], st, &ws, &rc)) return nullptr;
+  if (!norm_workspace(a[8], x, 0, a[9], st, &ws, &rc)) return nullptr;
   if (rc != DGQ_OK) return status(rc);
   const int type = dtype_of(x.x);
   void *p_add = ptr(x.add), *p_ws = ptr(ws);
   const float *p_gamma = ptr<float>(x.gamma), *p_beta = ptr<float>(x.beta);
-  const size_t bytes = ws.nbytes();
+  const size_t bytes = ws.defined() ? ws.nbytes() : 0;
   Py_BEGIN_ALLOW_THREADS
   rc = dgq_group_norm(&x.rx, p_add, x.ld_add, p_gamma, p_beta, &ry, type, x.B, x.P, x.C, x.n_groups, x.eps, x.act, p_ws, bytes, st);
   Py_END_ALLOW_THREADS
@@ -682,12 +682,12 @@ PyObject* group_norm_quantize(PyObject* const* a, Py_ssize_t n) {
     return nullptr;
   if (rows == 0) return output(a[12], xq);
   dgq_status rc;
-  if (!norm_workspace(a[13], x, a[14], st, &ws, &rc)) return nullptr;
+  if (!norm_workspace(a[13], x, 1, a[14], st, &ws, &rc)) return nullptr;
   if (rc != DGQ_OK) return status(rc);
   const int type = dtype_of(x.x);
   void *p_add = ptr(x.add), *p_ws = ptr(ws), *p_xq = ptr(xq);
   const float *p_gamma = ptr<float>(x.gamma), *p_beta = ptr<float>(x.beta);
-  const size_t bytes = ws.nbytes();
+  const size_t bytes = ws.defined() ? ws.nbytes() : 0;
   Py_BEGIN_ALLOW_THREADS
   rc = dgq_group_norm_quantize(static_cast<const dgq_groups*>(g), timestep, layout, &x.rx, p_add, x.ld_add, p_gamma, p_beta, type, x.B, x.P,
                                x.n_groups, x.eps, x.act, p_xq, p_ws, bytes, st);

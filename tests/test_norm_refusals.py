@@ -11,7 +11,7 @@ WORKSPACE = 4
 BIG = 1 << 24
 
 
-def norm(X=None, add=None, ld_add=64, gamma=None, beta=None, Y=None, dtype=0, B=2, P=10, c=64, groups=8, eps=1e-5, act=0, ws=PTR, size=BIG):
+def norm(X=None, add=None, ld_add=64, gamma=None, beta=None, Y=None, dtype=0, B=2, P=1 << 20, c=64, groups=8, eps=1e-5, act=0, ws=PTR, size=BIG):
     X, Y = X or rows(), Y or rows()
     return b.lib().dgq_group_norm(C.byref(X), C.c_void_p(add), C.c_int64(ld_add), C.c_void_p(gamma), C.c_void_p(beta), C.byref(Y), dtype, B, P, c, groups,
                                   C.c_float(eps), act, C.c_void_p(ws), C.c_size_t(size), None)
@@ -31,17 +31,18 @@ def test_group_norm(change, status):
 
 
 def test_workspace_bytes():
-    def need(B, P, c, groups):
+    def need(B, P, c, groups, quantize=1):
         n = C.c_size_t(7)
-        return b.lib().dgq_group_norm_workspace_bytes(B, P, c, groups, C.byref(n)), n.value
+        return b.lib().dgq_group_norm_workspace_bytes(B, P, c, groups, quantize, C.byref(n)), n.value
 
     assert need(2, 4096, 320, 32)[0] == 0 and 0 < need(2, 4096, 320, 32)[1] <= 1 << 20
+    assert need(2, 64, 1280, 32, 0) == (0, 0) and need(1, 1 << 18, 128, 32, 0)[1] > 0
     for bad in ((0, 1, 8, 1), (1, 0, 8, 1), (1, 1, 0, 1), (1, 1, 8, 0), (1, 1, 8, 3)):
         assert need(*bad)[0] == INVALID
-    assert b.lib().dgq_group_norm_workspace_bytes(1, 1, 8, 1, None) == INVALID
+    assert need(1, 1, 12, 1)[0] == UNSUPPORTED and need(1, 1, 4104, 1)[0] == UNSUPPORTED
+    assert b.lib().dgq_group_norm_workspace_bytes(1, 1, 8, 1, 1, None) == INVALID
     for B in (1, 7, 300, 65535):
-        n = C.c_size_t(0)
-        assert b.lib().dgq_group_norm_workspace_bytes(B, 1000, 64, 8, C.byref(n)) == 0 and n.value >= B * 8 * 16
+        assert need(B, 1000, 64, 8)[1] >= B * 8 * 16
 
 
 def test_codes():
