@@ -19,7 +19,7 @@ struct dgq_few_weight {
   int tiles = 0, blocks = 0, n_groups = 0;  // ceil(N / 16), ceil(K / 64), ceil(K / group)
   unsigned char* d_slab = nullptr;
   uint4* d_codes = nullptr;     // [tiles][blocks][32]
-  uint32_t* d_scale = nullptr;  // [tiles][scale columns][8]: fp16 scales of outputs r and r + 8
+  uint32_t* d_scale = nullptr;  // [tiles][scale columns][8]: fp16 scales of outputs r and r + 8 (groups of 32: [tiles][blocks][8][2])
   int device = 0;
 };
 
@@ -30,6 +30,14 @@ constexpr int FEW_MOST_ROWS = (1 << 21) - 32;  // 65535 times 32
 
 // Scale columns of a tile: the groups of whole blocks (a group of 128 has two blocks).
 __host__ __device__ inline int few_columns(int blocks, int group) { return group == 32 ? 2 * blocks : group == 64 ? blocks : (blocks + 1) / 2; }
+
+// Place of a scale in a tile's columns, in pairs of fp16.
+__host__ __device__ inline int few_scale_place(int column, int r, int group) {
+  return group == 32 ? ((column >> 1) * 8 + r) * 2 + (column & 1) : column * 8 + r;
+}
+// A warp may read this many blocks behind the end of a tile (the rows are zeros there): the next tile's, or what lies behind the last one,
+// of which the scales are zeros.
+constexpr int FEW_BEYOND = 64;
 
 #ifdef __CUDACC__
 
@@ -101,7 +109,7 @@ __global__ void __launch_bounds__(256) few_pack_kernel(const FewPackArgs a) {
   if (block < a.blocks) a.codes[((size_t)blockIdx.y * a.blocks + block) * 128 + (tid & 127)] = words[tid >> 7][tid & 127];
   const int column = k0 / a.group;
   if ((tid & 15) % per == 0 && column < a.columns)
-    a.scale_out[((size_t)blockIdx.y * a.columns + column) * 16 + (r & 7) * 2 + (r >> 3)] = in ? s : __ushort_as_half(0);
+    a.scale_out[((size_t)blockIdx.y * a.columns * 8 + few_scale_place(column, r & 7, a.group)) * 2 + (r >> 3)] = in ? s : __ushort_as_half(0);
 }
 
 // ------------------------------------------------------------------ products
@@ -114,9 +122,10 @@ struct FewArgs {
   uint16_t* Y;
   int64_t ldy;
   int M, N, K, blocks, columns, tiles;
+  int log_columns;  // 1 where two blocks share a scale column (groups of 128)
+  int silu;
+  int log_wk, wn;   // warps of a block: 2^log_wk along the input channels, wn along the outputs
 };
-
-constexpr int FEW_WARPS = 8;
 
 // Codes -> two 16-bit floats each.  fp16: 1024 + q has q in its low bits, 1024 + 16 q in bits 4 to 7.  bf16: 128 + q.
 template <bool BF>
@@ -153,89 +162,222 @@ __device__ __forceinline__ void few_mma(float (&d)[4], const uint32_t (&a)[4], u
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// NT tiles of outputs and MT times eight rows for a block, whose warps take every eighth block of 64 channels.
-template <bool BF, bool SILU, int GROUP, int NT, int MT>
-__global__ void __launch_bounds__(FEW_WARPS * 32) few_kernel(const __grid_constant__ FewArgs a) {
-  __shared__ float part[FEW_WARPS][MT * 8][NT * 16];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-  const int tile0 = blockIdx.x * NT, m0 = blockIdx.y * MT * 8;
-  pdl_launch_dependents();
-  pdl_wait();
-  float acc[NT][MT][4] = {};
-#pragma unroll 2
-  for (int kb = warp; kb < a.blocks; kb += FEW_WARPS) {
-    uint4 w[NT];
-    uint32_t s[NT][2];
+// the same from zero
+template <bool BF>
+__device__ __forceinline__ void few_mma_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if (BF)
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+// The warps' parts of a block's outputs, joined in a fixed order in shared memory, [2^log_wk][rows][outputs], and stored.
+template <bool BF, int MT>
+__device__ __forceinline__ void few_join(const FewArgs& a, unsigned char* smem, const float* acc, int wk, int wn, int rows, int m0) {
+  const int tid = threadIdx.x, n_threads = blockDim.x, r = (tid & 31) >> 2, c = tid & 3, width = a.wn * 16;
+  float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const int tile = min(tile0 + t, a.tiles - 1);
-      w[t] = __ldg(a.codes + ((size_t)tile * a.blocks + kb) * 32 + lane);
-      const uint32_t* sc = a.scale + (size_t)tile * a.columns * 8 + r;
-      if (GROUP == 32) {
-        s[t][0] = __ldg(sc + kb * 16);
-        s[t][1] = __ldg(sc + kb * 16 + 8);
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = 8 * m + 2 * c + (i & 1);
+      if (row < rows) part[(wk * rows + row) * width + wn * 16 + r + (i & 2) * 4] = acc[m * 4 + i];
+    }
+  __syncthreads();
+  const float per_width = 1.f / (float)width;
+  for (int i = tid; i < rows * width; i += n_threads) {
+    const int m = gn_div(i, per_width), o = i - m * width, n = blockIdx.x * width + o;
+    if (n >= a.N) continue;
+    float y = 0.f;
+    for (int k = 0; k < 1 << a.log_wk; ++k) y += part[(k * rows + m) * width + o];
+    if (a.bias) y += gn_up(a.bias[n], BF);
+    a.Y[(m0 + m) * a.ldy + n] = (uint16_t)pack16<BF>(y, 0.f);
+  }
+}
+
+// Up to eight rows as they are: a block has one tile, its warps split the input channels (four neighbouring blocks of 64 of a chunk for each),
+// and every lane reads its part of its row straight from memory, which the multiprocessor's blocks do at about the same time, a block of 64 ahead;
+// weights are asked for four blocks ahead.  Without barriers and shared memory as many warps are there as registers allow (7 x 5000 x 10007:
+// with the rows in shared memory, three chunks of 4 x 4 blocks, 17 us).
+template <bool BF, bool G32>
+__global__ void __launch_bounds__(512, 2) few_rows_kernel(const __grid_constant__ FewArgs a) {
+  extern __shared__ __align__(16) unsigned char few_smem[];
+  const int tid = threadIdx.x, wk = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3, tile = blockIdx.x;
+  const int per_chunk = 4 << a.log_wk, chunks = (a.blocks + per_chunk - 1) >> (2 + a.log_wk);
+  uint4 w[4];
+  uint2 s[4];
+  const uint4* codes = a.codes + ((size_t)tile * a.blocks + wk * 4) * 32 + lane;
+  const uint32_t* scales = a.scale + (size_t)tile * a.columns * 8 + (G32 ? (wk * 4 * 8 + r) * 2 : (wk * 4 >> a.log_columns) * 8 + r);
+  const int scale_step = G32 ? per_chunk * 16 : (per_chunk >> a.log_columns) * 8;
+  auto weights = [&](int i) {
+    w[i] = __ldg(codes + i * 32);
+    if (G32) s[i] = __ldg(reinterpret_cast<const uint2*>(scales + i * 16));
+    else s[i].x = __ldg(scales + (a.log_columns ? i >> 1 : i) * 8);
+  };
+  // (columns behind the last row are worked out and dropped)
+  const uint16_t* row = a.X + min(r, a.M - 1) * a.ldx + wk * 256 + c * 8;
+  int left = a.K - wk * 256 - c * 8;  // channels from this lane's first one to the end of the row
+  uint4 x[2][2];
+  auto rows = [&](int i) {
+    const uint4 none = make_uint4(0, 0, 0, 0);
+    x[i & 1][0] = i * 64 < left ? __ldg(reinterpret_cast<const uint4*>(row + i * 64)) : none;
+    x[i & 1][1] = i * 64 + 32 < left ? __ldg(reinterpret_cast<const uint4*>(row + i * 64 + 32)) : none;
+  };
+  float acc[4] = {};
+  // the weight is the caller's own object, complete since it was made: asked for before the kernel in front has ended
+#pragma unroll
+  for (int i = 0; i < 4; ++i) weights(i);
+  pdl_wait();
+  rows(0);
+  for (int ch = 0; ch < chunks; ++ch) {
+    codes += per_chunk * 32, scales += scale_step;  // those of the next chunk
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (i < 3) {
+        rows(i + 1);
+      } else if (ch + 1 < chunks) {
+        row += per_chunk * 64, left -= per_chunk * 64;
+        rows(0);
       } else {
-        s[t][0] = __ldg(sc + (GROUP == 64 ? kb : kb >> 1) * 8);
+        pdl_launch_dependents();
+      }
+      const uint32_t words[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+      const uint4 x0 = x[i & 1][0], x1 = x[i & 1][1];
+      const uint32_t b[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+      float d[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t op[4];
+        few_widen<BF>(words[j], op);
+        if (j == 0 || (G32 && j == 2)) few_mma_first<BF>(d, op, b[2 * j], b[2 * j + 1]);
+        else few_mma<BF>(d, op, b[2 * j], b[2 * j + 1]);
+        if (j == 3 || (G32 && j == 1)) {
+          const uint32_t pair = G32 && j == 3 ? s[i].y : s[i].x;
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&pair));
+          acc[0] = fmaf(d[0], f.x, acc[0]);
+          acc[1] = fmaf(d[1], f.x, acc[1]);
+          acc[2] = fmaf(d[2], f.y, acc[2]);
+          acc[3] = fmaf(d[3], f.y, acc[3]);
+        }
+      }
+      if (ch + 1 < chunks) weights(i);
+    }
+  }
+  few_join<BF, 1>(a, few_smem, acc, wk, 0, a.M, 0);
+}
+
+// A block has wn tiles of outputs and MT times eight rows.  Its warps split the input channels (2^log_wk ways, every warp four neighbouring blocks
+// of 64 of a chunk) and the tiles; the rows of a chunk stand in shared memory for all of them, three chunks in turn, so that one barrier a chunk is
+// enough.  A warp's weights are asked for a chunk ahead, in registers.
+template <bool BF, bool G32, int MT>
+__global__ void __launch_bounds__(512) few_kernel(const __grid_constant__ FewArgs a) {
+  extern __shared__ __align__(16) unsigned char few_smem[];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
+  const int wk = warp & ((1 << a.log_wk) - 1), wn = warp >> a.log_wk;
+  const int tile = min((int)blockIdx.x * a.wn + wn, a.tiles - 1), m0 = blockIdx.y * MT * 8, rows = min(MT * 8, a.M - m0);
+  const int per_chunk = 4 << a.log_wk, chunks = (a.blocks + per_chunk - 1) >> (2 + a.log_wk);
+  const int pitch = per_chunk * 128 + 64, set = rows * pitch;  // bytes; rows start in different halves of the banks
+  uint4 w[4];
+  uint2 s[4];
+  const uint4* codes = a.codes + ((size_t)tile * a.blocks + wk * 4) * 32 + lane;
+  const uint32_t* scales = a.scale + (size_t)tile * a.columns * 8 + (G32 ? (wk * 4 * 8 + r) * 2 : (wk * 4 >> a.log_columns) * 8 + r);
+  const int scale_step = G32 ? per_chunk * 16 : (per_chunk >> a.log_columns) * 8;
+  auto weights = [&](int i) {
+    w[i] = __ldg(codes + i * 32);
+    if (G32) s[i] = __ldg(reinterpret_cast<const uint2*>(scales + i * 16));
+    else s[i].x = __ldg(scales + (a.log_columns ? i >> 1 : i) * 8);
+  };
+  // Rows of chunk `ch` into shared memory, eight channels (which are in or out as a whole) of every wn-th row for a thread.
+  const int piece = tid & ((32 << a.log_wk) - 1);
+  auto stage = [&](int ch, int buffer) {
+    const int k = (ch * per_chunk * 8 + piece) * 8;
+    const bool in = k < a.K;
+    const uint16_t* src = a.X + (m0 + wn) * a.ldx + (in ? k : 0);
+    uint32_t to = smem_u32(few_smem) + buffer * set + wn * pitch + piece * 16;
+    for (int row = wn; row < rows; row += a.wn, src += a.wn * a.ldx, to += a.wn * pitch) {
+      if (!a.silu) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(src), "r"(in ? 16 : 0) : "memory");
+      } else {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (in) {
+          x = __ldg(reinterpret_cast<const uint4*>(src));
+          uint32_t* h = reinterpret_cast<uint32_t*>(&x);
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            const float2 f = unpack16<BF>(h[z]);
+            h[z] = pack16<BF>(gn_silu(f.x), gn_silu(f.y));
+          }
+        }
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
       }
     }
-    uint32_t x[MT][8];
+  };
+  // where this lane's part of the rows lies (columns behind the last row are worked out and dropped)
+  int mine[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const int row = m0 + 8 * m + r, k = kb * 64 + 8 * c;
-      const uint4* src = reinterpret_cast<const uint4*>(a.X + row * a.ldx + k);
-      const uint4 z = make_uint4(0, 0, 0, 0);
-      const uint4 x0 = row < a.M && k < a.K ? __ldg(src) : z, x1 = row < a.M && k + 32 < a.K ? __ldg(src + 4) : z;
-      x[m][0] = x0.x, x[m][1] = x0.y, x[m][2] = x0.z, x[m][3] = x0.w;
-      x[m][4] = x1.x, x[m][5] = x1.y, x[m][6] = x1.z, x[m][7] = x1.w;
-      if (SILU)
+  for (int m = 0; m < MT; ++m) mine[m] = min(8 * m + r, rows - 1) * pitch + c * 16 + wk * 512;
+  float acc[MT][4] = {};
+  // the weight is the caller's own object, complete since it was made: asked for before the kernel in front has ended
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float2 f = unpack16<BF>(x[m][i]);
-          x[m][i] = pack16<BF>(gn_silu(f.x), gn_silu(f.y));
-        }
-    }
+  for (int i = 0; i < 4; ++i) weights(i);
+  pdl_wait();
+  stage(0, 0);
+  asm volatile("cp.async.commit_group;" ::: "memory");
+  if (chunks > 1) stage(1, 1);
+  asm volatile("cp.async.commit_group;" ::: "memory");
+  int buffer = 0;
+  for (int ch = 0; ch < chunks; ++ch) {
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
+    __syncthreads();  // chunk ch is there, and everybody is done with the one before, whose place the one after the next takes
+    const int free = buffer == 0 ? 2 : buffer - 1;
+    if (ch + 2 < chunks) stage(ch + 2, free);
+    else pdl_launch_dependents();
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    const unsigned char* from = few_smem + buffer * set;
+    buffer = buffer == 2 ? 0 : buffer + 1;
+    codes += per_chunk * 32, scales += scale_step;  // those of the next chunk
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      const uint32_t words[4] = {w[t].x, w[t].y, w[t].z, w[t].w};
+    for (int i = 0; i < 4; ++i) {
+      uint32_t x[MT][8];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const uint4* p = reinterpret_cast<const uint4*>(from + mine[m] + i * 128);
+        const uint4 x0 = p[0], x1 = p[4];
+        x[m][0] = x0.x, x[m][1] = x0.y, x[m][2] = x0.z, x[m][3] = x0.w;
+        x[m][4] = x1.x, x[m][5] = x1.y, x[m][6] = x1.z, x[m][7] = x1.w;
+      }
+      const uint32_t words[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
       float d[MT][4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         uint32_t op[4];
         few_widen<BF>(words[j], op);
-        if (j == 0 || (GROUP == 32 && j == 2))
 #pragma unroll
-          for (int m = 0; m < MT; ++m) d[m][0] = d[m][1] = d[m][2] = d[m][3] = 0.f;
-#pragma unroll
-        for (int m = 0; m < MT; ++m) few_mma<BF>(d[m], op, x[m][2 * j], x[m][2 * j + 1]);
-        if (j == 3 || (GROUP == 32 && j == 1)) {
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&s[t][GROUP == 32 ? j >> 1 : 0]));
+        for (int m = 0; m < MT; ++m) {
+          if (j == 0 || (G32 && j == 2)) few_mma_first<BF>(d[m], op, x[m][2 * j], x[m][2 * j + 1]);
+          else few_mma<BF>(d[m], op, x[m][2 * j], x[m][2 * j + 1]);
+        }
+        if (j == 3 || (G32 && j == 1)) {
+          const uint32_t pair = G32 && j == 3 ? s[i].y : s[i].x;
+          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&pair));
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
-            acc[t][m][0] = fmaf(d[m][0], f.x, acc[t][m][0]);
-            acc[t][m][1] = fmaf(d[m][1], f.x, acc[t][m][1]);
-            acc[t][m][2] = fmaf(d[m][2], f.y, acc[t][m][2]);
-            acc[t][m][3] = fmaf(d[m][3], f.y, acc[t][m][3]);
+            acc[m][0] = fmaf(d[m][0], f.x, acc[m][0]);
+            acc[m][1] = fmaf(d[m][1], f.x, acc[m][1]);
+            acc[m][2] = fmaf(d[m][2], f.y, acc[m][2]);
+            acc[m][3] = fmaf(d[m][3], f.y, acc[m][3]);
           }
         }
       }
+      if (ch + 1 < chunks) weights(i);
     }
   }
-#pragma unroll
-  for (int t = 0; t < NT; ++t)
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) part[warp][8 * m + 2 * c + (i & 1)][16 * t + r + (i & 2) * 4] = acc[t][m][i];
-  __syncthreads();
-  for (int i = threadIdx.x; i < MT * 8 * NT * 16; i += FEW_WARPS * 32) {
-    const int m = i / (NT * 16), o = i - m * (NT * 16), row = m0 + m, n = tile0 * 16 + o;
-    if (row >= a.M || n >= a.N) continue;
-    float y = 0.f;
-#pragma unroll
-    for (int k = 0; k < FEW_WARPS; ++k) y += part[k][m][o];
-    if (a.bias) y += gn_up(a.bias[n], BF);
-    a.Y[row * a.ldy + n] = (uint16_t)pack16<BF>(y, 0.f);
-  }
+  __syncthreads();  // the rows' places are free
+  few_join<BF, MT>(a, few_smem, &acc[0][0], wk, wn, rows, m0);
 }
 #endif
 
@@ -254,19 +396,21 @@ static dgq_status few_build(const __half* W, const int8_t* wq, const __half* sca
   w->n_groups = (K + group - 1) / group;
   const int columns = few_columns(w->blocks, group);
   const size_t code_bytes = (size_t)w->tiles * w->blocks * 512, scale_bytes = ((size_t)w->tiles * columns * 32 + 255) / 256 * 256;
+  const size_t beyond = FEW_BEYOND * 512;  // of codes; of scales at most an eighth of it
   dgq_status st = DGQ_OK;
   auto ok = [&](cudaError_t e) {
     if (st == DGQ_OK && e != cudaSuccess) st = DGQ_ERR_CUDA;
     return st == DGQ_OK;
   };
   int bad = 0;
-  if (ok(cudaGetDevice(&w->device)) && ok(pool_alloc((void**)&w->d_slab, code_bytes + scale_bytes + 256, stream))) {
+  if (ok(cudaGetDevice(&w->device)) && ok(pool_alloc((void**)&w->d_slab, code_bytes + scale_bytes + beyond + 256, stream))) {
     w->d_codes = reinterpret_cast<uint4*>(w->d_slab);
     w->d_scale = reinterpret_cast<uint32_t*>(w->d_slab + code_bytes);
-    int* d_bad = reinterpret_cast<int*>(w->d_slab + code_bytes + scale_bytes);
+    int* d_bad = reinterpret_cast<int*>(w->d_slab + code_bytes + scale_bytes + beyond);
     FewPackArgs a = {W, wq, scales, N, K, group, w->n_groups, w->blocks, columns, reinterpret_cast<uint32_t*>(w->d_codes),
                      reinterpret_cast<__half*>(w->d_scale), d_bad};
-    if (ok(cudaMemsetAsync(d_bad, 0, sizeof(int), stream))) {
+    const size_t scale_end = code_bytes + (size_t)w->tiles * columns * 32;
+    if (ok(cudaMemsetAsync(w->d_slab + scale_end, 0, code_bytes + scale_bytes + beyond + sizeof(int) - scale_end, stream))) {
       few_pack_kernel<<<dim3((w->blocks + 1) / 2, w->tiles), 256, 0, stream>>>(a);
       g_launches += 1;
       ok(cudaGetLastError());
@@ -284,19 +428,57 @@ static dgq_status few_build(const __half* W, const int8_t* wq, const __half* sca
   return DGQ_OK;
 }
 
-template <bool BF, bool SILU, int GROUP, int NT>
-static dgq_status few_launch(const FewArgs& a, cudaStream_t stream) {
-  const int mt = std::min((a.M + 7) / 8, 4);
-  const dim3 grid((a.tiles + NT - 1) / NT, (a.M + mt * 8 - 1) / (mt * 8));
-  auto kernel = mt == 1 ? few_kernel<BF, SILU, GROUP, NT, 1> : mt == 2 ? few_kernel<BF, SILU, GROUP, NT, 2>
-              : mt == 3 ? few_kernel<BF, SILU, GROUP, NT, 3> : few_kernel<BF, SILU, GROUP, NT, 4>;
-  DGQ_CUDA_OK(launch_pdl(kernel, grid, dim3(FEW_WARPS * 32), 0, stream, a));
+// How a product is dealt out: warps along the input channels (a power of two) and along the outputs, eights of rows.
+struct FewPlan {
+  int log_wk, wn, mt;
+  size_t smem;
+};
+static FewPlan few_plan(int M, int tiles, int blocks) {
+  FewPlan p;
+  p.mt = M <= 8 ? 1 : M <= 16 ? 2 : 4;
+  const int rows = std::min(M, p.mt * 8);
+  const int64_t units = (int64_t)tiles * ((M + p.mt * 8 - 1) / (p.mt * 8));
+  // sixteen warps for each multiprocessor where the weights' bytes are waited for, eight where 32 rows keep the matrix unit busy; four
+  // blocks of 64 channels for a warp at least
+  p.log_wk = 0;
+  const int most = p.mt == 4 ? 2 : p.mt == 2 ? 3 : 4, warps = p.mt == 4 ? 8 : p.mt == 2 ? 12 : 16;
+  while (p.log_wk < most && units << p.log_wk < warps * 148 && (4 << p.log_wk) < blocks) ++p.log_wk;
+  // Along the outputs, with more than eight rows, which would be read over and over: the most that fill the multiprocessors as evenly as any other
+  // number does, of at most 14 warps of a block.
+  p.wn = 1;
+  double best = 0.;
+  for (int wn = 1; p.mt > 1 && wn << p.log_wk <= 14; ++wn) {
+    const int64_t n = (units + wn - 1) / wn, rounds = (n + 147) / 148;
+    const double full = (double)units / (double)(rounds * 148 * wn);
+    if (full > 0.97 * best) best = std::max(best, full), p.wn = wn;
+  }
+  const int per_chunk = 4 << p.log_wk, sets = std::min((blocks + per_chunk - 1) / per_chunk, 3);
+  p.smem = std::max((size_t)sets * rows * (per_chunk * 128 + 64), (size_t)(1 << p.log_wk) * rows * p.wn * 16 * sizeof(float));
+  return p;
+}
+
+template <bool BF, bool G32, int MT>
+static dgq_status few_launch(const FewArgs& a, const FewPlan& p, cudaStream_t stream) {
+  static std::atomic<bool> done[64];
+  int dev = 0;
+  DGQ_CUDA_OK(cudaGetDevice(&dev));
+  if (dev >= 64 || !done[dev].load()) {
+    DGQ_CUDA_OK(cudaFuncSetAttribute(few_kernel<BF, G32, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 208 * 1024));
+    if (dev < 64) done[dev].store(true);
+  }
+  const dim3 grid((a.tiles + p.wn - 1) / p.wn, (a.M + MT * 8 - 1) / (MT * 8));
+  DGQ_CUDA_OK(launch_pdl(few_kernel<BF, G32, MT>, grid, dim3((p.wn << p.log_wk) * 32), p.smem, stream, a));
   g_launches += 1;
   return DGQ_OK;
 }
-template <bool BF, bool SILU>
-static dgq_status few_pick(const FewArgs& a, int group, cudaStream_t stream) {
-  return group == 32 ? few_launch<BF, SILU, 32, 1>(a, stream) : group == 64 ? few_launch<BF, SILU, 64, 1>(a, stream) : few_launch<BF, SILU, 128, 1>(a, stream);
+template <bool BF, bool G32>
+static dgq_status few_pick(const FewArgs& a, const FewPlan& p, cudaStream_t stream) {
+  if (p.mt == 1 && !a.silu) {
+    DGQ_CUDA_OK(launch_pdl(few_rows_kernel<BF, G32>, dim3(a.tiles), dim3(32 << p.log_wk), (size_t)(1 << p.log_wk) * a.M * 16 * sizeof(float), stream, a));
+    g_launches += 1;
+    return DGQ_OK;
+  }
+  return p.mt == 1 ? few_launch<BF, G32, 1>(a, p, stream) : p.mt == 2 ? few_launch<BF, G32, 2>(a, p, stream) : few_launch<BF, G32, 4>(a, p, stream);
 }
 
 }  // namespace dgq
@@ -345,7 +527,7 @@ extern "C" dgq_status dgq_few_weight_export(const dgq_few_weight* w, int8_t* wq,
       }
     if (scales)
       for (int g = 0; g < w->n_groups; ++g)
-        scales[(size_t)n * w->n_groups + g] = sc[((size_t)(n >> 4) * columns + g) * 16 + (n & 7) * 2 + ((n >> 3) & 1)];
+        scales[(size_t)n * w->n_groups + g] = sc[((size_t)(n >> 4) * columns * 8 + few_scale_place(g, n & 7, w->group)) * 2 + ((n >> 3) & 1)];
   }
   return DGQ_OK;
 }
@@ -361,9 +543,10 @@ extern "C" dgq_status dgq_linear_few(const dgq_few_weight* w, const void* X, int
   int dev = 0;
   DGQ_CUDA_OK(cudaGetDevice(&dev));
   if (dev != w->device) return DGQ_ERR_INVALID_ARG;
-  FewArgs a = {w->d_codes, w->d_scale, (const uint16_t*)X, M > 1 ? ldx : 0, (const uint16_t*)bias, (uint16_t*)Y, M > 1 ? ldy : 0,
-               M, w->N, w->K, w->blocks, few_columns(w->blocks, w->group), w->tiles};
+  const FewPlan p = few_plan(M, w->tiles, w->blocks);
+  const FewArgs a = {w->d_codes, w->d_scale, (const uint16_t*)X, M > 1 ? ldx : 0, (const uint16_t*)bias, (uint16_t*)Y, M > 1 ? ldy : 0, M, w->N, w->K,
+                     w->blocks, few_columns(w->blocks, w->group), w->tiles, w->group == 128, act == DGQ_ACT_SILU, p.log_wk, p.wn};
   const cudaStream_t s = (cudaStream_t)stream;
-  if (dtype == DGQ_BF16) return act == DGQ_ACT_SILU ? few_pick<true, true>(a, w->group, s) : few_pick<true, false>(a, w->group, s);
-  return act == DGQ_ACT_SILU ? few_pick<false, true>(a, w->group, s) : few_pick<false, false>(a, w->group, s);
+  if (dtype == DGQ_BF16) return w->group == 32 ? few_pick<true, true>(a, p, s) : few_pick<true, false>(a, p, s);
+  return w->group == 32 ? few_pick<false, true>(a, p, s) : few_pick<false, false>(a, p, s);
 }

@@ -14,6 +14,7 @@
 namespace dgq {
 
 constexpr int GN_MAX_C = 4096;
+constexpr int GN_MAX_CODE_GROUPS = 2048;  // into codes: what shared memory holds beside the widest row
 constexpr int GN_MAX_THREADS = 512;  // one thread for every eight channels of the widest row
 constexpr size_t GN_SMEM_MAX = 232448 - 8 * 1024;  // beside what a kernel declares
 
@@ -30,8 +31,9 @@ struct GnArgs {
   float per_nvec, per_cpg;  // 1 / nvec, 1 / cpg
   int lines;                // rows that a block has under way at a time
   float per_lines;          // 1 / lines
-  int log_cluster;          // one kernel: blocks of a cluster
+  int log_cluster;          // blocks of a cluster (one kernel, sums)
   int slab_rows, clusters;  // sums: rows of a block, clusters of an image
+  int early;                // sums: the second kernel's blocks may come in at once
   int rows;                 // values and codes: rows of a block
   float eps;
   double per_count;  // 1 / (P cpg)
@@ -387,11 +389,15 @@ template <bool BF, int SEG>
 __global__ void __launch_bounds__(GN_MAX_THREADS) gn_sums_kernel(const __grid_constant__ GnArgs a) {
   extern __shared__ __align__(16) unsigned char gn_smem[];
   const int tid = threadIdx.x, n_threads = blockDim.x, nv = a.nvec, lines = a.lines, b = blockIdx.y;
-  double2* own = reinterpret_cast<double2*>(gn_smem);  // [n_groups]
-  double2* parts = own + a.n_groups;                   // [SEG][lines][nv], in the ring's place
+  const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
+  const int S = 1 << a.log_cluster, rank = blockIdx.x & (S - 1), per_block = (a.n_groups + S - 1) >> a.log_cluster;
+  double2* all = reinterpret_cast<double2*>(gn_smem);  // [S][per_block] of the cluster's blocks, of the groups that this one joins
+  double2* parts = all + S * per_block;                // [SEG][lines][nv], in the ring's place
+  cluster.barrier_arrive();  // (waited for before the first access to another block's shared memory: it has started by then)
   const int p0 = min((int64_t)a.P, (int64_t)blockIdx.x * a.slab_rows), p1 = min((int64_t)a.P, (int64_t)p0 + a.slab_rows), used = min(lines, p1 - p0);
   const int line = gn_div(tid, a.per_nvec), v = tid - line * nv;
   const GnRing ring(parts, tid, n_threads);
+  if (a.early) pdl_launch_dependents();
   pdl_wait();
   double2 t[SEG];
 #pragma unroll
@@ -434,12 +440,13 @@ __global__ void __launch_bounds__(GN_MAX_THREADS) gn_sums_kernel(const __grid_co
       else t[1].x += s[i], t[1].y += q[i];
     }
   }
-  pdl_launch_dependents();
+  if (!a.early) pdl_launch_dependents();
   __syncthreads();  // the ring is empty
   if (line < used)
 #pragma unroll
     for (int i = 0; i < SEG; ++i) parts[(i * lines + line) * nv + v] = t[i];
   __syncthreads();
+  cluster.barrier_wait();
   const int log_width = gn_width(n_threads, a.n_groups), width = 1 << log_width, per_round = n_threads >> log_width;
   for (int g0 = 0; g0 < a.n_groups; g0 += per_round) {
     const int g = min(g0 + (tid >> log_width), a.n_groups - 1), sub = tid & (width - 1);
@@ -452,39 +459,38 @@ __global__ void __launch_bounds__(GN_MAX_THREADS) gn_sums_kernel(const __grid_co
       s += __shfl_xor_sync(0xffffffffu, s, o);
       q += __shfl_xor_sync(0xffffffffu, q, o);
     }
-    if (sub == 0) own[g] = make_double2(s, q);
+    // to the block that joins this group's: the groups are dealt out to the blocks of the cluster in turn
+    if (g0 + (tid >> log_width) < a.n_groups && sub == 0) *cluster.map_shared_rank(all + rank * per_block + (g >> a.log_cluster), g & (S - 1)) = make_double2(s, q);
   }
-  // the blocks of a cluster: every one joins its share of the groups
-  const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
-  const int S = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
   cluster.sync();
-  for (int g = rank + S * tid; g < a.n_groups; g += S * n_threads) {
-    double2 t[8];
-#pragma unroll
-    for (int r = 0; r < 8; ++r) t[r] = *cluster.map_shared_rank(own + g, min(r, S - 1));
-    double s = t[0].x, q = t[0].y;
-#pragma unroll
-    for (int r = 1; r < 8; ++r)
-      if (r < S) s += t[r].x, q += t[r].y;
-    a.part[((int64_t)b * a.clusters + blockIdx.x / S) * a.n_groups + g] = make_double2(s, q);
+  for (int i = tid, g = rank + (tid << a.log_cluster); g < a.n_groups; i += n_threads, g += n_threads << a.log_cluster) {
+    double2 t = all[i];
+    for (int r = 1; r < S; ++r) t.x += all[r * per_block + i].x, t.y += all[r * per_block + i].y;
+    a.part[((int64_t)b * a.clusters + (blockIdx.x >> a.log_cluster)) * a.n_groups + g] = t;
   }
-  cluster.sync();  // nobody leaves while its shared memory is being read
 }
 
 // Mean and 1 / sqrt(var + eps) of every group of image b, into `stat` [n_groups].  A negative difference of the sums (all values
 // equal) counts as 0, NaN stays NaN.
-__device__ __forceinline__ void gn_stats(const GnArgs& a, int b, double2* stat) {
+// `meanwhile` is called between the requests and their arrival: loads of its own come behind the few that everybody waits for.
+template <typename F>
+__device__ __forceinline__ void gn_stats(const GnArgs& a, int b, double2* stat, F meanwhile) {
   const int tid = threadIdx.x, n_threads = blockDim.x;
   const int log_width = gn_width(n_threads, a.n_groups), width = 1 << log_width, per_round = n_threads >> log_width;
   for (int g0 = 0; g0 < a.n_groups; g0 += per_round) {
     const int g = min(g0 + (tid >> log_width), a.n_groups - 1), sub = tid & (width - 1);
     double s = 0.0, q = 0.0;
     const double2* p = a.part + (int64_t)b * a.clusters * a.n_groups + g;
-#pragma unroll 4
-    for (int k = sub; k < a.clusters; k += width) {
-      const double2 t = p[(int64_t)k * a.n_groups];
-      s += t.x;
-      q += t.y;
+    double2 t[5];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) t[i] = sub + i * width < a.clusters ? p[(int64_t)(sub + i * width) * a.n_groups] : make_double2(0.0, 0.0);
+    if (g0 == 0) meanwhile();
+#pragma unroll
+    for (int i = 0; i < 5; ++i) s += t[i].x, q += t[i].y;
+    for (int k = sub + 5 * width; k < a.clusters; k += width) {
+      const double2 u = p[(int64_t)k * a.n_groups];
+      s += u.x;
+      q += u.y;
     }
     for (int o = width >> 1; o > 0; o >>= 1) {
       s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -517,11 +523,12 @@ __global__ void __launch_bounds__(GN_MAX_THREADS) gn_values_kernel(const __grid_
   const int rows = line < lines && p0 + line < p1 ? (p1 - p0 - line + lines - 1) / lines : 0;
   const int64_t step = lines * a.xp;
   const uint16_t* src = a.X + (int64_t)b * a.xb + (p0 + line) * a.xp + v * 8;
-#pragma unroll
-  for (int k = 0; k < GN_RING - 1; ++k, src += step) ring.request(k, src, k < rows);
   GnEight own;
   if (rows > 0) own.request_scale(a, v * 8), own.request_add(a, b, v * 8);
-  gn_stats(a, b, stat);
+  gn_stats(a, b, stat, [&]() {
+#pragma unroll
+    for (int k = 0; k < GN_RING - 1; ++k, src += step) ring.request(k, src, k < rows);
+  });
   if (rows == 0) return;
   unsigned long long shift[4], factor[4], beta[4];
 #pragma unroll
@@ -605,21 +612,26 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
   __shared__ uint2 list[GN_LIST];  // first row, first channel
   __shared__ int listed;
   __shared__ unsigned int widest;  // (ROWS) the largest fixed part, as bits
+  __shared__ int n_pads;           // (ROWS)
   const int tid = threadIdx.x, n_threads = blockDim.x, nv = a.nvec, b = blockIdx.y;
   const int set_words = a.quads * a.K_pad;
   uint32_t* words = reinterpret_cast<uint32_t*>(gn_smem);                                   // [buffers][quads][K_pad], K_pad a multiple of 32
   double2* stat = reinterpret_cast<double2*>(words + (size_t)a.buffers * set_words);         // [n_groups]
-  // [4][4][nv], of channels 2 i and 2 i + 1: shift, factor | beta, places in bytes (16 bits each), limits (16 bits each; ROWS: groups) |
+  // [4][4][nv], of channels 2 i and 2 i + 1: shift, factor | beta, places in bytes (16 bits each), groups (later, unless ROWS: limits) |
   // -log2 e over the scale of the factor, -lo / L | what takes the zero-points out of four codes, bias, -
   // Factor and beta have 1 / (s L) in them unless ROWS, and beta has -lo / L where there is no SiLU.
   float4* chan = reinterpret_cast<float4*>(stat + a.n_groups);
   float4* cell = chan + 4 * 4 * nv;  // [R][G] 1 / (s L), -lo / L, 1 / s (ROWS, later: w), Z
+  // ROWS: [2][4 quads] first cell of each row of a round; places of padding in bytes, groups << 16
+  int* row_cells = reinterpret_cast<int*>(cell + a.R * a.G);
+  uint32_t* pads = reinterpret_cast<uint32_t*>(row_cells + 8 * a.quads);
   const int L = (1 << a.bits) - 1;
   const float Lf = (float)L, per_L = __fdividef(1.f, Lf);
   const bool centred = a.centred;
   const int p0 = (int)(gridDim.x - 1 - blockIdx.x) * a.rows, p1 = min(a.P, p0 + a.rows);
   const int64_t row0 = (int64_t)b * a.P;
-  if (tid == 0) listed = 0, widest = 0;
+  if (tid == 0) listed = 0, widest = 0, n_pads = 0;
+  if (ROWS) __syncthreads();
 #pragma unroll 4
   for (int i = tid; i < a.R * a.G; i += n_threads) {
     const int z = __ldg(a.zp + i);
@@ -634,8 +646,10 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
     const int c = __ldg(a.perm + i), g = __ldg(a.chunk_group + (i >> 4));
     if (c >= 0) {
       place_of(c) = (uint16_t)(4 * gn_shuffle(i));
-      if (ROWS) (&place_of(c))[2] = (uint16_t)g;
-    } else if (!ROWS) {  // padding: the clamped zero-point, 0 in the zero-centred layout
+      (&place_of(c))[2] = (uint16_t)g;
+    } else if (ROWS) {
+      pads[atomicAdd(&n_pads, 1)] = 4 * gn_shuffle(i) | g << 16;  // (in any order)
+    } else {  // padding: the clamped zero-point, 0 in the zero-centred layout
       const uint32_t w = centred ? 0u : 0x01010101u * (uint32_t)min(max(__ldg(a.zp + g), 0), L);
       for (int k = gn_shuffle(i); k < a.buffers * set_words; k += a.K_pad) words[k] = w;
     }
@@ -646,7 +660,7 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
   const bool active = quad < a.quads;
   const uint16_t* src = a.X + (int64_t)b * a.xb + (p0 + 4 * quad) * a.xp + v * 8;
   const int64_t src_step = 4 * a.quads * a.xp;
-  int position = 0, advance = 0;  // of the quad's first row among the pixel positions of the grouping
+  int position = 0, advance = 0, next = 0;  // of the quad's first row among the pixel positions of the grouping
   if (ROWS) {
     position = (int)((row0 + p0 + 4 * quad) % a.row_period);
     advance = 4 * a.quads % a.row_period;
@@ -660,46 +674,74 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
       w[j][0] = x.x, w[j][1] = x.y, w[j][2] = x.z, w[j][3] = x.w;
     }
     src += src_step;
+    if (ROWS && v == 0 && active) {
+      int at = position;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        row_cells[(next * a.quads + quad) * 4 + j] = __ldg(a.row_group + at) * a.G;
+        if (++at == a.row_period) at = 0;
+      }
+      position += advance;
+      if (position >= a.row_period) position -= a.row_period;
+      next ^= 1;
+    }
   };
   pdl_wait();
   {
-    GnEight own;
-    if (quad == 0) own.request_scale(a, v * 8), own.request_add(a, b, v * 8);
-    gn_stats(a, b, stat);  // (ends in a barrier: places and cells are set)
-    if (quad == 0)
+    // two neighbouring channels for a thread; what belongs to the first two pairs is asked for before the statistics are waited for
+    const int pairs = a.C >> 1;
+    float2 gamma[2], beta[2];
+    uint32_t add[2];
+    auto own = [&](int z, int pair) {
+      if (pair >= pairs) return;
+      const int c = 2 * pair;
+      gamma[z] = a.gamma ? make_float2(a.gamma[c], a.gamma[c + 1]) : make_float2(1.f, 1.f);
+      beta[z] = a.beta ? make_float2(a.beta[c], a.beta[c + 1]) : make_float2(0.f, 0.f);
+      const uint16_t* e = a.add + (int64_t)b * a.ld_add + c;
+      add[z] = a.add ? e[0] | (uint32_t)e[1] << 16 : 0u;
+    };
+    own(0, tid);
+    own(1, tid + n_threads);
+    gn_stats(a, b, stat, [&]() { request(p0 + 4 * quad); });  // (ends in a barrier: places and cells are set)
+    for (int pair = tid, z = 0; pair < pairs; pair += n_threads, ++z) {
+      if (z >= 2) own(0, pair);
+      const bool second = z == 1;
+      const int at = (pair & 3) * 4 * nv + (pair >> 2);
+      float4& one = chan[at + nv];
+      const uint32_t places = __float_as_uint(one.z), groups = __float_as_uint(one.w);
+      float t[2][6];  // shift, factor, beta, exponent's factor, -lo / L, zero-points
+      uint32_t w = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float t[2][7];  // shift, factor, beta, exponent's factor, -lo / L, w, zero-points
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int c = 2 * i + h;
-          const float2 k = gn_channel(own, stat[gn_div(v * 8 + c, a.per_cpg)], c, BF);
-          const float fixed = gn_fixed(k.x, k.y, own.beta[c]);
-          t[h][0] = k.x, t[h][1] = k.y, t[h][2] = own.beta[c];
-          t[h][3] = t[h][4] = t[h][5] = t[h][6] = 0.f;
-          if (ROWS) {
-            atomicMax(&widest, fixed < INFINITY ? __float_as_uint(fixed) : 0x7F800000u);  // (any order gives the same)
-          } else {
-            const float4 z = cell[__ldg(a.chunk_group + (place_of(v * 8 + c) >> 6))];
-            t[h][1] *= z.x;
-            t[h][2] = SILU ? own.beta[c] * z.x : fmaf(own.beta[c], z.x, z.y);
-            t[h][3] = __fdividef(-1.4426950408889634f, z.x);
-            t[h][4] = z.y;
-            t[h][5] = __uint_as_float(gn_limit<EIGHT>(z.z, -(float)__float_as_int(z.w), Lf, fixed));
-            t[h][6] = __uint_as_float(0x80808080u - 0x01010101u * __float_as_uint(z.w));
-          }
-        }
-        const uint32_t places = __float_as_uint(chan[(i * 4 + 1) * nv + v].z), w0 = __float_as_uint(t[0][5]), w1 = __float_as_uint(t[1][5]);
-        chan[i * 4 * nv + v] = make_float4(t[0][0], t[1][0], t[0][1], t[1][1]);
-        // one limit for both channels
-        const uint32_t w = max(w0, w1), below = min(gn_below<EIGHT>(w), 0xFFFFu);
-        float4& one = chan[(i * 4 + 1) * nv + v];
-        one = make_float4(t[0][2], t[1][2], __uint_as_float(places), ROWS ? one.w : __uint_as_float(below | below << 16));
-        if (!ROWS) {
-          chan[(i * 4 + 2) * nv + v] = make_float4(t[0][3], t[1][3], t[0][4], t[1][4]);
-          chan[(i * 4 + 3) * nv + v] = make_float4(t[0][6], t[1][6], gn_bias<EIGHT>(w), 0.f);
+      for (int h = 0; h < 2; ++h) {
+        const double2 st = stat[gn_div(2 * pair + h, a.per_cpg)];
+        const float2 g2 = second ? gamma[1] : gamma[0], b2 = second ? beta[1] : beta[0];
+        const uint32_t e2 = second ? add[1] : add[0];
+        const float be = h ? b2.y : b2.x;
+        t[h][0] = (float)((double)gn_up((uint16_t)(h ? e2 >> 16 : e2), BF) - st.x);
+        t[h][1] = (float)st.y * (h ? g2.y : g2.x);
+        t[h][2] = be;
+        t[h][3] = t[h][4] = t[h][5] = 0.f;
+        const float fixed = gn_fixed(t[h][0], t[h][1], be);
+        if (ROWS) {
+          atomicMax(&widest, fixed < INFINITY ? __float_as_uint(fixed) : 0x7F800000u);  // (any order gives the same)
+        } else {
+          const float4 z4 = cell[groups >> (16 * h) & 0xFFFFu];
+          w = max(w, gn_limit<EIGHT>(z4.z, -(float)__float_as_int(z4.w), Lf, fixed));  // one limit for both channels
+          t[h][1] *= z4.x;
+          t[h][2] = SILU ? be * z4.x : fmaf(be, z4.x, z4.y);
+          t[h][3] = __fdividef(-1.4426950408889634f, z4.x);
+          t[h][4] = z4.y;
+          t[h][5] = __uint_as_float(0x80808080u - 0x01010101u * __float_as_uint(z4.w));
         }
       }
+      const uint32_t below = min(gn_below<EIGHT>(w), 0xFFFFu);
+      chan[at] = make_float4(t[0][0], t[1][0], t[0][1], t[1][1]);
+      one = make_float4(t[0][2], t[1][2], __uint_as_float(places), __uint_as_float(ROWS ? groups : below | below << 16));
+      if (!ROWS) {
+        chan[at + 2 * nv] = make_float4(t[0][3], t[1][3], t[0][4], t[1][4]);
+        chan[at + 3 * nv] = make_float4(t[0][5], t[1][5], gn_bias<EIGHT>(w), 0.f);
+      }
+    }
   }
   __syncthreads();
   if (ROWS) {
@@ -713,27 +755,17 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
   auto exact = [&](int p, int c) {
     const uint16_t value = a.X[(int64_t)b * a.xb + p * a.xp + c];
     const int at = (ROWS ? __ldg(a.row_group + (row0 + p) % a.row_period) * a.G : 0) + __ldg(a.chunk_group + (place_of(c) >> 6));
-    return gn_code_exact(a, stat, SILU, BF, gn_up(value, BF), b, c, __ldg(a.inv_scale + at), __float_as_int(cell[at].w), centred);
+    return gn_code_exact(a, stat, SILU, BF, gn_up(value, BF), b, c, ROWS ? __ldg(a.inv_scale + at) : cell[at].z, __float_as_int(cell[at].w), centred);
   };
   // this thread's first 16 places on the way out, the same in every round
   int chunks = a.K_pad >> 4, out_quad = gn_div(tid, a.per_chunks), out_chunk = tid - out_quad * chunks;
   gn_keep(out_quad), gn_keep(out_chunk), gn_keep(chunks);
   uint32_t my_words = smem_u32(words + quad * a.K_pad);  // flips between the two sets
-  request(p0 + 4 * quad);
   for (int p = p0, round = 0; p < p1; p += 4 * a.quads, ++round) {
     const int r = p + 4 * quad;
     if (active && r < p1) {
-      int rg[4] = {0, 0, 0, 0};
-      if (ROWS) {
-        int at = position;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          rg[j] = __ldg(a.row_group + at) * a.G;
-          if (++at == a.row_period) at = 0;
-        }
-        position += advance;
-        if (position >= a.row_period) position -= a.row_period;
-      }
+      int4 rg = make_int4(0, 0, 0, 0);
+      if (ROWS) rg = *reinterpret_cast<const int4*>(row_cells + ((round & 1) * a.quads + quad) * 4);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float4 k0 = chan[i * 4 * nv + v], k1 = chan[(i * 4 + 1) * nv + v];
@@ -746,12 +778,16 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
         uint32_t m[2][4];
         bool near_border = false;
         uint32_t zero[2] = {0, 0};  // (ROWS, zero-centred) the rows' zero-points
+        float4 c0 = make_float4(0.f, 0.f, 0.f, 0.f), c1 = c0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const float2 f = unpack16<BF>(w[j][i]);
           float y0 = f.x + k0.x, y1 = f.y + k0.y, bias0 = k3.z, bias1 = k3.z;  // (NaN is cut off to the lower end)
           if (ROWS) {
-            const float4 c0 = cell[rg[j] + (int)(__float_as_uint(k1.w) & 0xFFFFu)], c1 = cell[rg[j] + (int)(__float_as_uint(k1.w) >> 16)];
+            const int mine = j == 0 ? rg.x : j == 1 ? rg.y : j == 2 ? rg.z : rg.w, before = j == 1 ? rg.x : j == 2 ? rg.y : rg.z;
+            if (j == 0 || mine != before) {  // (rows next to each other are mostly of one group)
+              c0 = cell[mine + (int)(__float_as_uint(k1.w) & 0xFFFFu)], c1 = cell[mine + (int)(__float_as_uint(k1.w) >> 16)];
+            }
             y0 = fmaf(y0, k0.z, k1.x), y1 = fmaf(y1, k0.w, k1.y);
             if (SILU) gn_silu2(y0, y1, -1.4426950408889634f, -1.4426950408889634f, y0, y1);
             y0 = gn_fma_sat(y0, c0.x, c0.y), y1 = gn_fma_sat(y1, c1.x, c1.y);
@@ -810,23 +846,21 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
     }
     request(r + 4 * a.quads);  // arrives while this round's rows leave
     uint32_t* out_words = words + (a.buffers == 2 && (round & 1) ? set_words : 0);
-    if (ROWS)  // padding
-      for (int i = tid; i < a.K_pad; i += n_threads) {
-        if (__ldg(a.perm + i) >= 0) continue;
-        const int g = __ldg(a.chunk_group + (i >> 4));
-        for (int q = 0; q < a.quads; ++q) {
-          uint32_t word = 0;
-          if (!centred) {
-            int at = (int)((row0 + p + 4 * q) % a.row_period);
+    if (ROWS) {  // padding
+      const int count = n_pads;
+      const float per_count = __fdividef(1.f, (float)count);
+      for (int i = tid; i < count * a.quads; i += n_threads) {
+        const int q = gn_div(i, per_count);
+        const uint32_t pad = pads[i - q * count];
+        uint32_t word = 0;
+        if (!centred) {
+          const int* rows = row_cells + ((round & 1) * a.quads + q) * 4;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              word |= (uint32_t)min(max(__ldg(a.zp + __ldg(a.row_group + at) * a.G + g), 0), L) << (8 * j);
-              if (++at == a.row_period) at = 0;
-            }
-          }
-          out_words[q * a.K_pad + gn_shuffle(i)] = word;
+          for (int j = 0; j < 4; ++j) word |= (uint32_t)min(max(__float_as_int(cell[rows[j] + (int)(pad >> 16)].w), 0), L) << (8 * j);
         }
+        out_words[q * a.K_pad + (int)(pad & 0xFFFFu) / 4] = word;
       }
+    }
     __syncthreads();
     if (p + 4 * a.quads >= p1) pdl_launch_dependents();  // (earlier, the next kernel's blocks would crowd this one's)
     for (int q = out_quad, ch = out_chunk; q < a.quads;) {
@@ -881,7 +915,7 @@ static inline GnSumsPlan gn_sums_plan(int B, int P, int C) {
   s.threads = (s.lines * s.nvec + 31) / 32 * 32;
   const int most = (P - 1) / (2 * s.lines) + 1;
   int slabs = std::max(1, std::min((296 + B - 1) / B, most));
-  s.cluster = slabs >= 8 ? 8 : slabs >= 4 ? 4 : slabs >= 2 ? 2 : 1;
+  s.cluster = slabs >= 128 ? 16 : slabs >= 8 ? 8 : slabs >= 4 ? 4 : slabs >= 2 ? 2 : 1;
   s.clusters = (slabs + s.cluster - 1) / s.cluster;
   slabs = s.clusters * s.cluster;
   s.rows = (P - 1) / slabs + 1;
@@ -1001,8 +1035,11 @@ static dgq_status gn_sums(GnArgs a, int B, cudaStream_t stream) {
   const GnSumsPlan s = gn_sums_plan(B, a.P, a.C);
   gn_shape(a, s.nvec, s.lines);
   a.slab_rows = s.rows;
+  // Where a map is small the second kernel's first steps hide behind this one's; where it is large its blocks would take the places of this one's.
+  a.early = (int64_t)B * a.P * a.C <= 8 << 20;
   a.clusters = s.clusters;
-  const size_t smem = a.n_groups * sizeof(double2) + std::max((size_t)SEG * s.lines * s.nvec * sizeof(double2), (size_t)s.threads * GN_RING * 16);
+  a.log_cluster = s.cluster == 16 ? 4 : s.cluster == 8 ? 3 : s.cluster / 2;
+  const size_t smem = (size_t)(a.n_groups + s.cluster) * sizeof(double2) + std::max((size_t)SEG * s.lines * s.nvec * sizeof(double2), (size_t)s.threads * GN_RING * 16);
   DGQ_CUDA_OK(gn_launch(gn_sums_kernel<BF, SEG>, dim3(s.clusters * s.cluster, B), s.threads, smem, s.cluster, stream, a, done));
   return DGQ_OK;
 }
@@ -1049,8 +1086,13 @@ static dgq_status gn_codes(GnArgs& a, int B, cudaStream_t stream) {
   // as many quads of rows as 256 threads have, within 48 KB
   a.quads = std::max(1, std::min({256 / a.nvec, 48 * 1024 / (a.K_pad * 4), (a.P + 3) / 4}));
   const int threads = (a.quads * a.nvec + 31) / 32 * 32, step = 4 * a.quads;
-  const size_t fixed = a.n_groups * sizeof(double2) + (size_t)a.C / 2 * 4 * sizeof(float4) + (size_t)a.R * a.G * sizeof(float4);
+  const size_t fixed = a.n_groups * sizeof(double2) + (size_t)a.C / 2 * 4 * sizeof(float4) + (size_t)a.R * a.G * sizeof(float4) +
+                       (ROWS ? (size_t)a.quads * 32 + (size_t)(a.K_pad - a.C) * 4 : 0);
   const size_t set = (size_t)a.quads * a.K_pad * 4;
+  static_assert((GN_MAX_C + 39 * DGQ_MAX_GROUPS) * 4 + GN_MAX_CODE_GROUPS * 16 + GN_MAX_C / 2 * 64 + DGQ_MAX_GROUPS * DGQ_MAX_GROUPS * 16 + 32 +
+                        39 * DGQ_MAX_GROUPS * 4 <=
+                    GN_SMEM_MAX,
+                "one quad of the widest row");
   // one wave of blocks, as many as registers (64 a thread) and shared memory (with 5 KB of the kernel's own and the system's) allow
   auto fit = [&](int buffers) { return std::max<int>(1, std::min<size_t>(1024 / threads, 233472 / (fixed + buffers * set + 5 * 1024 + 512))); };
   a.buffers = fit(2) == fit(1) ? 2 : 1;
@@ -1107,6 +1149,7 @@ extern "C" dgq_status dgq_group_norm_quantize(const dgq_groups* g, int timestep,
   dgq_status st = gn_check(X, add, ld_add, dtype, B, P, g->C, n_groups, eps, act);
   if (st != DGQ_OK) return st;
   if (!aligned16(Xq)) return DGQ_ERR_ALIGNMENT;
+  if (n_groups > GN_MAX_CODE_GROUPS) return DGQ_ERR_UNSUPPORTED;
   if (!g->filled[timestep]) return DGQ_ERR_NOT_CALIBRATED;
   const size_t trow = (size_t)timestep * g->R * g->G;
   const int L = (1 << g->bits) - 1;

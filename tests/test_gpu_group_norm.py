@@ -155,8 +155,8 @@ def codes_against(g, x, groups, gamma, beta, silu, e, timestep, centred, got, ep
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
-@pytest.mark.parametrize("B,P,C,groups", [s for s in SHAPES if s[1] * s[2] // s[3] > 1])
-@pytest.mark.parametrize("bits,G,R,centred", [(6, 16, 1, True), (8, 5, 2, False), (4, 1, 1, False), (6, 3, 3, True), (2, 32, 1, True)])
+@pytest.mark.parametrize("B,P,C,groups", [s for s in SHAPES if s[1] * s[2] // s[3] > 1 and s[3] <= 2048] + [(1, 40, 4096, 2048)])
+@pytest.mark.parametrize("bits,G,R,centred", [(6, 16, 1, True), (8, 5, 2, False), (4, 1, 1, False), (6, 3, 3, True), (2, 32, 1, True), (8, 32, 32, False)])
 def test_codes(B, P, C, groups, dtype, bits, G, R, centred):
     gpu()
     if B * P * C > 1 << 21 and (bits, R) != (6, 1):
@@ -292,5 +292,9 @@ def test_refusals_of_the_binding():
                  lambda: b.group_norm_quantize(grouping(1, 64, 10, 6, 2, 1, False), x, 8, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))):
         with pytest.raises(b.DgqError):
             call()
+    wide = torch.zeros(1, 2, 4096, dtype=F16, device="cuda")
+    with pytest.raises(b.DgqError) as refused:
+        b.group_norm_quantize(grouping(1, 4096, 2, 6, 2, 1, False), wide, 4096)
+    assert refused.value.status == 3
     empty = b.group_norm(x[:0], 8)
     assert empty.shape == (0, 10, 64) and b.group_norm(x[:, :0], 8).shape == (2, 0, 64)
