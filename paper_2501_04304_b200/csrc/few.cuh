@@ -38,6 +38,8 @@ __host__ __device__ inline int few_scale_place(int column, int r, int group) {
 // A warp may read this many blocks behind the end of a tile (the rows are zeros there): the next tile's, or what lies behind the last one,
 // of which the scales are zeros.
 constexpr int FEW_BEYOND = 64;
+// Warps of a block with the rows in shared memory: 72 registers a thread, 128 with 32 rows (at 72 300 bytes spill: 79 -> 123 us for 32 x 8192 x 28672).
+__host__ __device__ constexpr int few_most_warps(int mt) { return mt == 4 ? 16 : 26; }
 
 #ifdef __CUDACC__
 
@@ -274,7 +276,7 @@ __global__ void __launch_bounds__(512, 2) few_rows_kernel(const __grid_constant_
 // of 64 of a chunk) and the tiles; the rows of a chunk stand in shared memory for all of them, three chunks in turn, so that one barrier a chunk is
 // enough.  A warp's weights are asked for a chunk ahead, in registers.
 template <bool BF, bool G32, int MT>
-__global__ void __launch_bounds__(512) few_kernel(const __grid_constant__ FewArgs a) {
+__global__ void __launch_bounds__(few_most_warps(MT) * 32) few_kernel(const __grid_constant__ FewArgs a) {
   extern __shared__ __align__(16) unsigned char few_smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const int wk = warp & ((1 << a.log_wk) - 1), wn = warp >> a.log_wk;
@@ -342,34 +344,43 @@ __global__ void __launch_bounds__(512) few_kernel(const __grid_constant__ FewArg
     codes += per_chunk * 32, scales += scale_step;  // those of the next chunk
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      uint32_t x[MT][8];
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        const uint4* p = reinterpret_cast<const uint4*>(from + mine[m] + i * 128);
-        const uint4 x0 = p[0], x1 = p[4];
-        x[m][0] = x0.x, x[m][1] = x0.y, x[m][2] = x0.z, x[m][3] = x0.w;
-        x[m][4] = x1.x, x[m][5] = x1.y, x[m][6] = x1.z, x[m][7] = x1.w;
-      }
+      // 32 rows: a lane's part of all of them at once, of which the compiler makes the better order; fewer: one half after the other, for the registers
+      constexpr int HALVES = MT == 4 ? 1 : 2;
       const uint32_t words[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
       float d[MT][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t op[4];
-        few_widen<BF>(words[j], op);
+      for (int half = 0; half < HALVES; ++half) {
+        uint32_t x[MT][8 / HALVES];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-          if (j == 0 || (G32 && j == 2)) few_mma_first<BF>(d[m], op, x[m][2 * j], x[m][2 * j + 1]);
-          else few_mma<BF>(d[m], op, x[m][2 * j], x[m][2 * j + 1]);
+          const uint4* p = reinterpret_cast<const uint4*>(from + mine[m] + i * 128 + half * 64);
+          const uint4 x0 = p[0];
+          x[m][0] = x0.x, x[m][1] = x0.y, x[m][2] = x0.z, x[m][3] = x0.w;
+          if constexpr (HALVES == 1) {
+            const uint4 x1 = p[4];
+            x[m][4] = x1.x, x[m][5] = x1.y, x[m][6] = x1.z, x[m][7] = x1.w;
+          }
         }
-        if (j == 3 || (G32 && j == 1)) {
-          const uint32_t pair = G32 && j == 3 ? s[i].y : s[i].x;
-          const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&pair));
+#pragma unroll
+        for (int k = 0; k < 4 / HALVES; ++k) {
+          const int j = half * 2 + k;
+          uint32_t op[4];
+          few_widen<BF>(words[j], op);
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
-            acc[m][0] = fmaf(d[m][0], f.x, acc[m][0]);
-            acc[m][1] = fmaf(d[m][1], f.x, acc[m][1]);
-            acc[m][2] = fmaf(d[m][2], f.y, acc[m][2]);
-            acc[m][3] = fmaf(d[m][3], f.y, acc[m][3]);
+            if (j == 0 || (G32 && j == 2)) few_mma_first<BF>(d[m], op, x[m][2 * k], x[m][2 * k + 1]);
+            else few_mma<BF>(d[m], op, x[m][2 * k], x[m][2 * k + 1]);
+          }
+          if (j == 3 || (G32 && j == 1)) {
+            const uint32_t pair = G32 && j == 3 ? s[i].y : s[i].x;
+            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&pair));
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              acc[m][0] = fmaf(d[m][0], f.x, acc[m][0]);
+              acc[m][1] = fmaf(d[m][1], f.x, acc[m][1]);
+              acc[m][2] = fmaf(d[m][2], f.y, acc[m][2]);
+              acc[m][3] = fmaf(d[m][3], f.y, acc[m][3]);
+            }
           }
         }
       }
@@ -438,16 +449,16 @@ static FewPlan few_plan(int M, int tiles, int blocks) {
   p.mt = M <= 8 ? 1 : M <= 16 ? 2 : 4;
   const int rows = std::min(M, p.mt * 8);
   const int64_t units = (int64_t)tiles * ((M + p.mt * 8 - 1) / (p.mt * 8));
-  // sixteen warps for each multiprocessor where the weights' bytes are waited for, eight where 32 rows keep the matrix unit busy; four
+  // sixteen warps for each multiprocessor (eight with 32 rows), four
   // blocks of 64 channels for a warp at least
   p.log_wk = 0;
-  const int most = p.mt == 4 ? 2 : p.mt == 2 ? 3 : 4, warps = p.mt == 4 ? 8 : p.mt == 2 ? 12 : 16;
+  const int most = p.mt == 4 ? 2 : p.mt == 2 ? 3 : 4, warps = p.mt == 4 ? 8 : 16;
   while (p.log_wk < most && units << p.log_wk < warps * 148 && (4 << p.log_wk) < blocks) ++p.log_wk;
   // Along the outputs, with more than eight rows, which would be read over and over: the most that fill the multiprocessors as evenly as any other
-  // number does, of at most 14 warps of a block.
+  // number does.
   p.wn = 1;
   double best = 0.;
-  for (int wn = 1; p.mt > 1 && wn << p.log_wk <= 14; ++wn) {
+  for (int wn = 1; p.mt > 1 && wn << p.log_wk <= few_most_warps(p.mt); ++wn) {
     const int64_t n = (units + wn - 1) / wn, rounds = (n + 147) / 148;
     const double full = (double)units / (double)(rounds * 148 * wn);
     if (full > 0.97 * best) best = std::max(best, full), p.wn = wn;

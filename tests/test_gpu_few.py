@@ -29,7 +29,8 @@ def against(x, wq, scales, group, silu, c, y):
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("M,K,N", [(1, 8, 1), (2, 1280, 320), (1, 4096, 4096), (7, 5000, 1007), (8, 72, 16), (9, 136, 17), (16, 640, 1280), (17, 1000, 33),
                                    (24, 96, 100), (31, 2048, 250), (32, 320, 640), (33, 128, 48), (100, 768, 320), (3, 10240, 1280), (1, 200, 5000),
-                                   (4, 64, 20001), (5, 8192, 15)])
+                                   (4, 64, 20001), (5, 8192, 15), (12, 4096, 1600), (32, 1024, 6150), (20, 520, 12500), (45, 1288, 3100),
+                                   (16, 8192, 800), (9, 712, 6300), (33, 4160, 3000)])
 def test_products(M, K, N, group, dtype):
     gpu()
     x, wq, scales, c = make(M + K + N, M, K, N, group, dtype, bias=N % 2 == 0)
