@@ -34,6 +34,7 @@ struct GnArgs {
   int log_cluster;          // blocks of a cluster (one kernel, sums)
   int slab_rows, clusters;  // sums: rows of a block, clusters of an image
   int early;                // sums: the second kernel's blocks may come in at once
+  int past;                 // values: the output is as large as half of L2
   int rows;                 // values and codes: rows of a block
   float eps;
   double per_count;  // 1 / (P cpg)
@@ -553,7 +554,9 @@ __global__ void __launch_bounds__(GN_MAX_THREADS) gn_values_kernel(const __grid_
       w[i] = pack16<BF>(y0, y1);
     }
     ring.request(k + GN_RING - 1, src, k + GN_RING - 1 < rows);  // into the piece before this one
-    *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+    // what would push out of L2 the map that is still to be read goes past it
+    if (a.past) __stcs(reinterpret_cast<uint4*>(dst), make_uint4(w[0], w[1], w[2], w[3]));
+    else *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
   }
 }
 
@@ -958,6 +961,9 @@ static inline GnChipPlan gn_chip_plan(int B, int P, int C, int cpg) {
     const int64_t bytes = (int64_t)rows * s.nvec * 16;
     if ((blocks * cluster >= 96 && bytes <= 48 * 1024) || bytes <= 16 * 1024) break;
   }
+  // Blocks that fill a multiprocessor each, in several rounds, read, join and write one after the other: two kernels are faster then (8 x 4096 x
+  // 960: 42 against 60 us; in one round 2 x 3000 x 1000 in 5 groups 17 against 13, smaller blocks 8 x 4096 x 640 33 against 31).
+  if (s.smem > 110 * 1024 && blocks * s.cluster > 148) s.ok = false;
   return s;
 }
 
@@ -1072,6 +1078,7 @@ static dgq_status gn_values(GnArgs& a, int B, cudaStream_t stream) {
   const int threads = (a.lines * a.nvec + 31) / 32 * 32;
   const int step = 4 * a.lines, rounds = (int)(((int64_t)B * a.P + 444ll * step - 1) / (444ll * step));  // three blocks for each multiprocessor
   a.rows = (int)std::min<int64_t>((int64_t)rounds * step, 1 << 30);
+  a.past = (int64_t)B * a.P * a.C >= 24 << 20;  // (1 x 262144 x 128: 49.8 -> 46.6 us)
   DGQ_CUDA_OK(gn_launch(gn_values_kernel<BF, SILU>, dim3((a.P - 1) / a.rows + 1, B), threads,
                         a.n_groups * sizeof(double2) + (size_t)threads * GN_RING * 16, 1, stream, a, done));
   return DGQ_OK;
