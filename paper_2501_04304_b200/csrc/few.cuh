@@ -62,7 +62,21 @@ struct FewPackArgs {
   uint32_t* codes;
   __half* scale_out;
   int* bad;
+  int aligned;  // eight values lie at a multiple of their size
 };
+// Eight neighbouring values as the registers of one load, where they are aligned.
+template <typename T, typename V>
+__device__ __forceinline__ void few_load8(const T* p, bool aligned, V& v) {
+  static_assert(sizeof(V) == 8 * sizeof(T), "eight values");
+  if (aligned) {
+    v = __ldg(reinterpret_cast<const V*>(p));
+  } else {
+    T t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = p[i];
+    memcpy(&v, t, sizeof(V));
+  }
+}
 
 // One block per tile of 16 outputs and 128 input channels; a thread has eight channels of one output.
 __global__ void __launch_bounds__(256) few_pack_kernel(const FewPackArgs a) {
@@ -78,9 +92,12 @@ __global__ void __launch_bounds__(256) few_pack_kernel(const FewPackArgs a) {
   if (a.W) {
     // s = max |w| / 7 rounded up, so that no code is beyond 7; code = rint(w / s)
     float w[8], top = 0.f;
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    if (in) few_load8(a.W + (size_t)n * a.K + k0, a.aligned, raw);
+    const uint32_t h[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      w[i] = in ? __half2float(a.W[(size_t)n * a.K + k0 + i]) : 0.f;
+      w[i] = gn_up((uint16_t)(i & 1 ? h[i >> 1] >> 16 : h[i >> 1]), false);
       bad |= !(fabsf(w[i]) < INFINITY);
       top = fmaxf(top, fabsf(w[i]));
     }
@@ -93,18 +110,26 @@ __global__ void __launch_bounds__(256) few_pack_kernel(const FewPackArgs a) {
   } else if (in) {
     s = a.scales[(size_t)n * a.n_groups + k0 / a.group];
     bad |= !(fabsf(__half2float(s)) < INFINITY);
+    uint2 raw;
+    few_load8(a.wq + (size_t)n * a.K + k0, a.aligned, raw);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      q[i] = a.wq[(size_t)n * a.K + k0 + i];
+      q[i] = (int8_t)((i < 4 ? raw.x : raw.y) >> (8 * (i & 3)));
       bad |= q[i] < -8 || q[i] > 7;
     }
   }
   if (bad) *a.bad = 1;
+  // four neighbouring channels of an output lie in one word, with those of the output eight further
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    int word, shift;
-    few_place(r, (k0 + i) & 63, &word, &shift);
-    atomicOr(&words[(tid & 15) >> 3][word], (uint32_t)((q[i] + 8) & 15) << shift);
+  for (int i = 0; i < 8; i += 4) {
+    uint32_t v = 0;
+    int word = 0, shift;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      few_place(r, ((k0 + i) & 63) + j, &word, &shift);
+      v |= (uint32_t)((q[i + j] + 8) & 15) << shift;
+    }
+    atomicOr(&words[(tid & 15) >> 3][word], v);
   }
   __syncthreads();
   const int block = blockIdx.x * 2 + (tid >> 7);
@@ -125,7 +150,6 @@ struct FewArgs {
   int64_t ldy;
   int M, N, K, blocks, columns, tiles;
   int log_columns;  // 1 where two blocks share a scale column (groups of 128)
-  int silu;
   int log_wk, wn;   // warps of a block: 2^log_wk along the input channels, wn along the outputs
 };
 
@@ -274,15 +298,16 @@ __global__ void __launch_bounds__(512, 2) few_rows_kernel(const __grid_constant_
 
 // A block has wn tiles of outputs and MT times eight rows.  Its warps split the input channels (2^log_wk ways, every warp four neighbouring blocks
 // of 64 of a chunk) and the tiles; the rows of a chunk stand in shared memory for all of them, three chunks in turn, so that one barrier a chunk is
-// enough.  A warp's weights are asked for a chunk ahead, in registers.
-template <bool BF, bool G32, int MT>
+// enough.  A warp's weights are asked for a chunk ahead, in registers.  A SiLU's results enter as a 16-bit number and what it leaves of
+// the 32-bit one, rounded too: rounded once only, they would put half as much error again on the result's own.
+template <bool BF, bool G32, int MT, bool SILU>
 __global__ void __launch_bounds__(few_most_warps(MT) * 32) few_kernel(const __grid_constant__ FewArgs a) {
   extern __shared__ __align__(16) unsigned char few_smem[];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, c = lane & 3;
   const int wk = warp & ((1 << a.log_wk) - 1), wn = warp >> a.log_wk;
   const int tile = min((int)blockIdx.x * a.wn + wn, a.tiles - 1), m0 = blockIdx.y * MT * 8, rows = min(MT * 8, a.M - m0);
   const int per_chunk = 4 << a.log_wk, chunks = (a.blocks + per_chunk - 1) >> (2 + a.log_wk);
-  const int pitch = per_chunk * 128 + 64, set = rows * pitch;  // bytes; rows start in different halves of the banks
+  const int pitch = per_chunk * 128 + 64, part = rows * pitch, set = SILU ? 2 * part : part;  // bytes; rows start in different halves of the banks
   uint4 w[4];
   uint2 s[4];
   const uint4* codes = a.codes + ((size_t)tile * a.blocks + wk * 4) * 32 + lane;
@@ -301,20 +326,25 @@ __global__ void __launch_bounds__(few_most_warps(MT) * 32) few_kernel(const __gr
     const uint16_t* src = a.X + (m0 + wn) * a.ldx + (in ? k : 0);
     uint32_t to = smem_u32(few_smem) + buffer * set + wn * pitch + piece * 16;
     for (int row = wn; row < rows; row += a.wn, src += a.wn * a.ldx, to += a.wn * pitch) {
-      if (!a.silu) {
+      if (!SILU) {
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(src), "r"(in ? 16 : 0) : "memory");
       } else {
-        uint4 x = make_uint4(0, 0, 0, 0);
+        uint4 x = make_uint4(0, 0, 0, 0), y = x;
         if (in) {
           x = __ldg(reinterpret_cast<const uint4*>(src));
           uint32_t* h = reinterpret_cast<uint32_t*>(&x);
+          uint32_t* l = reinterpret_cast<uint32_t*>(&y);
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
             const float2 f = unpack16<BF>(h[z]);
-            h[z] = pack16<BF>(gn_silu(f.x), gn_silu(f.y));
+            const float v0 = gn_silu(f.x), v1 = gn_silu(f.y);
+            h[z] = pack16<BF>(v0, v1);
+            const float2 g = unpack16<BF>(h[z]);
+            l[z] = pack16<BF>(v0 - g.x, v1 - g.y);
           }
         }
         asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to + part), "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w) : "memory");
       }
     }
   };
@@ -345,17 +375,19 @@ __global__ void __launch_bounds__(few_most_warps(MT) * 32) few_kernel(const __gr
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       // 32 rows: a lane's part of all of them at once, of which the compiler makes the better order; fewer: one half after the other, for the registers
-      constexpr int HALVES = MT == 4 ? 1 : 2;
+      constexpr int HALVES = MT == 4 && !SILU ? 1 : 2;
       const uint32_t words[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
       float d[MT][4];
 #pragma unroll
       for (int half = 0; half < HALVES; ++half) {
         uint32_t x[MT][8 / HALVES];
+        uint4 y[MT];
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           const uint4* p = reinterpret_cast<const uint4*>(from + mine[m] + i * 128 + half * 64);
           const uint4 x0 = p[0];
           x[m][0] = x0.x, x[m][1] = x0.y, x[m][2] = x0.z, x[m][3] = x0.w;
+          if constexpr (SILU) y[m] = *reinterpret_cast<const uint4*>(from + mine[m] + i * 128 + half * 64 + part);
           if constexpr (HALVES == 1) {
             const uint4 x1 = p[4];
             x[m][4] = x1.x, x[m][5] = x1.y, x[m][6] = x1.z, x[m][7] = x1.w;
@@ -370,6 +402,7 @@ __global__ void __launch_bounds__(few_most_warps(MT) * 32) few_kernel(const __gr
           for (int m = 0; m < MT; ++m) {
             if (j == 0 || (G32 && j == 2)) few_mma_first<BF>(d[m], op, x[m][2 * k], x[m][2 * k + 1]);
             else few_mma<BF>(d[m], op, x[m][2 * k], x[m][2 * k + 1]);
+            if constexpr (SILU) few_mma<BF>(d[m], op, k ? y[m].z : y[m].x, k ? y[m].w : y[m].y);
           }
           if (j == 3 || (G32 && j == 1)) {
             const uint32_t pair = G32 && j == 3 ? s[i].y : s[i].x;
@@ -419,7 +452,8 @@ static dgq_status few_build(const __half* W, const int8_t* wq, const __half* sca
     w->d_scale = reinterpret_cast<uint32_t*>(w->d_slab + code_bytes);
     int* d_bad = reinterpret_cast<int*>(w->d_slab + code_bytes + scale_bytes + beyond);
     FewPackArgs a = {W, wq, scales, N, K, group, w->n_groups, w->blocks, columns, reinterpret_cast<uint32_t*>(w->d_codes),
-                     reinterpret_cast<__half*>(w->d_scale), d_bad};
+                     reinterpret_cast<__half*>(w->d_scale), d_bad,
+                     W ? aligned16(W) : (reinterpret_cast<uintptr_t>(wq) & 7u) == 0};
     const size_t scale_end = code_bytes + (size_t)w->tiles * columns * 32;
     if (ok(cudaMemsetAsync(w->d_slab + scale_end, 0, code_bytes + scale_bytes + beyond + sizeof(int) - scale_end, stream))) {
       few_pack_kernel<<<dim3((w->blocks + 1) / 2, w->tiles), 256, 0, stream>>>(a);
@@ -439,12 +473,13 @@ static dgq_status few_build(const __half* W, const int8_t* wq, const __half* sca
   return DGQ_OK;
 }
 
+constexpr size_t FEW_SMEM_MAX = 208 * 1024;
 // How a product is dealt out: warps along the input channels (a power of two) and along the outputs, eights of rows.
 struct FewPlan {
   int log_wk, wn, mt;
   size_t smem;
 };
-static FewPlan few_plan(int M, int tiles, int blocks) {
+static FewPlan few_plan(int M, int tiles, int blocks, bool silu) {
   FewPlan p;
   p.mt = M <= 8 ? 1 : M <= 16 ? 2 : 4;
   const int rows = std::min(M, p.mt * 8);
@@ -454,6 +489,12 @@ static FewPlan few_plan(int M, int tiles, int blocks) {
   p.log_wk = 0;
   const int most = p.mt == 4 ? 2 : p.mt == 2 ? 3 : 4, warps = p.mt == 4 ? 8 : 16;
   while (p.log_wk < most && units << p.log_wk < warps * 148 && (4 << p.log_wk) < blocks) ++p.log_wk;
+  // (a SiLU's results take twice the place: the channels are split less where they do not fit)
+  auto staged = [&]() {
+    const int per_chunk = 4 << p.log_wk, sets = std::min((blocks + per_chunk - 1) / per_chunk, 3);
+    return (size_t)sets * rows * (per_chunk * 128 + 64) * (silu ? 2 : 1);
+  };
+  while (p.log_wk > 0 && staged() > FEW_SMEM_MAX) --p.log_wk;
   // Along the outputs, with more than eight rows, which would be read over and over: the most that fill the multiprocessors as evenly as any other
   // number does.
   p.wn = 1;
@@ -463,33 +504,35 @@ static FewPlan few_plan(int M, int tiles, int blocks) {
     const double full = (double)units / (double)(rounds * 148 * wn);
     if (full > 0.97 * best) best = std::max(best, full), p.wn = wn;
   }
-  const int per_chunk = 4 << p.log_wk, sets = std::min((blocks + per_chunk - 1) / per_chunk, 3);
-  p.smem = std::max((size_t)sets * rows * (per_chunk * 128 + 64), (size_t)(1 << p.log_wk) * rows * p.wn * 16 * sizeof(float));
+  p.smem = std::max(staged(), (size_t)(1 << p.log_wk) * rows * p.wn * 16 * sizeof(float));
   return p;
 }
 
-template <bool BF, bool G32, int MT>
+template <bool BF, bool G32, int MT, bool SILU>
 static dgq_status few_launch(const FewArgs& a, const FewPlan& p, cudaStream_t stream) {
   static std::atomic<bool> done[64];
   int dev = 0;
   DGQ_CUDA_OK(cudaGetDevice(&dev));
   if (dev >= 64 || !done[dev].load()) {
-    DGQ_CUDA_OK(cudaFuncSetAttribute(few_kernel<BF, G32, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, 208 * 1024));
+    DGQ_CUDA_OK(cudaFuncSetAttribute(few_kernel<BF, G32, MT, SILU>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)FEW_SMEM_MAX));
     if (dev < 64) done[dev].store(true);
   }
   const dim3 grid((a.tiles + p.wn - 1) / p.wn, (a.M + MT * 8 - 1) / (MT * 8));
-  DGQ_CUDA_OK(launch_pdl(few_kernel<BF, G32, MT>, grid, dim3((p.wn << p.log_wk) * 32), p.smem, stream, a));
+  DGQ_CUDA_OK(launch_pdl(few_kernel<BF, G32, MT, SILU>, grid, dim3((p.wn << p.log_wk) * 32), p.smem, stream, a));
   g_launches += 1;
   return DGQ_OK;
 }
+template <bool BF, bool G32, bool SILU>
+static dgq_status few_rows(const FewArgs& a, const FewPlan& p, cudaStream_t stream) {
+  return p.mt == 1 ? few_launch<BF, G32, 1, SILU>(a, p, stream) : p.mt == 2 ? few_launch<BF, G32, 2, SILU>(a, p, stream) : few_launch<BF, G32, 4, SILU>(a, p, stream);
+}
 template <bool BF, bool G32>
-static dgq_status few_pick(const FewArgs& a, const FewPlan& p, cudaStream_t stream) {
-  if (p.mt == 1 && !a.silu) {
-    DGQ_CUDA_OK(launch_pdl(few_rows_kernel<BF, G32>, dim3(a.tiles), dim3(32 << p.log_wk), (size_t)(1 << p.log_wk) * a.M * 16 * sizeof(float), stream, a));
-    g_launches += 1;
-    return DGQ_OK;
-  }
-  return p.mt == 1 ? few_launch<BF, G32, 1>(a, p, stream) : p.mt == 2 ? few_launch<BF, G32, 2>(a, p, stream) : few_launch<BF, G32, 4>(a, p, stream);
+static dgq_status few_pick(const FewArgs& a, const FewPlan& p, bool silu, cudaStream_t stream) {
+  if (silu) return few_rows<BF, G32, true>(a, p, stream);
+  if (p.mt > 1) return p.mt == 2 ? few_launch<BF, G32, 2, false>(a, p, stream) : few_launch<BF, G32, 4, false>(a, p, stream);
+  DGQ_CUDA_OK(launch_pdl(few_rows_kernel<BF, G32>, dim3(a.tiles), dim3(32 << p.log_wk), (size_t)(1 << p.log_wk) * a.M * 16 * sizeof(float), stream, a));
+  g_launches += 1;
+  return DGQ_OK;
 }
 
 }  // namespace dgq
@@ -554,10 +597,11 @@ extern "C" dgq_status dgq_linear_few(const dgq_few_weight* w, const void* X, int
   int dev = 0;
   DGQ_CUDA_OK(cudaGetDevice(&dev));
   if (dev != w->device) return DGQ_ERR_INVALID_ARG;
-  const FewPlan p = few_plan(M, w->tiles, w->blocks);
+  const bool silu = act == DGQ_ACT_SILU;
+  const FewPlan p = few_plan(M, w->tiles, w->blocks, silu);
   const FewArgs a = {w->d_codes, w->d_scale, (const uint16_t*)X, M > 1 ? ldx : 0, (const uint16_t*)bias, (uint16_t*)Y, M > 1 ? ldy : 0, M, w->N, w->K,
-                     w->blocks, few_columns(w->blocks, w->group), w->tiles, w->group == 128, act == DGQ_ACT_SILU, p.log_wk, p.wn};
+                     w->blocks, few_columns(w->blocks, w->group), w->tiles, w->group == 128, p.log_wk, p.wn};
   const cudaStream_t s = (cudaStream_t)stream;
-  if (dtype == DGQ_BF16) return w->group == 32 ? few_pick<true, true>(a, p, s) : few_pick<true, false>(a, p, s);
-  return w->group == 32 ? few_pick<false, true>(a, p, s) : few_pick<false, false>(a, p, s);
+  if (dtype == DGQ_BF16) return w->group == 32 ? few_pick<true, true>(a, p, silu, s) : few_pick<true, false>(a, p, silu, s);
+  return w->group == 32 ? few_pick<false, true>(a, p, silu, s) : few_pick<false, false>(a, p, silu, s);
 }

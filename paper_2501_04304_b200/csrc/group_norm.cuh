@@ -14,6 +14,7 @@
 namespace dgq {
 
 constexpr int GN_MAX_C = 4096;
+constexpr int GN_MAX_PIXELS = 1 << 30;
 constexpr int GN_MAX_CODE_GROUPS = 2048;  // into codes: what shared memory holds beside the widest row
 constexpr int GN_MAX_THREADS = 512;  // one thread for every eight channels of the widest row
 constexpr size_t GN_SMEM_MAX = 232448 - 8 * 1024;  // beside what a kernel declares
@@ -96,15 +97,12 @@ __device__ __forceinline__ float gn_silu(float y) {
 // Eight neighbouring channels lie in at most two groups where a group has four channels or at least seven (SEG 2: a part of each, the
 // second one may be empty), else every channel counts as a part of its own (SEG 8).  What threads have summed up for the parts stands
 // in shared memory as [part][line][eight].
-template <int SEG>
 struct GnParts {
   int first, split;  // group of channel 0, channels of it
   __device__ __forceinline__ GnParts(int v, int cpg, float per_cpg) {
     first = gn_div(v * 8, per_cpg);
     split = min(8, (first + 1) * cpg - v * 8);
   }
-  __device__ __forceinline__ int part(int i) const { return SEG == 8 ? i : i < split ? 0 : 1; }
-  __device__ __forceinline__ int length(int k) const { return SEG == 8 ? 1 : k == 0 ? split : 8 - split; }
 };
 // The entries of a group: calls f(index of the entry in [part][line][eight], its line, channels) for those of lane `sub` of `width`.
 template <int SEG, typename F>
@@ -180,7 +178,7 @@ __global__ void __maxnreg__(80) gn_chip_kernel(const __grid_constant__ GnArgs a)
   gn_keep(line), gn_keep(v);
   const int full = gn_div(R, a.per_lines), more = R - full * lines;  // rows of a line: full, one more for the first ones
   const int n = line < lines ? full + (line < more) : 0;             // rows of this thread
-  const GnParts<SEG> part(v, a.cpg, a.per_cpg);
+  const GnParts part(v, a.cpg, a.per_cpg);
   const int c0 = blockIdx.y * W + v * 8;
   const cooperative_groups::cluster_group cluster = cooperative_groups::this_cluster();
   if (S > 1) cluster.barrier_arrive();  // (waited for before the first access to another block's shared memory: it has started by then)
@@ -427,7 +425,7 @@ __global__ void __launch_bounds__(GN_MAX_THREADS) gn_sums_kernel(const __grid_co
       }
       ring.request(k + GN_RING - 1, src, k + GN_RING - 1 < rows);  // into the piece before this one
     }
-    const GnParts<SEG> part(v, a.cpg, a.per_cpg);
+    const GnParts part(v, a.cpg, a.per_cpg);
     const double n = (double)rows;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -971,7 +969,7 @@ static dgq_status gn_check(const dgq_rows* X, const void* add, int64_t ld_add, i
   if (!rows_pointer_ok(X) || B <= 0 || P <= 0 || C <= 0 || n_groups <= 0 || C % n_groups || (dtype != DGQ_F16 && dtype != DGQ_BF16) ||
       (act != DGQ_ACT_NONE && act != DGQ_ACT_SILU) || !(eps >= 0x1p-126f) || !std::isfinite(eps) || (add && B > 1 && ld_add < 0))
     return DGQ_ERR_INVALID_ARG;
-  if (C % 8 || C > GN_MAX_C || P > (1 << 30) || B > 65535) return DGQ_ERR_UNSUPPORTED;
+  if (C % 8 || C > GN_MAX_C || P > GN_MAX_PIXELS || B > 65535) return DGQ_ERR_UNSUPPORTED;
   return rows_check(*X, B, P, 1, false);
 }
 static void gn_fill(GnArgs& a, const dgq_rows* X, const void* add, int64_t ld_add, const float* gamma, const float* beta, int B, int P, int C,
@@ -1121,7 +1119,7 @@ static dgq_status gn_codes_pick(GnArgs& a, int B, cudaStream_t stream) {
 extern "C" dgq_status dgq_group_norm_workspace_bytes(int B, int P, int C, int n_groups, int quantize, size_t* bytes) {
   using namespace dgq;
   if (!bytes || B <= 0 || P <= 0 || C <= 0 || n_groups <= 0 || C % n_groups) return DGQ_ERR_INVALID_ARG;
-  if (C % 8 || C > GN_MAX_C) return DGQ_ERR_UNSUPPORTED;
+  if (C % 8 || C > GN_MAX_C || P > GN_MAX_PIXELS || B > 65535) return DGQ_ERR_UNSUPPORTED;
   *bytes = !quantize && gn_chip_plan(B, P, C, C / n_groups).ok ? 0 : gn_sums_bytes(B, P, C, n_groups);
   return DGQ_OK;
 }

@@ -67,8 +67,9 @@ def few(x, wq, scales, group, silu, bias):
 
 
 def few_bound(y, size, dtype, silu, k):
-    """The output's rounding; a SiLU's rounding to the inputs' type and its error in 32 bits, on every term; sums in 32 bits: the products
-    are exact, each is part of at most k / 16 + 30 additions of its chain, of a group's scale and of the warps' parts, whose rounding
-    (or, inside the matrix instruction, cutting) is at most 2^-23 of the sizes' sum."""
+    """The output's rounding; sums in 32 bits: the products are exact, each is part of at most k / 16 + 30 additions of its chain, of a group's
+    scale and of the warps' parts, whose rounding (or, inside the matrix instruction, cutting) is at most 2^-23 of the sizes' sum; a SiLU's
+    error in 32 bits (2^-20 of it) and the rounding of what its first 16-bit part leaves (half a step of half a step, and in fp16 2^-25 where
+    that part is below the smallest normal number, which 2^-20 of the sizes' sum covers where the rows are about 1)."""
     t = HALF_STEP[dtype] * y.abs() + (k / 16 + 30) * 2.0 ** -23 * size + 2.0 ** -25
-    return t + (HALF_STEP[dtype] * 1.01 + 2.0 ** -20) * size * (1 if silu else 0)
+    return t + (HALF_STEP[dtype] ** 2 + 2.0 ** -19) * size * (1 if silu else 0)

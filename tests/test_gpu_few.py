@@ -55,6 +55,23 @@ def test_every_code_is_at_its_place(group):
     assert np.array_equal(codes, wq.cpu().numpy()) and np.array_equal(s, scales.cpu().numpy())
 
 
+def test_weights_that_start_anywhere():
+    """Codes and fp16 weights one element behind an aligned place."""
+    gpu()
+    _, wq, scales, _ = make(9, 1, 200, 21, 32, F16)
+    want = b.few_weight_from_codes(wq, scales, 32).export()
+    buf = torch.zeros(21 * 200 + 1, dtype=torch.int8, device="cuda")
+    buf[1:] = wq.flatten()
+    got = b.few_weight_from_codes(buf[1:].view(21, 200), scales, 32).export()
+    assert all(np.array_equal(p, q) for p, q in zip(got, want))
+    W = torch.randn(21, 200, device="cuda").half()
+    want = b.few_weight_prepare(W, 64).export()
+    buf = torch.zeros(21 * 200 + 1, dtype=F16, device="cuda")
+    buf[1:] = W.flatten()
+    got = b.few_weight_prepare(buf[1:].view(21, 200), 64).export()
+    assert all(np.array_equal(p, q) for p, q in zip(got, want))
+
+
 @pytest.mark.parametrize("group", [32, 64, 128])
 @pytest.mark.parametrize("N,K", [(40, 328), (16, 128), (5, 1000), (1, 8)])
 def test_round_to_nearest(N, K, group):

@@ -253,6 +253,22 @@ def test_another_stream_and_graphs(shape):
     assert all(torch.equal(p, q) for p, (_, q) in zip(want, graphs))
 
 
+def test_two_streams_at_once():
+    gpu()
+    made = [(make(30 + i, *s, F16), n) for i, (s, n) in enumerate((((2, 4096, 320), 32), ((1, 100000, 128), 32)))]
+    g = [grouping(20 + i, x.shape[2], x.shape[1], 6, 8, 1, True) for i, ((x, *_), _) in enumerate(made)]
+    call = lambda i, **k: (b.group_norm(made[i][0][0], made[i][1], *made[i][0][1:3], add=made[i][0][3], **k),
+                           b.group_norm_quantize(g[i], made[i][0][0], made[i][1], *made[i][0][1:3], act=b.ACT_SILU, **k))
+    want = [call(i) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[call(i, stream=streams[i]) for _ in range(5)] for i in range(2)]
+    torch.cuda.synchronize()
+    for i in range(2):
+        for out in got[i]:
+            assert all(torch.equal(p, q) for p, q in zip(want[i], out))
+
+
 def test_many_calls_in_a_row_and_a_workspace_of_the_callers():
     gpu()
     shapes = [(2, 64, 1280), (1, 300, 64), (2, 4096, 320), (1, 90000, 128), (3, 7, 24)]

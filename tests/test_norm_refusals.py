@@ -39,7 +39,8 @@ def test_workspace_bytes():
     assert need(2, 64, 1280, 32, 0) == (0, 0) and need(1, 1 << 18, 128, 32, 0)[1] > 0
     for bad in ((0, 1, 8, 1), (1, 0, 8, 1), (1, 1, 0, 1), (1, 1, 8, 0), (1, 1, 8, 3)):
         assert need(*bad)[0] == INVALID
-    assert need(1, 1, 12, 1)[0] == UNSUPPORTED and need(1, 1, 4104, 1)[0] == UNSUPPORTED
+    for bad in ((1, 1, 12, 1), (1, 1, 4104, 1), (65536, 1, 8, 1), (2 ** 31 - 1, 1, 8, 1), (1, (1 << 30) + 1, 8, 1), (1, 2 ** 31 - 1, 8, 1)):
+        assert need(*bad)[0] == UNSUPPORTED
     assert b.lib().dgq_group_norm_workspace_bytes(1, 1, 8, 1, 1, None) == INVALID
     for B in (1, 7, 300, 65535):
         assert need(B, 1000, 64, 8)[1] >= B * 8 * 16
