@@ -1100,7 +1100,8 @@ static dgq_status gn_codes(GnArgs& a, int B, cudaStream_t stream) {
                 "one quad of the widest row");
   // one wave of blocks, as many as registers (64 a thread) and shared memory (with 5 KB of the kernel's own and the system's) allow
   auto fit = [&](int buffers) { return std::max<int>(1, std::min<size_t>(1024 / threads, 233472 / (fixed + buffers * set + 5 * 1024 + 512))); };
-  a.buffers = fit(2) == fit(1) ? 2 : 1;
+  // (one set fits beside any table, two do not beside the widest row with the most groups and cells)
+  a.buffers = fit(2) == fit(1) && fixed + 2 * set <= GN_SMEM_MAX ? 2 : 1;
   const int64_t wave = 148ll * fit(a.buffers) * step, rounds = ((int64_t)B * a.P + wave - 1) / wave;
   if (rounds == 1) a.buffers = 1;
   a.rows = (int)std::min<int64_t>(rounds * step, 1 << 30);

@@ -314,3 +314,16 @@ def test_refusals_of_the_binding():
     assert refused.value.status == 3
     empty = b.group_norm(x[:0], 8)
     assert empty.shape == (0, 10, 64) and b.group_norm(x[:, :0], 8).shape == (2, 0, 64)
+
+
+def test_codes_of_the_widest_table():
+    """Cells, statistics and channels that leave shared memory room for one set of a row's words, over more rows than one round of blocks has."""
+    gpu()
+    C, P = 4096, 600
+    x, gamma, beta, e = make(17, 1, P, C, F16)
+    rng = np.random.default_rng(18)
+    scale = np.exp(rng.uniform(-0.5, 0.5, (1, 32, 32))).astype(np.float32) / np.float32(32)
+    g = b.groups_from_host(C, P, 8, np.arange(C) % 32, np.arange(P) % 32, scale, rng.integers(0, 256, (1, 32, 32)))
+    for silu in (False, True):
+        q = b.group_norm_quantize(g, x, 2048, gamma, beta, act=b.ACT_SILU if silu else b.ACT_NONE, add=e)
+        codes_against(g, x, 2048, gamma, beta, silu, e, 0, False, q)
