@@ -18,6 +18,8 @@ constexpr int GN_MAX_PIXELS = 1 << 30;
 constexpr int GN_MAX_CODE_GROUPS = 2048;  // into codes: what shared memory holds beside the widest row
 constexpr int GN_MAX_THREADS = 512;  // one thread for every eight channels of the widest row
 constexpr size_t GN_SMEM_MAX = 232448 - 8 * 1024;  // beside what a kernel declares
+// 1 / deviation below which (bf16 only) 32 bits may not hold the differences from the mean, nor with full precision what they are multiplied with
+constexpr float GN_FAR = 0x1p-60f;
 
 struct GnArgs {
   const uint16_t* X;
@@ -576,7 +578,9 @@ __device__ __noinline__ uint32_t gn_code_exact(const GnArgs& a, const double2* s
 // 3 |beta| + |shift factor|), a SiLU's slope of at most 1.1 times that; its exponential's argument and result, the sums, the reciprocal and the
 // products by 2.2 * 2^-22 of |v| for y > 0, where |y| <= |v| + 0.28, and by 2^-22 where y < 0 and y^2 e^y < 0.55; the rounded 1 / (s L) and
 // lo / L and the two sums behind them by 2^-24 (|t| + 2 |lo| + 3 L).  In all 2^-22 (5 max(|lo|, |lo + L|) + L + 4 + inv (2.1 + 0.9 |beta| +
-// 0.3 |shift factor|)), t beyond the ends of the range being cut off there, and one unit for the last sum's own rounding.
+// 0.3 |shift factor|)), t beyond the ends of the range being cut off there, and one unit for the last sum's own rounding.  That holds as long as no
+// number leaves the range of 32 bits: a value is at most 2^21 deviations from its group's mean, so that deviations up to 2^60 (all that fp16 has) keep it
+// below 2^81, where a factor below 2^-126 costs less than 2^-69; groups of larger ones take the long form.
 constexpr uint32_t GN_ALWAYS = 0x7FFF;  // the limit of channels whose codes all take the long form
 __device__ __forceinline__ float gn_fixed(float shift, float factor, float beta) { return 2.1f + 0.9f * fabsf(beta) + 0.3f * fabsf(shift * factor); }
 // w; GN_ALWAYS where it is too large, or a scale so far out that the short form's factors may leave the range of 32 bits
@@ -722,7 +726,7 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
         t[h][1] = (float)st.y * (h ? g2.y : g2.x);
         t[h][2] = be;
         t[h][3] = t[h][4] = t[h][5] = 0.f;
-        const float fixed = gn_fixed(t[h][0], t[h][1], be);
+        const float fixed = BF && st.y < (double)GN_FAR ? INFINITY : gn_fixed(t[h][0], t[h][1], be);
         if (ROWS) {
           atomicMax(&widest, fixed < INFINITY ? __float_as_uint(fixed) : 0x7F800000u);  // (any order gives the same)
         } else {

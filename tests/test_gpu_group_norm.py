@@ -327,3 +327,44 @@ def test_codes_of_the_widest_table():
     for silu in (False, True):
         q = b.group_norm_quantize(g, x, 2048, gamma, beta, act=b.ACT_SILU if silu else b.ACT_NONE, add=e)
         codes_against(g, x, 2048, gamma, beta, silu, e, 0, False, q)
+
+
+# ------------------------------------------------------------------ bf16 maps up to the type's end
+def far_map(kind, B, P, C, groups):
+    """outlier: two values of 3e38 among those around -3e38; wide: deviations of 1e38; addend: the sums with the addend leave 32 bits; mixed: every
+    second group has deviations of 1e38, the others of 1."""
+    rng = np.random.default_rng(B + P + C)
+    n = np.clip(rng.standard_normal((B, P, C)).astype(np.float32), -3, 3)
+    e = None
+    if kind == "outlier":
+        n = np.float32(-3e38) * (1 + np.float32(0.01) * n)
+        n[0, 0, 0] = n[-1, P // 2, C // 2] = 3e38
+    elif kind == "mixed":
+        n[:, :, np.arange(C) // (C // groups) % 2 == 1] *= np.float32(1e38)
+    else:
+        n *= np.float32(1e38)
+        if kind == "addend":
+            e = torch.from_numpy(np.clip(rng.standard_normal((B, C)).astype(np.float32) * 3, -3, 3) * np.float32(1e38)).to(BF16).cuda()
+    gamma = torch.from_numpy((1 + 0.2 * rng.standard_normal(C)).astype(np.float32)).cuda()
+    beta = torch.from_numpy((0.2 * rng.standard_normal(C)).astype(np.float32)).cuda()
+    x = torch.from_numpy(n).to(BF16).cuda()
+    assert torch.isfinite(x).all()
+    return x, gamma, beta, e
+
+
+FAR_KINDS = ["outlier", "wide", "addend", "mixed"]
+
+
+@pytest.mark.parametrize("silu", [False, True])
+@pytest.mark.parametrize("bits,R,centred", [(8, 1, False), (6, 1, True), (8, 3, False), (6, 3, True)])
+@pytest.mark.parametrize("B,P,C,groups", [(2, 500, 64, 8), (1, 333, 24, 8), (1, 4096, 96, 8)])
+@pytest.mark.parametrize("kind", FAR_KINDS)
+def test_codes_of_far_bf16(kind, B, P, C, groups, bits, R, centred, silu):
+    gpu()
+    x, gamma, beta, e = far_map(kind, B, P, C, groups)
+    rng = np.random.default_rng(bits + R)
+    scale = np.exp(rng.uniform(-0.5, 0.5, (1, R, 4))).astype(np.float32) * np.float32(128.0 / 2 ** bits)  # an outlier's code is none of the ends
+    g = b.groups_from_host(C, P, bits, np.arange(C) % 4, np.arange(P) % R, scale, rng.integers(0, 2 ** bits // 4, (1, R, 4)))
+    q = b.group_norm_quantize(g, x, groups, gamma, beta, act=b.ACT_SILU if silu else b.ACT_NONE, add=e,
+                              layout=b.CODES_S8_CENTRED if centred else b.CODES_U8)
+    codes_against(g, x, groups, gamma, beta, silu, e, 0, centred, q)
