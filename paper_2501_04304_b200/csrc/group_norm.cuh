@@ -95,6 +95,19 @@ __device__ __forceinline__ float gn_silu(float y) {
   return y * r;
 }
 
+// f(channel, value) of eight 16-bit values one after the other, for the few of which 32 bits hold no part of the formula.
+template <bool BF, typename F>
+__device__ __forceinline__ uint4 gn_each(uint4 x, F f) {
+  unsigned long long lo = x.x | (unsigned long long)x.y << 32, hi = x.z | (unsigned long long)x.w << 32;
+#pragma unroll 1
+  for (int c = 0; c < 8; ++c) {  // values leave at the bottom, results enter at the top
+    const unsigned long long y = pack16<BF>(f(c, gn_up((uint16_t)lo, BF)), 0.f) & 0xFFFFu;
+    lo = lo >> 16 | hi << 48;
+    hi = hi >> 16 | y << 48;
+  }
+  return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+}
+
 // ------------------------------------------------------------------ eight channels and their groups
 // Eight neighbouring channels lie in at most two groups where a group has four channels or at least seven (SEG 2: a part of each, the
 // second one may be empty), else every channel counts as a part of its own (SEG 8).  What threads have summed up for the parts stands
@@ -158,11 +171,13 @@ struct GnEight {
 // of their deviation too); they become means and squared deviations, which the threads of a block and the blocks of the cluster join
 // relative to the first one's mean (by the same reason no worse than the number of threads times 2^-24, and that only where all the
 // deviation is that first thread's; in 64 bits their chains took 0.4 us).  Blocks write theirs into each other's shared memory, so that one barrier
-// of the cluster is all.  (bf16 has values whose squares 32 bits do not hold: groups whose deviations are not
-// finite are gone over once more with everything 2^-100 times as large.)
+// of the cluster is all.  (bf16 has values whose squares, or sums with the addend, 32 bits do not hold: groups whose deviations are not
+// finite are gone over once more with everything 2^-100 times as large, statistics and values.)
 // What bounds it where the map is small: the chain of reading, joining, waiting for the cluster and writing, about a microsecond each.
 struct GnChipStat {
-  float mean, dev;  // dev: sum of squared deviations, then 1 / sqrt(var + eps); NaN where a sum is not finite
+  // dev: sum of squared deviations, then 1 / sqrt(var + eps); NaN where a sum is not finite; negative, of 2^-100 times the values, as mean is too, where
+  // that takes the scaled form
+  float mean, dev;
 };
 template <bool BF, bool SILU, int SEG>
 __global__ void __maxnreg__(80) gn_chip_kernel(const __grid_constant__ GnArgs a) {
@@ -209,7 +224,7 @@ __global__ void __maxnreg__(80) gn_chip_kernel(const __grid_constant__ GnArgs a)
         stat[g] = GnChipStat{mean, dev < INFINITY ? __frsqrt_rn(var + a.eps) : __int_as_float(0x7FC00000)};
         finite &= dev < INFINITY;
       } else if (isnan(stat[g].dev)) {
-        stat[g] = GnChipStat{mean * 0x1p100f, dev < INFINITY ? __frsqrt_rn(var + 0x1p-126f) * 0x1p-100f : __int_as_float(0x7FC00000)};
+        stat[g] = GnChipStat{mean, dev < INFINITY ? -__frsqrt_rn(var + fmaxf(a.eps * unit * unit, 0x1p-126f)) : __int_as_float(0x7FC00000)};
       }
     };
     if (n > 0) {
@@ -315,10 +330,27 @@ __global__ void __maxnreg__(80) gn_chip_kernel(const __grid_constant__ GnArgs a)
   };
   // (the same answer in every block of the cluster: they have joined the same numbers)
   const bool finite = attempt(std::false_type{});
+  auto group = [&](int c) { return SEG == 8 ? gn_div(v * 8 + c, a.per_cpg) : part.first + (c < part.split ? 0 : 1); };
   if (BF) {
     if (__syncthreads_or(!finite)) {
       attempt(std::true_type{});
       __syncthreads();
+      bool far = false;
+      for (int c = 0; c < 8; ++c) far |= stat[group(c)].dev < 0.f;
+      if (far) {
+        uint16_t* dst = a.Y + (int64_t)b * a.yb + (p0 + line) * a.yp + c0;
+#pragma unroll 1
+        for (int k = 0; k < n; ++k, dst += lines * a.yp)
+          *reinterpret_cast<uint4*>(dst) = gn_each<BF>(rows[k * n_threads], [&](int c, float x) {
+            const GnChipStat st = stat[group(c)];
+            const float unit = st.dev < 0.f ? 0x1p-100f : 1.f;
+            const float e = a.add ? gn_up(a.add[(int64_t)b * a.ld_add + c0 + c], BF) : 0.f;
+            // (the sum first, as in the statistics: equal sums are equal to their mean)
+            const float y = fmaf((fmaf(x, unit, e * unit) - st.mean) * fabsf(st.dev), a.gamma ? a.gamma[c0 + c] : 1.f, a.beta ? a.beta[c0 + c] : 0.f);
+            return SILU ? gn_silu(y) : y;
+          });
+        return;
+      }
     }
   } else {
     __syncthreads();
@@ -332,7 +364,7 @@ __global__ void __maxnreg__(80) gn_chip_kernel(const __grid_constant__ GnArgs a)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int c = 2 * i + h;
-        const GnChipStat st = stat[SEG == 8 ? gn_div(v * 8 + c, a.per_cpg) : part.first + (c < part.split ? 0 : 1)];
+        const GnChipStat st = stat[group(c)];
         t[h][0] = addend(c) - st.mean;
         t[h][1] = st.dev * of.gamma[c];
       }
@@ -510,6 +542,9 @@ __device__ __forceinline__ float2 gn_channel(const GnEight& k, const double2& st
   return make_float2((float)((double)k.addend(i, bf) - stat.x), (float)stat.y * k.gamma[i]);
 }
 
+// Whether that leaves the range of 32 bits (see GN_FAR; a constant map may have no deviation and a mean beyond it).
+__device__ __forceinline__ bool gn_far(const double2& stat, float shift) { return stat.y < (double)GN_FAR || fabsf(shift) > 0x1p126f; }
+
 // ------------------------------------------------------------------ ... and values ...
 template <bool BF, bool SILU>
 __global__ void __launch_bounds__(GN_MAX_THREADS) gn_values_kernel(const __grid_constant__ GnArgs a) {
@@ -532,14 +567,30 @@ __global__ void __launch_bounds__(GN_MAX_THREADS) gn_values_kernel(const __grid_
   });
   if (rows == 0) return;
   unsigned long long shift[4], factor[4], beta[4];
+  bool far = false;  // whether this takes 64 bits
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 t0 = gn_channel(own, stat[gn_div(v * 8 + 2 * i, a.per_cpg)], 2 * i, BF), t1 = gn_channel(own, stat[gn_div(v * 8 + 2 * i + 1, a.per_cpg)], 2 * i + 1, BF);
     shift[i] = pack_f32x2(t0.x, t1.x);
     factor[i] = pack_f32x2(t0.y, t1.y);
     beta[i] = pack_f32x2(own.beta[2 * i], own.beta[2 * i + 1]);
+    if (BF) far |= gn_far(stat[gn_div(v * 8 + 2 * i, a.per_cpg)], t0.x) || gn_far(stat[gn_div(v * 8 + 2 * i + 1, a.per_cpg)], t1.x);
   }
   uint16_t* dst = a.Y + (int64_t)b * a.yb + (p0 + line) * a.yp + v * 8;
+  if (BF && far) {
+#pragma unroll 1
+    for (int k = 0; k < rows; ++k, src += step, dst += lines * a.yp) {
+      *reinterpret_cast<uint4*>(dst) = gn_each<BF>(ring.take(k), [&](int i, float x) {
+        const int c = v * 8 + i;
+        const double2 st = stat[gn_div(c, a.per_cpg)];
+        const double u = (double)x + (a.add ? (double)gn_up(a.add[(int64_t)b * a.ld_add + c], BF) : 0.0);
+        const float y = (float)fma((u - st.x) * st.y, a.gamma ? (double)a.gamma[c] : 1.0, a.beta ? (double)a.beta[c] : 0.0);
+        return SILU ? gn_silu(y) : y;
+      });
+      ring.request(k + GN_RING - 1, src, k + GN_RING - 1 < rows);
+    }
+    return;
+  }
 #pragma unroll 2
   for (int k = 0; k < rows; ++k, src += step, dst += lines * a.yp) {
     const uint4 x = ring.take(k);

@@ -368,3 +368,26 @@ def test_codes_of_far_bf16(kind, B, P, C, groups, bits, R, centred, silu):
     q = b.group_norm_quantize(g, x, groups, gamma, beta, act=b.ACT_SILU if silu else b.ACT_NONE, add=e,
                               layout=b.CODES_S8_CENTRED if centred else b.CODES_U8)
     codes_against(g, x, groups, gamma, beta, silu, e, 0, centred, q)
+
+
+@pytest.mark.parametrize("silu", [False, True])
+@pytest.mark.parametrize("B,P,C,groups", [(2, 500, 64, 8), (1, 333, 24, 8), (1, 1000, 96, 8), (2, 4096, 320, 32), (1, 2, 8, 1), (1, 90000, 128, 32),
+                                          (1, 70001, 8, 2), (1, 150000, 24, 8)])
+@pytest.mark.parametrize("kind", FAR_KINDS)
+def test_values_of_far_bf16(kind, B, P, C, groups, silu):
+    gpu()
+    x, gamma, beta, e = far_map(kind, B, P, C, groups)
+    against(x, groups, gamma, beta, 1e-5, silu, e, b.group_norm(x, groups, gamma, beta, act=b.ACT_SILU if silu else b.ACT_NONE, add=e))
+
+
+@pytest.mark.parametrize("P", [64, 150000])
+def test_far_bf16_with_a_large_eps_and_far_constants(P):
+    """An eps of ten times the variance counts; equal values give beta, also where 32 bits do not hold them."""
+    gpu()
+    x, gamma, beta, _ = far_map("wide", 1, P, 64, 8)
+    x = (x.double() * 1e-20).to(BF16)
+    against(x, 8, gamma, beta, 1e37, False, None, b.group_norm(x, 8, gamma, beta, eps=1e37))
+    x.fill_(3e38)
+    e = torch.full((1, 64), 2e38, dtype=BF16, device="cuda")
+    for add in (None, e):
+        assert torch.equal(b.group_norm(x, 8, gamma, beta, add=add), beta.to(BF16).expand(1, P, 64))
