@@ -340,7 +340,8 @@ __global__ void __launch_bounds__(few_most_warps(MT) * 32) few_kernel(const __gr
             const float v0 = gn_silu(f.x), v1 = gn_silu(f.y);
             h[z] = pack16<BF>(v0, v1);
             const float2 g = unpack16<BF>(h[z]);
-            l[z] = pack16<BF>(v0 - g.x, v1 - g.y);
+            // (an infinity leaves nothing: inf - inf would be NaN)
+            l[z] = pack16<BF>(g.x < INFINITY ? v0 - g.x : 0.f, g.y < INFINITY ? v1 - g.y : 0.f);
           }
         }
         asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");

@@ -201,3 +201,25 @@ def test_refusals():
         assert e.value.status == 1
     with pytest.raises(b.DgqError):  # rows of 60 channels do not start on 16 bytes
         b.linear_few(b.few_weight_from_codes(wq[:, :56].contiguous(), scales, 64), torch.zeros(2, 60, dtype=F16, device="cuda")[:, :56])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("M", [1, 8, 12, 30, 70])
+def test_infinities_and_silu(M, group, dtype):
+    """silu(inf) is inf: the outputs are infinities of the codes' signs; the other rows are what they were."""
+    gpu()
+    K, N = 712, 100
+    x, wq, scales, c = make(10 + M, M, K, N, group, dtype)
+    at = [3, K - 1, 300]
+    sign = torch.where(torch.arange(N, device="cuda") % 3 == 0, -1, 1).to(torch.int8)
+    for k in at:
+        wq[:, k] = sign * (1 + k % 7)
+    w = b.few_weight_from_codes(wq, scales, group)
+    want = b.linear_few(w, x, bias=c, act=b.ACT_SILU)
+    rows = sorted({0, M // 2, M - 1})
+    for i, m in enumerate(rows):
+        x[m, at[i]] = float("inf")
+        want[m] = sign.to(dtype) * float("inf")
+    assert torch.equal(b.linear_few(w, x, bias=c, act=b.ACT_SILU), want)
+    assert torch.equal(b.linear_few(w, x, bias=c)[rows], want[rows])
