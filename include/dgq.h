@@ -317,8 +317,8 @@ enum { DGQ_ACT_NONE = 0, DGQ_ACT_SILU = 1 }; /* SiLU: y / (1 + e^-y) */
  * image and channel (dev [B, C] of the same type, rows ld_add elements apart, 0 for one that all images share; NULL: none):
  *   u = x + add[b, c];  y = (u - mean) / sqrt(var + eps) * gamma[c] + beta[c];  Y = act(y), rounded once,
  * mean and (biased) variance over the P pixels and C / n_groups neighbouring channels of a group.  gamma, beta: dev fp32 [C], NULL for 1
- * and 0.  Sums are held in 32 bits or more.  A group that holds a value that is not finite gives NaN.  Y may be X (the
- * same pointer and strides); it may not overlap X otherwise.
+ * and 0.  Sums are held in 32 bits or more.  A group that holds a value that is not finite gives NaN.  (Of a y far
+ * below nought a SiLU leaves up to 2^-60 |y|.)  Y may be X (the same pointer and strides); it may not overlap X otherwise.
  * C a multiple of 8 up to 4096, any n_groups that divides it, eps at least 2^-126.
  * workspace: dev, 256-byte aligned, at least dgq_group_norm_workspace_bytes(); contents undefined on entry and exit; calls that may
  * overlap on the GPU need separate ones.

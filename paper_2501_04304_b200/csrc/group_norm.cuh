@@ -73,20 +73,26 @@ __device__ __forceinline__ unsigned long long gn_pair(uint32_t w) {
   return pack_f32x2(f.x, f.y);
 }
 
-// y / (1 + e^-y) of two values with three special-function operations: the reciprocal is that of the product of both denominators.  The
-// exponents stop at 2^60, so that the product stays in range; what that leaves of a value below -41 is off by less than 2^-60 |y|.
+// y / (1 + e^-y) of two values with three special-function operations: the reciprocal is that of the product of both denominators e0 and e1.  The
+// exponents stop at 2^60, so that the product stays in range; what that leaves of a value below -41 is less than 2^-60 |y| (a bound on y itself would
+// leave nothing, and cost 2 % of a large map's time).  ANY: e1 / (e0 e1) first, since y e1 leaves the range where y is beyond 2^68; else y is not
+// (gn_far_silu) and y e1 is there before the reciprocal (large fp16 maps: 45.7 against 47.7 us for 1 x 262144 x 128; bf16 takes the same for both, and on
+// the chip the question costs more than the product).
 __device__ __forceinline__ void gn_silu_parts(float y0, float y1, float k0, float k1, float& e0, float& e1, float& per) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(fminf(y0 * k0, 60.f)));
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(fminf(y1 * k1, 60.f)));
   e0 += 1.f, e1 += 1.f;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(per) : "f"(e0 * e1));
 }
-__device__ __forceinline__ void gn_silu2(float y0, float y1, float k0, float k1, float& v0, float& v1) {
+template <bool ANY>
+__device__ __forceinline__ void gn_silu2(float y0, float y1, float& v0, float& v1) {
   float e0, e1, per;
-  gn_silu_parts(y0, y1, k0, k1, e0, e1, per);
-  v0 = y0 * e1 * per;
-  v1 = y1 * e0 * per;
+  gn_silu_parts(y0, y1, -1.4426950408889634f, -1.4426950408889634f, e0, e1, per);
+  v0 = ANY ? y0 * (e1 * per) : y0 * e1 * per;
+  v1 = ANY ? y1 * (e0 * per) : y1 * e0 * per;
 }
+// Whether y may be beyond 2^68: a value is at most 2^21 deviations from its group's mean.
+__device__ __forceinline__ bool gn_far_silu(float gamma, float beta) { return fmaxf(fabsf(gamma), fabsf(beta)) > 0x1p46f; }
 // y / (1 + e^-y) of one value
 __device__ __forceinline__ float gn_silu(float y) {
   float e, r;
@@ -382,7 +388,7 @@ __global__ void __maxnreg__(80) gn_chip_kernel(const __grid_constant__ GnArgs a)
         const unsigned long long y = fma_f32x2(add_f32x2(gn_pair<BF>(w[i]), shift[i]), factor[i], beta[i]);
         float y0, y1;
         unpack_f32x2(y, y0, y1);
-        if (SILU) gn_silu2(y0, y1, -1.4426950408889634f, -1.4426950408889634f, y0, y1);
+        if (SILU) gn_silu2<true>(y0, y1, y0, y1);
         w[i] = pack16<BF>(y0, y1);
       }
       *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -575,9 +581,10 @@ __global__ void __launch_bounds__(GN_MAX_THREADS) gn_values_kernel(const __grid_
     factor[i] = pack_f32x2(t0.y, t1.y);
     beta[i] = pack_f32x2(own.beta[2 * i], own.beta[2 * i + 1]);
     if (BF) far |= gn_far(stat[gn_div(v * 8 + 2 * i, a.per_cpg)], t0.x) || gn_far(stat[gn_div(v * 8 + 2 * i + 1, a.per_cpg)], t1.x);
+    else if (SILU) far |= gn_far_silu(own.gamma[2 * i], own.beta[2 * i]) || gn_far_silu(own.gamma[2 * i + 1], own.beta[2 * i + 1]);
   }
   uint16_t* dst = a.Y + (int64_t)b * a.yb + (p0 + line) * a.yp + v * 8;
-  if (BF && far) {
+  if ((BF || SILU) && far) {
 #pragma unroll 1
     for (int k = 0; k < rows; ++k, src += step, dst += lines * a.yp) {
       *reinterpret_cast<uint4*>(dst) = gn_each<BF>(ring.take(k), [&](int i, float x) {
@@ -601,7 +608,7 @@ __global__ void __launch_bounds__(GN_MAX_THREADS) gn_values_kernel(const __grid_
       const unsigned long long y = fma_f32x2(add_f32x2(gn_pair<BF>(w[i]), shift[i]), factor[i], beta[i]);
       float y0, y1;
       unpack_f32x2(y, y0, y1);
-      if (SILU) gn_silu2(y0, y1, -1.4426950408889634f, -1.4426950408889634f, y0, y1);
+      if (SILU) gn_silu2<BF>(y0, y1, y0, y1);
       w[i] = pack16<BF>(y0, y1);
     }
     ring.request(k + GN_RING - 1, src, k + GN_RING - 1 < rows);  // into the piece before this one
@@ -629,11 +636,14 @@ __device__ __noinline__ uint32_t gn_code_exact(const GnArgs& a, const double2* s
 // 3 |beta| + |shift factor|), a SiLU's slope of at most 1.1 times that; its exponential's argument and result, the sums, the reciprocal and the
 // products by 2.2 * 2^-22 of |v| for y > 0, where |y| <= |v| + 0.28, and by 2^-22 where y < 0 and y^2 e^y < 0.55; the rounded 1 / (s L) and
 // lo / L and the two sums behind them by 2^-24 (|t| + 2 |lo| + 3 L).  In all 2^-22 (5 max(|lo|, |lo + L|) + L + 4 + inv (2.1 + 0.9 |beta| +
-// 0.3 |shift factor|)), t beyond the ends of the range being cut off there, and one unit for the last sum's own rounding.  That holds as long as no
+// 0.3 |shift factor| + 2^-17 |gamma|)), t beyond the ends of the range being cut off there, and one unit for the last sum's own rounding; the term of gamma
+// is what a SiLU leaves of an argument far below nought, 2^-60 |y| with |y - beta| <= 2^21 |gamma|.  That holds as long as no
 // number leaves the range of 32 bits: a value is at most 2^21 deviations from its group's mean, so that deviations up to 2^60 (all that fp16 has) keep it
 // below 2^81, where a factor below 2^-126 costs less than 2^-69; groups of larger ones take the long form.
 constexpr uint32_t GN_ALWAYS = 0x7FFF;  // the limit of channels whose codes all take the long form
-__device__ __forceinline__ float gn_fixed(float shift, float factor, float beta) { return 2.1f + 0.9f * fabsf(beta) + 0.3f * fabsf(shift * factor); }
+__device__ __forceinline__ float gn_fixed(float shift, float factor, float gamma, float beta) {
+  return 2.1f + 0.9f * fabsf(beta) + 0.3f * fabsf(shift * factor) + 0x1p-17f * fabsf(gamma);
+}
 // w; GN_ALWAYS where it is too large, or a scale so far out that the short form's factors may leave the range of 32 bits
 template <bool EIGHT>
 __device__ __forceinline__ uint32_t gn_limit(float inv, float lo, float Lf, float fixed) {
@@ -777,7 +787,7 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
         t[h][1] = (float)st.y * (h ? g2.y : g2.x);
         t[h][2] = be;
         t[h][3] = t[h][4] = t[h][5] = 0.f;
-        const float fixed = BF && st.y < (double)GN_FAR ? INFINITY : gn_fixed(t[h][0], t[h][1], be);
+        const float fixed = BF && st.y < (double)GN_FAR ? INFINITY : gn_fixed(t[h][0], t[h][1], h ? g2.y : g2.x, be);
         if (ROWS) {
           atomicMax(&widest, fixed < INFINITY ? __float_as_uint(fixed) : 0x7F800000u);  // (any order gives the same)
         } else {
@@ -845,7 +855,7 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
               c0 = cell[mine + (int)(__float_as_uint(k1.w) & 0xFFFFu)], c1 = cell[mine + (int)(__float_as_uint(k1.w) >> 16)];
             }
             y0 = fmaf(y0, k0.z, k1.x), y1 = fmaf(y1, k0.w, k1.y);
-            if (SILU) gn_silu2(y0, y1, -1.4426950408889634f, -1.4426950408889634f, y0, y1);
+            if (SILU) gn_silu2<true>(y0, y1, y0, y1);
             y0 = gn_fma_sat(y0, c0.x, c0.y), y1 = gn_fma_sat(y1, c1.x, c1.y);
             bias0 = gn_bias<EIGHT>(__float_as_uint(c0.z)), bias1 = gn_bias<EIGHT>(__float_as_uint(c1.z));
             m[0][j] = __float_as_uint(fmaf(y0, Lf, bias0)) << (EIGHT ? 1 : 0);
@@ -857,7 +867,7 @@ __global__ void __maxnreg__(64) gn_codes_kernel(const __grid_constant__ GnArgs a
             y0 = fmaf(y0, k0.z, k1.x), y1 = fmaf(y1, k0.w, k1.y);
             float e0, e1, per;
             gn_silu_parts(y0, y1, k2.x, k2.y, e0, e1, per);
-            y0 = gn_fma_sat(y0 * e1, per, k2.z), y1 = gn_fma_sat(y1 * e0, per, k2.w);
+            y0 = gn_fma_sat(y0, e1 * per, k2.z), y1 = gn_fma_sat(y1, e0 * per, k2.w);
           } else {
             y0 = gn_fma_sat(y0, k0.z, k1.x), y1 = gn_fma_sat(y1, k0.w, k1.y);
           }

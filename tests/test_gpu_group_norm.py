@@ -391,3 +391,40 @@ def test_far_bf16_with_a_large_eps_and_far_constants(P):
     e = torch.full((1, 64), 2e38, dtype=BF16, device="cuda")
     for add in (None, e):
         assert torch.equal(b.group_norm(x, 8, gamma, beta, add=add), beta.to(BF16).expand(1, P, 64))
+
+
+@pytest.mark.parametrize("size", [1e12, 1e22, 1e30])
+@pytest.mark.parametrize("P", [300, 150000])
+def test_silu_of_far_values(P, size):
+    """Factors so large that a SiLU's argument is far out: it is the argument or, below, at most 2^-60 of it (and its rounding)."""
+    gpu()
+    x, gamma, beta, _ = make(19, 1, P, 24, BF16, add=False)
+    gamma = gamma * size
+    y = b.group_norm(x, 8, gamma, beta, act=b.ACT_SILU)
+    v, u, c = nl.norm(x, 8, gamma, beta, 1e-5, True)
+    nl.check(y, v, nl.norm_bound(v, u, c, BF16))
+    assert (y.cpu().double().abs() <= 2.0 ** -59 * u.abs())[u < -100].all()
+
+
+@pytest.mark.parametrize("size", [1e12, 1e16, 1e22, 1e30])
+@pytest.mark.parametrize("R", [1, 2])
+def test_codes_of_far_silus(R, size):
+    gpu()
+    x, gamma, beta, _ = make(20, 1, 300, 64, F16, add=False)
+    x[:, 150:] = -x[:, :150]  # a mean of 0, so that nothing but the factor is large
+    gamma = gamma * size
+    for bits, centred in ((8, False), (6, True)):
+        g = grouping(13, 64, 300, bits, 4, R, True)
+        q = b.group_norm_quantize(g, x, 8, gamma, beta, act=b.ACT_SILU, layout=b.CODES_S8_CENTRED if centred else b.CODES_U8)
+        codes_against(g, x, 8, gamma, beta, True, None, 0, centred, q)
+
+
+@pytest.mark.parametrize("P", [300, 150000])
+def test_silu_of_far_values_f16(P):
+    gpu()
+    x, gamma, beta, _ = make(19, 1, P, 24, F16, add=False)
+    gamma = gamma * 1e22
+    y = b.group_norm(x, 8, gamma, beta, act=b.ACT_SILU).cpu().double()
+    _, u, _ = nl.norm(x, 8, gamma, beta, 1e-5, True)
+    assert torch.isposinf(y[u > 1e6]).all()
+    assert (y.abs() <= 2.0 ** -59 * u.abs())[u < -1e6].all()
