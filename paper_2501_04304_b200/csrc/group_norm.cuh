@@ -40,7 +40,7 @@ struct GnArgs {
   int past;                 // values: the output is as large as half of L2
   int rows;                 // values and codes: rows of a block
   float eps;
-  double per_count;  // 1 / (P cpg)
+  double count, per_count;  // P cpg, 1 / (P cpg)
   double2* part;  // [B][clusters][n_groups]
   // codes
   uint8_t* Xq;
@@ -535,7 +535,9 @@ __device__ __forceinline__ void gn_stats(const GnArgs& a, int b, double2* stat, 
       s += __shfl_xor_sync(0xffffffffu, s, o);
       q += __shfl_xor_sync(0xffffffffu, q, o);
     }
-    const double mean = s * a.per_count;
+    // s / count, rounded: a map of equal values has them for its mean, and nothing is left of u - mean, whatever it is multiplied with
+    double mean = s * a.per_count;
+    mean = fma(fma(-a.count, mean, s), a.per_count, mean);
     double var = fma(-mean, mean, q * a.per_count);
     if (var < 0.0) var = 0.0;
     if (sub == 0) stat[g] = make_double2(mean, rsqrt(var + (double)a.eps));
@@ -1054,7 +1056,8 @@ static void gn_fill(GnArgs& a, const dgq_rows* X, const void* add, int64_t ld_ad
   a.eps = eps;
   a.part = (double2*)workspace;
   a.per_cpg = 1.f / (float)a.cpg;
-  a.per_count = 1.0 / ((double)P * (double)a.cpg);
+  a.count = (double)P * (double)a.cpg;
+  a.per_count = 1.0 / a.count;
 }
 static void gn_shape(GnArgs& a, int nvec, int lines) {
   a.nvec = nvec;

@@ -428,3 +428,17 @@ def test_silu_of_far_values_f16(P):
     _, u, _ = nl.norm(x, 8, gamma, beta, 1e-5, True)
     assert torch.isposinf(y[u > 1e6]).all()
     assert (y.abs() <= 2.0 ** -59 * u.abs())[u < -1e6].all()
+
+
+@pytest.mark.parametrize("R", [1, 2])
+@pytest.mark.parametrize("value", [7.0, 9984.0, 222 * 2.0 ** 60, 222 * 2.0 ** 120])
+@pytest.mark.parametrize("P,groups", [(333, 8), (75, 24), (25, 8), (77, 24)])
+def test_codes_of_constant_maps(P, groups, value, R):
+    """Equal values, 75 of them (whose sum times the reciprocal of 75 need not be them) among others: the code of beta, however far out they are."""
+    gpu()
+    x, gamma, beta, _ = make(21, 1, P, 24, BF16, add=False)
+    x.fill_(value)
+    assert (x.double() == value).all()
+    g = grouping(14, 24, P, 8, 3, R, False)
+    q = b.group_norm_quantize(g, x, groups, gamma, beta)
+    codes_against(g, x, groups, gamma, beta, False, None, 0, False, q)
