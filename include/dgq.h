@@ -322,7 +322,7 @@ enum { DGQ_ACT_NONE = 0, DGQ_ACT_SILU = 1 }; /* SiLU: y / (1 + e^-y) */
  * C a multiple of 8 up to 4096, any n_groups that divides it, eps at least 2^-126.
  * workspace: dev, 256-byte aligned, at least dgq_group_norm_workspace_bytes(); contents undefined on entry and exit; calls that may
  * overlap on the GPU need separate ones.
- * Errors: INVALID_ARG (also: pixel rows of Y that overlap), ALIGNMENT, UNSUPPORTED (also: B > 65535, P > 2^30), WORKSPACE, CUDA. */
+ * Errors: INVALID_ARG (also: pixel rows of Y, of one image or of two, that overlap), ALIGNMENT, UNSUPPORTED (also: B > 65535, P > 2^30), WORKSPACE, CUDA. */
 dgq_status dgq_group_norm(const dgq_rows* X, const void* add, int64_t ld_add, const float* gamma, const float* beta,
                           const dgq_rows* Y, int dtype, int B, int P, int C, int n_groups, float eps, int act, void* workspace,
                           size_t workspace_bytes, void* stream);

@@ -1039,6 +1039,18 @@ static dgq_status gn_check(const dgq_rows* X, const void* add, int64_t ld_add, i
   if (C % 8 || C > GN_MAX_C || P > GN_MAX_PIXELS || B > 65535) return DGQ_ERR_UNSUPPORTED;
   return rows_check(*X, B, P, 1, false);
 }
+// Whether two rows of C elements of an output with pixels at least C apart meet: rows p of image 0 and q of image d do if d * batch lies within C of (p - q) * token.
+static bool gn_overlap(const dgq_rows& y, int B, int P, int C) {
+  if (B == 1) return false;
+  if (P == 1 || y.batch < C) return y.batch < C;
+  if (y.token >= (B - 1) * y.batch + C) return false;  // pixels outermost
+  for (int64_t d = 1; d < B; ++d) {
+    const int64_t p = d * y.batch / y.token, past = d * y.batch % y.token;
+    if (p >= P) return false;  // images outermost from here on
+    if (past < C || (p + 1 < P && y.token - past < C)) return true;
+  }
+  return false;
+}
 static void gn_fill(GnArgs& a, const dgq_rows* X, const void* add, int64_t ld_add, const float* gamma, const float* beta, int B, int P, int C,
                     int n_groups, float eps, void* workspace) {
   const dgq_rows x = rows_normal(*X, B, P, 1);
@@ -1203,6 +1215,7 @@ extern "C" dgq_status dgq_group_norm(const dgq_rows* X, const void* add, int64_t
   if (P > 1 && Y->token < C) return DGQ_ERR_INVALID_ARG;
   const size_t need = gn_chip_plan(B, P, C, C / n_groups).ok ? 0 : gn_sums_bytes(B, P, C, n_groups);
   if ((st = gn_workspace_check(need, workspace, workspace_bytes)) != DGQ_OK) return st;
+  if (gn_overlap(*Y, B, P, C)) return DGQ_ERR_INVALID_ARG;
   GnArgs a = {};
   gn_fill(a, X, add, ld_add, gamma, beta, B, P, C, n_groups, eps, workspace);
   const dgq_rows y = rows_normal(*Y, B, P, 1);

@@ -442,3 +442,28 @@ def test_codes_of_constant_maps(P, groups, value, R):
     g = grouping(14, 24, P, 8, 3, R, False)
     q = b.group_norm_quantize(g, x, groups, gamma, beta)
     codes_against(g, x, groups, gamma, beta, False, None, 0, False, q)
+
+
+def test_images_apart_and_overlapping():
+    """Every distance of images and of pixels up to 13 times eight channels: what does not overlap is written as it is asked for, all else refused."""
+    gpu()
+    B, P, C = 3, 4, 16
+    x, gamma, beta, _ = make(23, B, P, C, F16, add=False)
+    want = b.group_norm(x, 2, gamma, beta)
+    refused = 0
+    for batch in range(0, 104, 8):
+        for token in range(0, 104, 8):
+            buf = torch.full((4096,), 7.0, dtype=F16, device="cuda")
+            out = buf.as_strided((B, P, C), (batch, token, 1))
+            places = (torch.arange(B)[:, None, None] * batch + torch.arange(P)[:, None] * token + torch.arange(C)).flatten()
+            if places.unique().numel() < B * P * C:
+                refused += 1
+                with pytest.raises(b.DgqError) as e:
+                    b.group_norm(x, 2, gamma, beta, out=out)
+                assert e.value.status == 1 and (buf == 7).all()
+            else:
+                b.group_norm(x, 2, gamma, beta, out=out)
+                left = torch.full_like(buf, 7.0)
+                left[places.cuda()] = want.flatten()
+                assert torch.equal(buf, left)
+    assert 80 < refused < 160

@@ -76,3 +76,9 @@ def test_large_integers():
         b.native().linear_few(0, 2 ** 31, 64, None, 0, None, None, None)
     with pytest.raises(ValueError, match="32 bits"):
         b.native().group_norm(None, 2 ** 32 + 8, None, None, 1e-5, 0, None, None, None, None)
+
+
+@pytest.mark.parametrize("B,P,batch,token", [(2, 1 << 20, 4096, 256), (2, 16, 64, 64), (2, 16, 960, 64), (3, 16, 512, 256), (2, 1, 56, 64), (2, 3, 8, 64), (4, 3, 64, 192),
+                                             (65535, 2, 64, 65534 * 64), (3, 1 << 30, 1 << 36, 72), (2, 4, 176, 128)])
+def test_images_that_overlap(B, P, batch, token):
+    assert norm(Y=rows(batch=batch, token=token), B=B, P=P) == INVALID
