@@ -354,8 +354,9 @@ dgq_status dgq_few_weight_destroy(dgq_few_weight* w);
 dgq_status dgq_few_weight_export(const dgq_few_weight* w, int8_t* wq, uint16_t* scales);
 /* Y[m, n] = bias[n] + sum_g s[n, g] * sum over the channels k of group g of q[n, k] * act(X[m, k]), summed in fp32 and rounded once.
  * X dev [M, K], Y dev [M, N], bias dev [N] or NULL, all of type `dtype`; X 16-byte aligned, its rows ldx elements apart (a multiple of 8,
- * 0 allowed), those of Y ldy.  SiLU's results enter the product as two numbers of `dtype` (good to 2^-16 of them, fp16 2^-21).  Any M; the weight is read once for every 32 rows,
- * so that for many rows dgq_linear is the better call.
+ * 0 allowed), those of Y ldy.  SiLU's results enter the product as two numbers of `dtype`, off by at most 2^-15 of them and 2^-119 (bf16), 2^-20 of
+ * them and 2^-25 (fp16, whose second number is below the smallest normal one where the result is below 1/8).  A sum over a group's q and x that fp32 does
+ * not hold is infinite.  Any M; the weight is read once for every 32 rows, so that for many rows dgq_linear is the better call.
  * Errors: INVALID_ARG (also: a weight of another device than the current one), ALIGNMENT, UNSUPPORTED (M > 2^21 - 32), CUDA. */
 dgq_status dgq_linear_few(const dgq_few_weight* w, const void* X, int64_t ldx, int dtype, int M, int act, const void* bias, void* Y,
                           int64_t ldy, void* stream);

@@ -299,7 +299,8 @@ __global__ void __launch_bounds__(512, 2) few_rows_kernel(const __grid_constant_
 // A block has wn tiles of outputs and MT times eight rows.  Its warps split the input channels (2^log_wk ways, every warp four neighbouring blocks
 // of 64 of a chunk) and the tiles; the rows of a chunk stand in shared memory for all of them, three chunks in turn, so that one barrier a chunk is
 // enough.  A warp's weights are asked for a chunk ahead, in registers.  A SiLU's results enter as a 16-bit number and what it leaves of
-// the 32-bit one, rounded too: rounded once only, they would put half as much error again on the result's own.
+// the 32-bit one, rounded too: rounded once only, they would put half as much error again on the result's own.  (Half a step of half a step, 2^-16 or
+// 2^-22 of the result; in fp16 at least 2^-25, the second number being subnormal where the result is below 1/8; and the 32-bit SiLU's own error.)
 template <bool BF, bool G32, int MT, bool SILU>
 __global__ void __launch_bounds__(few_most_warps(MT) * 32) few_kernel(const __grid_constant__ FewArgs a) {
   extern __shared__ __align__(16) unsigned char few_smem[];

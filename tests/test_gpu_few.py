@@ -223,3 +223,21 @@ def test_infinities_and_silu(M, group, dtype):
         want[m] = sign.to(dtype) * float("inf")
     assert torch.equal(b.linear_few(w, x, bias=c, act=b.ACT_SILU), want)
     assert torch.equal(b.linear_few(w, x, bias=c)[rows], want[rows])
+
+
+@pytest.mark.parametrize("M", [2, 12, 30])
+@pytest.mark.parametrize("size", [1.0, 1e-2, 1e-3, 1e-5])
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+def test_silu_of_small_rows(dtype, size, M):
+    """A SiLU's results are good to 2^-20 of them and 2^-25 (fp16), 2^-15 of them and 2^-119 (bf16): a part each of the sum of the terms' sizes and of the
+    weights'.  Beside them the output's rounding and the sums' (as in few_bound)."""
+    gpu()
+    K, N, group = 320, 64, 64
+    x, wq, scales, _ = make(20 + M, M, K, N, group, dtype, bias=False)
+    x = (x.double() * size).to(dtype)
+    y = b.linear_few(b.few_weight_from_codes(wq, scales, group), x, act=b.ACT_SILU)
+    ref, terms = nl.few(x, wq, scales, group, True, None)
+    _, weights = nl.few(torch.ones_like(x), wq, scales, group, False, None)
+    part, least = (2.0 ** -20, 2.0 ** -25) if dtype == F16 else (2.0 ** -15, 2.0 ** -119)
+    limit = nl.HALF_STEP[dtype] * ref.abs() + 2.0 ** -25 * (dtype == F16) + ((K / 16 + 30) * 2.0 ** -23 + part) * terms + least * weights
+    nl.check(y, ref, limit)
