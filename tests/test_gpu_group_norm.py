@@ -467,3 +467,41 @@ def test_images_apart_and_overlapping():
                 left[places.cuda()] = want.flatten()
                 assert torch.equal(buf, left)
     assert 80 < refused < 160
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("B,P,C,groups", [(2, 64, 1280, 32), (1, 333, 320, 32), (1, 257, 72, 24), (3, 37, 24, 8)])
+@pytest.mark.parametrize("bits,G,R,centred,z", [(8, 5, 1, True, 128), (8, 5, 3, True, 128), (7, 4, 1, True, None), (7, 4, 3, True, None), (7, 4, 1, False, None),
+                                                (5, 3, 2, True, None), (3, 3, 1, True, None), (3, 2, 4, False, None)])
+def test_codes_of_other_widths(B, P, C, groups, dtype, bits, G, R, centred, z):
+    """Zero-centred codes of 8 bits (their zero-point is 128), of 7, the most that leave a bit free, and of odd widths."""
+    gpu()
+    x, gamma, beta, e = make(B + P + C + bits, B, P, C, dtype, add=P % 2 == 0)
+    for silu in (False, True):
+        g = grouping(P + bits, C, P, bits, G, R, silu, z=z)
+        q = b.group_norm_quantize(g, x, groups, gamma, beta, act=b.ACT_SILU if silu else b.ACT_NONE, add=e,
+                                  layout=b.CODES_S8_CENTRED if centred else b.CODES_U8)
+        codes_against(g, x, groups, gamma, beta, silu, e, 0, centred, q)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 70, 64), (2, 5000, 320), (2, 120000, 64)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_addends_that_are_not_finite(shape, bad, dtype):
+    """The group of that image is NaN, and its codes are 0; the others are what they were."""
+    gpu()
+    x, gamma, beta, e = make(22, *shape, dtype)
+    n = shape[2] // 16
+    at = slice(5 // n * n, 5 // n * n + n)
+    g = grouping(15, shape[2], shape[1], 8, 4, 1, False)
+    place = torch.from_numpy(np.argsort(np.where((p := g.export()["perm"]) < 0, 1 << 20, p), kind="stable")[:shape[2]]).cuda()  # of every channel
+    clean, codes = b.group_norm(x, 16, gamma, beta, add=e), b.group_norm_quantize(g, x, 16, gamma, beta, add=e)
+    e[1, 5] = bad
+    y, q = b.group_norm(x, 16, gamma, beta, add=e), b.group_norm_quantize(g, x, 16, gamma, beta, add=e)
+    assert torch.isnan(y[1, :, at]).all()
+    y[1, :, at] = clean[1, :, at]
+    assert torch.equal(y, clean)
+    rows = slice(shape[1], 2 * shape[1])
+    assert (q[rows][:, place[at]] == 0).all()
+    q[rows][:, place[at]] = codes[rows][:, place[at]]
+    assert torch.equal(q, codes)
