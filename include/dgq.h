@@ -330,7 +330,7 @@ dgq_status dgq_group_norm(const dgq_rows* X, const void* add, int64_t ld_add, co
  * of `timestep` (row i = b * P + p is pixel position i mod the grouping's own P), C channels of the grouping.  The value that is
  * quantized is act(y) itself, not its rounding to 16 bits:
  *   q = clamp(rint(act(y) * inv_s) + Z, 0, 2^b - 1)   as 64-bit arithmetic on the 16-bit inputs gives it (inv_s is the table's fp32
- * number): the codes do not depend on how the sums were split.  NaN gives code 0.
+ * number; var is a difference of 64-bit sums, off by 2^-50 of mean^2 + add^2): the codes do not depend on how the sums were split.  NaN gives code 0.
  * DGQ_CODES_S8_CENTRED has the limits of dgq_quantize_act.  Xq is 16-byte aligned and does not overlap X.  n_groups at most 2048.
  * Errors: as above, NOT_CALIBRATED, INVALID_ARG also for a grouping of another device than the current one. */
 dgq_status dgq_group_norm_quantize(const dgq_groups* g, int timestep, int layout, const dgq_rows* X, const void* add,

@@ -227,8 +227,8 @@ __device__ __forceinline__ void few_join(const FewArgs& a, unsigned char* smem, 
 
 // Up to eight rows as they are: a block has one tile, its warps split the input channels (four neighbouring blocks of 64 of a chunk for each),
 // and every lane reads its part of its row straight from memory, which the multiprocessor's blocks do at about the same time, a block of 64 ahead;
-// weights are asked for four blocks ahead.  Without barriers and shared memory as many warps are there as registers allow (7 x 5000 x 10007:
-// with the rows in shared memory, three chunks of 4 x 4 blocks, 17 us).
+// weights are asked for four blocks ahead.  No barriers, and shared memory for the join alone (7 x 5000 x 10007: 10.6 to 12.6 us; with the rows in
+// shared memory, three chunks of 4 x 4 blocks, 17).  Registers would hold 32 warps a multiprocessor, few_plan asks for sixteen.
 template <bool BF, bool G32>
 __global__ void __launch_bounds__(512, 2) few_rows_kernel(const __grid_constant__ FewArgs a) {
   extern __shared__ __align__(16) unsigned char few_smem[];

@@ -37,7 +37,7 @@ struct GnArgs {
   int log_cluster;          // blocks of a cluster (one kernel, sums)
   int slab_rows, clusters;  // sums: rows of a block, clusters of an image
   int early;                // sums: the second kernel's blocks may come in at once
-  int past;                 // values: the output is as large as half of L2
+  int past;                 // values: outputs of 48 MiB and more go past L2
   int rows;                 // values and codes: rows of a block
   float eps;
   double count, per_count;  // P cpg, 1 / (P cpg)
@@ -399,7 +399,8 @@ __global__ void __maxnreg__(80) gn_chip_kernel(const __grid_constant__ GnArgs a)
 // ------------------------------------------------------------------ two kernels: sums ...
 // For maps that do not fit, and for codes, which a row's whole width is permuted into.  The first kernel adds up x and x^2 of every channel
 // over a slab of rows, in 64 bits, puts the addend in (sum u = sum x + n add, sum u^2 = sum x^2 + 2 add sum x + n add^2) and leaves one
-// pair of sums for each group and cluster of slabs.  In 64 bits the difference of the two sums is good to 2^-52 mean^2 / var, so that there is
+// pair of sums for each group and cluster of slabs.  In 64 bits the difference of the two sums is good to 2^-52 mean^2 / var, or add^2 / var where an addend
+// takes off what the values have, so that there is
 // no second pass over the values; a conversion and two additions an element are what the 64-bit units do at the rate at which memory delivers 16-bit
 // values.  The second kernel adds the clusters up in a fixed order (every block for itself), turns them into a shift and a factor per
 // channel and passes over the map once more.  No atomics: a result does not depend on the order in which blocks run.
@@ -1026,8 +1027,11 @@ static inline GnChipPlan gn_chip_plan(int B, int P, int C, int cpg) {
     const int64_t bytes = (int64_t)rows * s.nvec * 16;
     if ((blocks * cluster >= 96 && bytes <= 48 * 1024) || bytes <= 16 * 1024) break;
   }
-  // Blocks that fill a multiprocessor each, in several rounds, read, join and write one after the other: two kernels are faster then (8 x 4096 x
-  // 960: 42 against 60 us; in one round 2 x 3000 x 1000 in 5 groups 17 against 13, smaller blocks 8 x 4096 x 640 33 against 31).
+  // Blocks that fill a multiprocessor each, in several rounds, read, join and write one after the other: two kernels are faster then (with a SiLU, one
+  // kernel against two: 1 x 16384 x 1280 46.8 and 37.9 us, 2 x 9216 x 960 39.7 and 29.2, 4 x 4096 x 960 36 and 27, 8 x 4096 x 960 62 and 43, 8 x 16384 x
+  // 320 79 and 54).  In one round one is (64 blocks, 1 x 4096 x 960: 12.5 and 15.6), though not where sixteen clusters of eight, one of which has to
+  // wait, count as one round here (128 blocks, 2 x 4096 x 960: 23.8 and 18.7).  Of smaller blocks neither is for all (8 x 4096 x 640 33.0 and 32.5,
+  // 2 x 9216 x 640 19.2 and 22.8, 2 x 9216 x 1280 35.1 and 40.4; without an activation 30.5 and 27.6, 18.2 and 19.7, 33.0 and 30.3).
   if (s.smem > 110 * 1024 && blocks * s.cluster > 148) s.ok = false;
   return s;
 }
@@ -1156,7 +1160,9 @@ static dgq_status gn_values(GnArgs& a, int B, cudaStream_t stream) {
   const int threads = (a.lines * a.nvec + 31) / 32 * 32;
   const int step = 4 * a.lines, rounds = (int)(((int64_t)B * a.P + 444ll * step - 1) / (444ll * step));  // three blocks for each multiprocessor
   a.rows = (int)std::min<int64_t>((int64_t)rounds * step, 1 << 30);
-  a.past = (int64_t)B * a.P * a.C >= 24 << 20;  // (1 x 262144 x 128: 49.8 -> 46.6 us)
+  // (without an activation 8 x 4096 x 960 38.4 -> 37.0 us, 4 x 65536 x 128 39.7 -> 38.8, 1 x 262144 x 128 41.2 -> 40.7; with a SiLU, below and from twice
+  // that size on the same to 0.5 % either way)
+  a.past = (int64_t)B * a.P * a.C >= 24 << 20;
   DGQ_CUDA_OK(gn_launch(gn_values_kernel<BF, SILU>, dim3((a.P - 1) / a.rows + 1, B), threads,
                         a.n_groups * sizeof(double2) + (size_t)threads * GN_RING * 16, 1, stream, a, done));
   return DGQ_OK;
